@@ -19,7 +19,7 @@
  *    outputs.  Calls on distinct streams may run concurrently.
  *  - Every call returns an MPQ_* status; mpq_last_error() describes the
  *    last failure of the calling thread.  No C++ exception crosses the ABI.
- *  - Inputs must be finite.
+ *  - Inputs must be finite (but for the microscaled calls, mpq_mx_*).
  *
  * Codes and scales (readings of the paper, shared with the test oracle)
  *  - bits b in [2, 8]; codes are the integers [-M, M] with M = 2^(b-1) - 1,
@@ -417,6 +417,166 @@ typedef struct mpq_int_layer {
 } mpq_int_layer;
 int mpq_integer_forward_layers(const mpq_int_layer *layers, int n_layers, int max_points, int p,
                                void *stream);
+
+/*
+ * Microscaled formats: what a quantized language model is served from.
+ *
+ * A block of MPQ_MX_BLOCK = 32 consecutive elements of a row shares the power
+ * of two 2^(s - 127), s one byte; the element with code c stands for
+ * value(c) * 2^(s - 127).
+ *   MPQ_MX_FP4  E2M1: 1 sign bit, 2 exponent bits (bias 1), 1 mantissa bit:
+ *               0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; two codes a
+ *               byte, the even element in the low half.
+ *   MPQ_MX_FP8  E4M3: 1 sign bit, 4 exponent bits (bias 7), 3 mantissa bits,
+ *               largest 448 (the codes 0x7f and 0xff are no numbers and are
+ *               not produced).
+ * Quantization of a block with largest magnitude a: s = floor(log2 a) + 127 -
+ * (2 for fp4, 8 for fp8), at least 0; each x / 2^(s - 127) is rounded to the
+ * nearest element, ties to the even mantissa, magnitudes past the largest
+ * element to it.  a = 0: s = 0.  A block that holds an infinity or a NaN has
+ * s = 255 and codes 0, and stands for NaN throughout; other blocks are not
+ * affected (these calls alone take inputs that are not finite).
+ *
+ * A dtype argument is MPQ_F32, MPQ_F16 or MPQ_BF16.  Strides (ld, *_stride)
+ * are in elements; the innermost dimension is contiguous; matrices of a dtype
+ * need only be aligned to their element.  Code arrays are 16-byte aligned,
+ * fp4 rows' scale arrays and caches' scale arrays 4-byte aligned.  A value
+ * past f16's range is rounded to f16 as the hardware does (to infinity).
+ *
+ * Rows of an output do not overlap: where it has several rows, their stride is
+ * at least their length.
+ *
+ * fp4 rows: a row of d elements is held as D = ceil(d / 128) 128 elements,
+ * zeros past d: codes [rows][D / 2], scales [rows][D / 32].
+ */
+#define MPQ_F32 0
+#define MPQ_F16 1
+#define MPQ_BF16 2
+#define MPQ_MX_FP4 0
+#define MPQ_MX_FP8 1
+#define MPQ_MX_BLOCK 32
+#define MPQ_MX_ROW 128
+#define MPQ_MX_MAX_D 4194304        /* d of fp4 rows */
+#define MPQ_MX_MAX_N 1048576        /* tokens of a product */
+#define MPQ_MX_MAX_HEAD_DIM 256
+#define MPQ_MX_MAX_TOKENS 536870912 /* tokens of one sequence: columns of the page table times page_size */
+
+/*
+ * mpq_mx_quantize - rows to fp4 blocks.
+ *   X      [rows][ld] of dtype, the first d of each row (input); ld >= d.
+ *   codes  [rows][D / 2], scales [rows][D / 32] (outputs).
+ *   rows >= 0, 1 <= d <= MPQ_MX_MAX_D.
+ * mpq_mx_dequantize - the values that they stand for, rounded to dtype (exact
+ * in fp32 and bf16).  Y [rows][ld] of dtype (output).
+ * Errors: MPQ_ERR_INVALID_ARG, MPQ_ERR_HIP.
+ */
+int mpq_mx_quantize(const void *X, int dtype, int64_t rows, int64_t d, int64_t ld, uint8_t *codes,
+                    uint8_t *scales, void *stream);
+int mpq_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t d, void *Y, int dtype,
+                      int64_t ld, void *stream);
+
+/*
+ * mpq_mx_product - Y = X W^T + b of two matrices of fp4 rows, on the 4-bit
+ * matrix cores: products of elements and block scales are exact, sums fp32, Y
+ * rounded once.
+ *   x_codes, x_scales  [n] rows of d (inputs): the tokens.
+ *   w_codes, w_scales  [c_out] rows of d (inputs): the weights.
+ *   bias_opt           NULL or [c_out] fp32 (input), added in fp32.
+ *   Y                  [n][ld] of dtype (output), ld >= c_out.
+ *   0 <= n <= MPQ_MX_MAX_N, c_out >= 0.
+ *
+ * mpq_mx_linear - Y = Q(X) W^T + b: the tokens X [n][x_ld] of x_dtype are
+ * quantized as mpq_mx_quantize does (bitwise the result of the two calls).
+ *   workspace_opt      NULL, or a DEVICE buffer (16-byte aligned) of at least
+ *                      mpq_mx_linear_workspace(n, c_out, d) bytes, which the call
+ *                      overwrites; it may be reused by the next call on the
+ *                      same stream.  NULL: stream-ordered scratch of the
+ *                      library (MPQ_WORKSPACE_LIMIT applies).  With a
+ *                      workspace the call allocates nothing and can be captured.
+ * mpq_mx_linear_workspace returns the size (>= 0), or a negative status.
+ * Errors: MPQ_ERR_INVALID_ARG, MPQ_ERR_NOMEM, MPQ_ERR_HIP.
+ */
+int mpq_mx_product(const uint8_t *x_codes, const uint8_t *x_scales, int64_t n, const uint8_t *w_codes,
+                   const uint8_t *w_scales, int64_t c_out, int64_t d, const float *bias_opt, void *Y, int dtype,
+                   int64_t ld, void *stream);
+int64_t mpq_mx_linear_workspace(int64_t n, int64_t c_out, int64_t d);
+int mpq_mx_linear(const void *X, int x_dtype, int64_t n, int64_t x_ld, const uint8_t *w_codes,
+                  const uint8_t *w_scales, int64_t c_out, int64_t d, const float *bias_opt, void *Y, int dtype,
+                  int64_t ld, void *workspace_opt, int64_t workspace_bytes, void *stream);
+
+/*
+ * A paged cache of keys and values, quantized in blocks along each head's
+ * dimensions.  With nb = ceil(head_dim / 32) and R the bytes of 32 nb codes
+ * (16 nb for fp4, 32 nb for fp8; dimensions past head_dim are zeros):
+ *   k_codes, v_codes    [n_pages][kv_heads][page_size][R]
+ *   k_scales, v_scales  [n_pages][kv_heads][nb][page_size]
+ * The caller owns the arrays (DEVICE pointers in a HOST struct, read before
+ * the call returns) and the pages.  Slot p * page_size + i is place i of
+ * page p.
+ *   n_pages >= 1; page_size a multiple of 16; 1 <= head_dim <=
+ *   MPQ_MX_MAX_HEAD_DIM; kv_heads >= 1; n_pages * page_size < 2^40.
+ */
+typedef struct mpq_mx_cache {
+    uint8_t *k_codes, *v_codes;
+    uint8_t *k_scales, *v_scales;
+    int64_t n_pages;
+    int32_t page_size, kv_heads, head_dim;
+    int32_t format; /* MPQ_MX_FP4 or MPQ_MX_FP8 */
+} mpq_mx_cache;
+
+/*
+ * mpq_mx_cache_write - quantizes the keys and values of n tokens into their
+ * slots.  mpq_mx_cache_read - the values held at n slots, rounded to dtype.
+ *   K, V    [n][kv_heads][head_dim] of dtype, with the strides of tokens and
+ *           heads (inputs of the write, outputs of the read).
+ *   slots   [n] int64 (DEVICE, input).  The write skips a token whose slot
+ *           is outside [0, n_pages * page_size); the read gives zeros there.
+ *           The slots of one write are distinct.
+ * Errors: MPQ_ERR_INVALID_ARG, MPQ_ERR_HIP.
+ */
+int mpq_mx_cache_write(const mpq_mx_cache *cache, const void *K, int64_t k_stride, int64_t k_head_stride,
+                       const void *V, int64_t v_stride, int64_t v_head_stride, int dtype, int64_t n,
+                       const int64_t *slots, void *stream);
+int mpq_mx_cache_read(const mpq_mx_cache *cache, void *K, int64_t k_stride, int64_t k_head_stride, void *V,
+                      int64_t v_stride, int64_t v_head_stride, int dtype, int64_t n, const int64_t *slots,
+                      void *stream);
+
+/*
+ * mpq_mx_attend - attention of one new token of each sequence over its
+ * cached tokens:
+ *   O[b][h] = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale Q[b][h] . k_j),
+ * j over the tokens [max(0, len - window), len) of sequence b (window = 0:
+ * all), k_j and v_j the held values of cache head h / (q_heads / kv_heads).
+ * Token j is place j % page_size of page page_table[b][j / page_size].
+ *   Q, O        [batch][q_heads][head_dim] of dtype, with the strides of
+ *               sequences and heads (input, output).
+ *   q_heads     a multiple of kv_heads.
+ *   page_table  [batch][table_ld] int32 (DEVICE), its first max_pages columns
+ *               used; entries past a sequence's last page are not read as
+ *               pages.  A token whose entry is outside [0, n_pages) takes no
+ *               part.
+ *   lengths     [batch] int32 (DEVICE): len, the new token included when its key
+ *               was written; taken as at most max_pages * page_size (which is at
+ *               most MPQ_MX_MAX_TOKENS), a negative one as 0.
+ *   scale       finite.
+ *   lse_opt     NULL or [batch][q_heads] fp32 (output): log sum_j p_j.
+ * A sequence without tokens has O = 0 and lse = -infinity.  What the cache
+ * holds outside the tokens named, NaN included, has no influence.  Sums and
+ * softmax statistics are fp32; p_j enters the matrix cores as two or three
+ * bf16 pieces (relative error 2^-16 for 16-bit dtypes, 2^-24 for fp32).
+ *   workspace_opt, workspace_bytes  as for mpq_mx_linear, of at least
+ *               mpq_mx_attend_workspace(cache, batch, q_heads, max_pages)
+ *               bytes (enough for any window).
+ * Where a sequence is cut into pieces follows from batch, max_pages, window
+ * and the heads, and so do the last bits of its results; they do not depend on
+ * the other sequences' contents.
+ * Errors: MPQ_ERR_INVALID_ARG, MPQ_ERR_NOMEM, MPQ_ERR_HIP.
+ */
+int64_t mpq_mx_attend_workspace(const mpq_mx_cache *cache, int64_t batch, int64_t q_heads, int64_t max_pages);
+int mpq_mx_attend(const mpq_mx_cache *cache, const void *Q, int64_t q_stride, int64_t q_head_stride, int dtype,
+                  int64_t batch, int64_t q_heads, const int32_t *page_table, int64_t table_ld, int64_t max_pages,
+                  const int32_t *lengths, int64_t window, float scale, void *O, int64_t o_stride,
+                  int64_t o_head_stride, float *lse_opt, void *workspace_opt, int64_t workspace_bytes, void *stream);
 
 /*
  * Per-launch timing (instrumentation, not part of the method).  While it is

@@ -19,6 +19,10 @@ namespace {
 
 thread_local std::string g_last_error;
 
+}  // namespace
+
+namespace mpq {
+
 int fail(int code, const char *fmt, ...)
 {
     char buf[512];
@@ -34,6 +38,13 @@ int hip_fail(hipError_t e, const char *what)
 {
     return fail(MPQ_ERR_HIP, "%s: %s (%d)", what, hipGetErrorString(e), (int)e);
 }
+
+}  // namespace mpq
+
+namespace {
+
+using mpq::fail;
+using mpq::hip_fail;
 
 // Largest dynamic LDS a workgroup may use on the current device (queried
 // once per device).

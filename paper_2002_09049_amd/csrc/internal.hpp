@@ -8,6 +8,11 @@
 
 namespace mpq {
 
+// Keep a failure's text for mpq_last_error() of the calling thread and return
+// its status.
+int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+int hip_fail(hipError_t e, const char *what);
+
 // Brackets one kernel launch with events on its stream while timing is on
 // (mpq_timing_enable); otherwise does nothing.
 class LaunchTimer {
@@ -304,5 +309,66 @@ static_assert(sizeof(IntGroup) <= 4096, "kernel arguments");
 constexpr int kIntModes = 3;
 int int_forward_mode(const IntLayer &L);
 hipError_t launch_int_forward(IntGroup &g, int mode, hipStream_t s);
+
+// Microscaled operators (mpq_mx_*; formats in mx.hpp).  A dtype is an
+// MPQ_F32, MPQ_F16 or MPQ_BF16.
+inline int64_t mx_row(int64_t d) { return (d + 127) / 128 * 128; }   // elements of a padded row of fp4 codes
+
+hipError_t launch_mx_quantize(const void *X, int dtype, int64_t rows, int64_t d, int64_t ld, uint8_t *codes,
+                              uint8_t *scales, hipStream_t s);
+hipError_t launch_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t d, void *Y,
+                                int dtype, int64_t ld, hipStream_t s);
+
+struct MxProduct {
+    const uint8_t *xc, *xs;   // [n][16 nb], [n][nb]
+    const uint8_t *wc, *ws;   // [c][16 nb], [c][nb]
+    const float *bias;        // [c] or nullptr
+    void *Y;                  // [n][ldy]
+    int dtype;
+    int nb;                   // blocks of a row, a multiple of four
+    int64_t n, c, ldy;
+};
+hipError_t launch_mx_product(const MxProduct &p, hipStream_t s);
+
+struct MxCacheView {
+    uint8_t *k, *v;     // [n_pages][heads][page][row bytes]
+    uint8_t *ks, *vs;   // [n_pages][heads][nb][page]
+    int64_t n_pages;
+    int page, heads, dim, nb, fmt;   // nb = ceil(dim / 32)
+};
+struct MxRows {
+    void *K, *V;                               // [tokens][heads][dim], strides in elements
+    int64_t k_tok, k_head, v_tok, v_head;
+    int dtype;
+};
+hipError_t launch_mx_cache_write(const MxCacheView &c, const MxRows &r, int64_t tokens, const int64_t *slots,
+                                 hipStream_t s);
+hipError_t launch_mx_cache_read(const MxCacheView &c, const MxRows &r, int64_t tokens, const int64_t *slots,
+                                hipStream_t s);
+
+struct MxAttend {
+    MxCacheView c;
+    const void *Q;              // [batch][q_heads][dim]
+    int64_t q_batch, q_head;    // strides in elements
+    void *O;
+    int64_t o_batch, o_head;
+    int dtype;                  // of Q and O
+    float *lse;                 // [batch][q_heads] or nullptr
+    const int32_t *table;       // [batch][table_ld]
+    int64_t table_ld;
+    const int32_t *lengths;     // [batch]
+    int64_t batch;
+    int q_heads, group;         // group = q_heads / c.heads
+    int most;                   // tokens that the table's columns hold
+    int window;                 // 0: none
+    float scale;
+    // set by mx_attend_plan: a sequence's tokens in pieces of `piece`, at most
+    // `pieces`; with more than one, part holds their results
+    int piece, pieces;
+    float *part;
+};
+// Fills piece and pieces; returns the bytes of part.
+size_t mx_attend_plan(MxAttend &a);
+hipError_t launch_mx_attend(const MxAttend &a, hipStream_t s);
 
 }  // namespace mpq

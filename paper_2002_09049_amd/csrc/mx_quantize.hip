@@ -1,0 +1,101 @@
+// Rows to fp4 blocks and back (mpq_mx_quantize, mpq_mx_dequantize).
+//
+// Both stream: a thread holds eight consecutive elements, so the four lanes
+// of a quad hold a block and its largest magnitude takes two DPP steps.  A
+// workgroup takes 2048 consecutive elements of the rows laid end to end
+// (each row w elements, w a multiple of 128 at or above d), whatever their
+// length, and only its first element's row takes a 64-bit division.
+#include "mpq.h"
+#include "mx.hpp"
+
+namespace mpq {
+
+namespace {
+
+constexpr int kThreads = 256, kPerThread = 8, kElems = kThreads * kPerThread;
+
+// The row and the place in it of this thread's eight elements.
+__device__ __forceinline__ void place(int w, int64_t &row, int &j)
+{
+    const int64_t first = (int64_t)blockIdx.x * kElems;
+    const int64_t row0 = first / w;
+    const uint32_t off = (uint32_t)(first - row0 * w) + kPerThread * threadIdx.x;
+    row = row0 + off / (uint32_t)w;
+    j = (int)(off % (uint32_t)w);
+}
+
+template <class T>
+__global__ void __launch_bounds__(kThreads) mx_quantize_kernel(const T *X, int64_t rows, int d, int64_t ld, int w,
+                                                               uint8_t *codes, uint8_t *scales)
+{
+    int64_t row;
+    int j;
+    place(w, row, j);
+    if (row >= rows) return;   // whole quads: w is a multiple of 32
+    float x[8];
+    load8(X + row * ld + j, d - j, x);
+    const uint32_t s = mx_scale_byte<kFp4>(quad_max(largest_bits(x)));
+    uint32_t c[1];
+    mx_codes<kFp4>(x, s, c);
+    *(uint32_t *)(codes + row * (w / 2) + j / 2) = c[0];
+    if (j % kMxBlock == 0) scales[row * (w / kMxBlock) + j / kMxBlock] = (uint8_t)s;
+}
+
+template <class T>
+__global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t *codes, const uint8_t *scales,
+                                                                 int64_t rows, int d, int w, T *Y, int64_t ld)
+{
+    int64_t row;
+    int j;
+    place(w, row, j);
+    if (row >= rows || j >= d) return;
+    const uint32_t c[1] = {*(const uint32_t *)(codes + row * (w / 2) + j / 2)};
+    const uint32_t s = scales[row * (w / kMxBlock) + j / kMxBlock];
+    float x[8];
+    mx_values<kFp4>(c, s, x);
+    store8(Y + row * ld + j, d - j, x);
+}
+
+}  // namespace
+
+hipError_t launch_mx_quantize(const void *X, int dtype, int64_t rows, int64_t d, int64_t ld, uint8_t *codes,
+                              uint8_t *scales, hipStream_t s)
+{
+    const int64_t w = mx_row(d), blocks = (rows * w + kElems - 1) / kElems;
+    if (blocks <= 0) return hipSuccess;
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    LaunchTimer timer(s, "mx_quantize_kernel");
+    const dim3 grid((unsigned)blocks), threads(kThreads);
+    if (dtype == MPQ_F32)
+        hipLaunchKernelGGL(mx_quantize_kernel<float>, grid, threads, 0, s, (const float *)X, rows, (int)d, ld, (int)w,
+                           codes, scales);
+    else if (dtype == MPQ_F16)
+        hipLaunchKernelGGL(mx_quantize_kernel<_Float16>, grid, threads, 0, s, (const _Float16 *)X, rows, (int)d, ld,
+                           (int)w, codes, scales);
+    else
+        hipLaunchKernelGGL(mx_quantize_kernel<__bf16>, grid, threads, 0, s, (const __bf16 *)X, rows, (int)d, ld,
+                           (int)w, codes, scales);
+    return hipGetLastError();
+}
+
+hipError_t launch_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t d, void *Y,
+                                int dtype, int64_t ld, hipStream_t s)
+{
+    const int64_t w = mx_row(d), blocks = (rows * w + kElems - 1) / kElems;
+    if (blocks <= 0) return hipSuccess;
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    LaunchTimer timer(s, "mx_dequantize_kernel");
+    const dim3 grid((unsigned)blocks), threads(kThreads);
+    if (dtype == MPQ_F32)
+        hipLaunchKernelGGL(mx_dequantize_kernel<float>, grid, threads, 0, s, codes, scales, rows, (int)d, (int)w,
+                           (float *)Y, ld);
+    else if (dtype == MPQ_F16)
+        hipLaunchKernelGGL(mx_dequantize_kernel<_Float16>, grid, threads, 0, s, codes, scales, rows, (int)d, (int)w,
+                           (_Float16 *)Y, ld);
+    else
+        hipLaunchKernelGGL(mx_dequantize_kernel<__bf16>, grid, threads, 0, s, codes, scales, rows, (int)d, (int)w,
+                           (__bf16 *)Y, ld);
+    return hipGetLastError();
+}
+
+}  // namespace mpq

@@ -33,7 +33,15 @@ EXPORTS = ("mpq_fit_layer", "mpq_fit_layer_dense", "mpq_fit_layers", "mpq_fit_ma
            "mpq_reconstruct_layers", "mpq_last_error", "mpq_timing_enable", "mpq_timing_only", "mpq_timing_read",
            "mpq_fit_kernel_of", "mpq_quantize_layers", "mpq_fit_layer_calib",
            "mpq_fit_layers_calib", "mpq_integer_scales", "mpq_integer_forward",
-           "mpq_integer_forward_layers", "mpq_fit_layers_ex", "mpq_output_error_noalloc")
+           "mpq_integer_forward_layers", "mpq_fit_layers_ex", "mpq_output_error_noalloc",
+           "mpq_mx_quantize", "mpq_mx_dequantize", "mpq_mx_product", "mpq_mx_linear",
+           "mpq_mx_linear_workspace", "mpq_mx_cache_write", "mpq_mx_cache_read", "mpq_mx_attend",
+           "mpq_mx_attend_workspace")
+
+MX_BLOCK = 32
+MX_ROW = 128
+MX_FORMATS = {"fp4": 0, "fp8": 1}
+_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
 class Layer(ctypes.Structure):
@@ -59,6 +67,15 @@ class IntLayer(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("A", ctypes.c_void_p), ("counts", ctypes.c_void_p),
                 ("c_out", ctypes.c_int64), ("d", ctypes.c_int64), ("X", ctypes.c_void_p),
                 ("n", ctypes.c_int64), ("Y", ctypes.c_void_p)]
+
+
+class MXCacheView(ctypes.Structure):
+    """struct mpq_mx_cache (include/mpq.h)."""
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("format", ctypes.c_int32)]
 
 
 _lib = None
@@ -116,6 +133,25 @@ def load(path: str = LIB_PATH):
     lib.mpq_output_error_layers.restype = i32
     lib.mpq_reconstruct_layers.argtypes = [P, i32, i32, P]
     lib.mpq_reconstruct_layers.restype = i32
+    lib.mpq_mx_quantize.argtypes = [P, i32, i64, i64, i64, P, P, P]
+    lib.mpq_mx_quantize.restype = i32
+    lib.mpq_mx_dequantize.argtypes = [P, P, i64, i64, P, i32, i64, P]
+    lib.mpq_mx_dequantize.restype = i32
+    lib.mpq_mx_product.argtypes = [P, P, i64, P, P, i64, i64, P, P, i32, i64, P]
+    lib.mpq_mx_product.restype = i32
+    lib.mpq_mx_linear_workspace.argtypes = [i64, i64, i64]
+    lib.mpq_mx_linear_workspace.restype = i64
+    lib.mpq_mx_linear.argtypes = [P, i32, i64, i64, P, P, i64, i64, P, P, i32, i64, P, i64, P]
+    lib.mpq_mx_linear.restype = i32
+    lib.mpq_mx_cache_write.argtypes = [P, P, i64, i64, P, i64, i64, i32, i64, P, P]
+    lib.mpq_mx_cache_write.restype = i32
+    lib.mpq_mx_cache_read.argtypes = [P, P, i64, i64, P, i64, i64, i32, i64, P, P]
+    lib.mpq_mx_cache_read.restype = i32
+    lib.mpq_mx_attend_workspace.argtypes = [P, i64, i64, i64]
+    lib.mpq_mx_attend_workspace.restype = i64
+    lib.mpq_mx_attend.argtypes = [P, P, i64, i64, i32, i64, i64, P, i64, i64, P, i64, f32, P, i64, i64,
+                                  P, P, i64, P]
+    lib.mpq_mx_attend.restype = i32
     lib.mpq_last_error.argtypes = []
     lib.mpq_last_error.restype = ctypes.c_char_p
     lib.mpq_timing_enable.argtypes = [i32]
@@ -318,6 +354,242 @@ def integer_forward_layers(layers, max_points: int, p: int, stream=None):
         L.c_out, L.d, L.n = C, d, X.shape[0]
     _check(load().mpq_integer_forward_layers(ctypes.addressof(arr), len(layers), max_points, int(p),
                                              _stream(stream)))
+
+
+def _mx_dtype(dtype, name: str) -> int:
+    if dtype not in _DTYPES:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16 (got {dtype})")
+    return _DTYPES[dtype]
+
+
+def _rows(x: torch.Tensor, name: str):
+    """(pointer, dtype number, row stride) of a 2-D device tensor whose rows
+    are contiguous."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise ValueError(f"{name} must be a ROCm device tensor")
+    if x.dim() != 2:
+        raise ValueError(f"{name} must be 2-D")
+    dt = _mx_dtype(x.dtype, name)
+    if x.shape[1] > 1 and x.stride(1) != 1:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    ld = x.stride(0) if x.shape[0] > 1 else max(x.shape[1], 1)
+    return x.data_ptr(), dt, ld
+
+
+def _heads(x: torch.Tensor, shape, name: str):
+    """(pointer, stride of dimension 0, of dimension 1) of a 3-D device tensor
+    whose last dimension is contiguous."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise ValueError(f"{name} must be a ROCm device tensor")
+    if tuple(x.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)} (got {tuple(x.shape)})")
+    if x.shape[2] > 1 and x.stride(2) != 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    return x.data_ptr(), x.stride(0), x.stride(1)
+
+
+def _fp4(codes: torch.Tensor, scales: torch.Tensor, d: int, name: str):
+    wide = -(-d // MX_ROW) * MX_ROW
+    if codes.dim() != 2 or codes.shape[1] != wide // 2 or scales.shape != (codes.shape[0], wide // MX_BLOCK):
+        raise ValueError(f"{name}: codes and scales do not hold rows of {d}")
+    return _dev(codes, torch.uint8, f"{name} codes"), _dev(scales, torch.uint8, f"{name} scales")
+
+
+def _space(workspace):
+    if workspace is None:
+        return None, 0
+    return _dev(workspace, torch.uint8, "workspace"), workspace.numel()
+
+
+def _out(out, shape, dtype, device, name: str):
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(out.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)} (got {tuple(out.shape)})")
+    return out
+
+
+def mx_quantize(X: torch.Tensor, stream=None, out=None):
+    """mpq_mx_quantize: rows X [r, d] (fp32, fp16 or bf16; rows may be apart)
+    to fp4 blocks.  Returns (codes [r, D / 2] uint8, scales [r, D / 32] uint8),
+    D = d rounded up to a multiple of 128."""
+    ptr, dt, ld = _rows(X, "X")
+    r, d = X.shape
+    wide = -(-d // MX_ROW) * MX_ROW
+    if out is None:
+        out = (torch.empty((r, wide // 2), dtype=torch.uint8, device=X.device),
+               torch.empty((r, wide // MX_BLOCK), dtype=torch.uint8, device=X.device))
+    codes, scales = out
+    cp, sp = _fp4(codes, scales, d, "out")
+    if codes.shape[0] != r:
+        raise ValueError(f"out must hold {r} rows")
+    _check(load().mpq_mx_quantize(ptr, dt, r, d, ld, cp, sp, _stream(stream)))
+    return codes, scales
+
+
+def mx_dequantize(codes: torch.Tensor, scales: torch.Tensor, d: int, dtype=torch.float32, stream=None,
+                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """mpq_mx_dequantize: the values [r, d] that fp4 blocks stand for."""
+    cp, sp = _fp4(codes, scales, d, "rows")
+    Y = _out(out, (codes.shape[0], d), dtype, codes.device, "out")
+    yp, dt, ld = _rows(Y, "out")
+    _check(load().mpq_mx_dequantize(cp, sp, codes.shape[0], d, yp, dt, ld, _stream(stream)))
+    return Y
+
+
+def mx_product(x_codes: torch.Tensor, x_scales: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
+               d: int, bias: Optional[torch.Tensor] = None, dtype=torch.float32, stream=None,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """mpq_mx_product: Y [n, c] = X W^T + bias of two matrices of fp4 rows of d
+    (tokens X, weights W), as mx_quantize gives them."""
+    xc, xs = _fp4(x_codes, x_scales, d, "tokens")
+    wc, ws = _fp4(codes, scales, d, "weights")
+    n, c = x_codes.shape[0], codes.shape[0]
+    if bias is not None and bias.shape != (c,):
+        raise ValueError(f"bias must be ({c},)")
+    Y = _out(out, (n, c), dtype, codes.device, "out")
+    yp, dt, ld = _rows(Y, "out")
+    _check(load().mpq_mx_product(xc, xs, n, wc, ws, c, d,
+                                 None if bias is None else _dev(bias, torch.float32, "bias"), yp, dt, ld,
+                                 _stream(stream)))
+    return Y
+
+
+def mx_linear_workspace(n: int, c: int, d: int) -> int:
+    """mpq_mx_linear_workspace: the bytes of a workspace of mx_linear."""
+    v = load().mpq_mx_linear_workspace(n, c, d)
+    if v < 0:
+        _check(int(v))
+    return int(v)
+
+
+def mx_linear(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bias: Optional[torch.Tensor] = None,
+              dtype=None, stream=None, out: Optional[torch.Tensor] = None, workspace=None) -> torch.Tensor:
+    """mpq_mx_linear: Y [n, c] = Q(X) W^T + bias, X [n, d] quantized to fp4 in
+    the call, W as mx_quantize gives it.  dtype of Y: X's unless given.
+    workspace: an uint8 device tensor of mx_linear_workspace(n, c, d) bytes, or
+    None for the library's own scratch."""
+    xp, xt, x_ld = _rows(X, "X")
+    n, d = X.shape
+    wc, ws = _fp4(codes, scales, d, "weights")
+    c = codes.shape[0]
+    if bias is not None and bias.shape != (c,):
+        raise ValueError(f"bias must be ({c},)")
+    Y = _out(out, (n, c), X.dtype if dtype is None else dtype, X.device, "out")
+    yp, dt, ld = _rows(Y, "out")
+    wp, wn = _space(workspace)
+    _check(load().mpq_mx_linear(xp, xt, n, x_ld, wc, ws, c, d,
+                                None if bias is None else _dev(bias, torch.float32, "bias"), yp, dt, ld, wp, wn,
+                                _stream(stream)))
+    return Y
+
+
+class MXCache:
+    """A paged block-scaled cache of keys and values (struct mpq_mx_cache).
+
+    k_codes, v_codes [pages, kv_heads, page_size, row bytes] and k_scales,
+    v_scales [pages, kv_heads, ceil(head_dim / 32), page_size] are uint8 device
+    tensors, kept for the life of the cache; fmt "fp4" or "fp8".
+    MXCache.empty allocates them."""
+
+    def __init__(self, k_codes, v_codes, k_scales, v_scales, head_dim: int, fmt: str):
+        if fmt not in MX_FORMATS:
+            raise ValueError(f"fmt must be one of {sorted(MX_FORMATS)} (got {fmt!r})")
+        nb = -(-head_dim // MX_BLOCK)
+        if k_codes.dim() != 4:
+            raise ValueError("k_codes must be 4-D")
+        pages, heads, page = k_codes.shape[:3]
+        for x, name, last in ((k_codes, "k_codes", (page, nb * (16 if fmt == "fp4" else 32))),
+                              (v_codes, "v_codes", (page, nb * (16 if fmt == "fp4" else 32))),
+                              (k_scales, "k_scales", (nb, page)), (v_scales, "v_scales", (nb, page))):
+            if tuple(x.shape) != (pages, heads) + last:
+                raise ValueError(f"{name} must be {(pages, heads) + last} (got {tuple(x.shape)})")
+        self.tensors = (k_codes, v_codes, k_scales, v_scales)
+        self.pages, self.kv_heads, self.page_size = pages, heads, page
+        self.head_dim, self.fmt = head_dim, fmt
+        self.view = MXCacheView(*(_dev(x, torch.uint8, "cache") for x in self.tensors), pages, page, heads,
+                                head_dim, MX_FORMATS[fmt])
+        self._at = ctypes.addressof(self.view)
+
+    @classmethod
+    def empty(cls, pages: int, page_size: int, kv_heads: int, head_dim: int, fmt: str = "fp8", device="cuda"):
+        """A cache of `pages` empty pages."""
+        if fmt not in MX_FORMATS:
+            raise ValueError(f"fmt must be one of {sorted(MX_FORMATS)} (got {fmt!r})")
+        nb = -(-head_dim // MX_BLOCK)
+        row = nb * (16 if fmt == "fp4" else 32)
+        shapes = [(pages, kv_heads, page_size, row)] * 2 + [(pages, kv_heads, nb, page_size)] * 2
+        return cls(*(torch.zeros(s, dtype=torch.uint8, device=device) for s in shapes), head_dim, fmt)
+
+    def write(self, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, stream=None):
+        """mpq_mx_cache_write: quantizes K, V [n, kv_heads, head_dim] into the
+        slots [n] (int64; page * page_size + place, distinct; a token whose
+        slot is not of the cache is skipped)."""
+        n = slots.numel()
+        shape = (n, self.kv_heads, self.head_dim)
+        kp, kt, kh = _heads(K, shape, "K")
+        vp, vt, vh = _heads(V, shape, "V")
+        if K.dtype != V.dtype:
+            raise ValueError("K and V must have one dtype")
+        _check(load().mpq_mx_cache_write(self._at, kp, kt, kh, vp, vt, vh, _mx_dtype(K.dtype, "K"), n,
+                                         _dev(slots, torch.int64, "slots"), _stream(stream)))
+
+    def read(self, slots: torch.Tensor, dtype=torch.float32, stream=None, out=None):
+        """mpq_mx_cache_read: the keys and values [n, kv_heads, head_dim] held
+        at the slots, as (K, V); zeros for a slot that is not of the cache."""
+        n = slots.numel()
+        shape = (n, self.kv_heads, self.head_dim)
+        K, V = (torch.empty(shape, dtype=dtype, device=slots.device) for _ in "KV") if out is None else out
+        kp, kt, kh = _heads(K, shape, "K")
+        vp, vt, vh = _heads(V, shape, "V")
+        if K.dtype != V.dtype:
+            raise ValueError("K and V must have one dtype")
+        _check(load().mpq_mx_cache_read(self._at, kp, kt, kh, vp, vt, vh, _mx_dtype(K.dtype, "dtype"), n,
+                                        _dev(slots, torch.int64, "slots"), _stream(stream)))
+        return K, V
+
+    def attend_workspace(self, batch: int, q_heads: int, max_pages: int) -> int:
+        """mpq_mx_attend_workspace: the bytes of a workspace of attend."""
+        v = load().mpq_mx_attend_workspace(self._at, batch, q_heads, max_pages)
+        if v < 0:
+            _check(int(v))
+        return int(v)
+
+    def attend(self, Q: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+               scale: Optional[float] = None, window: int = 0, with_lse: bool = False, stream=None,
+               out: Optional[torch.Tensor] = None, workspace=None):
+        """mpq_mx_attend: attention of one new token of each sequence, Q
+        [batch, q_heads, head_dim], over the lengths[b] tokens in the pages
+        page_table[b] (int32 both); window > 0: over the last `window` of them.
+        scale: 1 / sqrt(head_dim) unless given.  Returns O like Q, or
+        (O, lse [batch, q_heads] fp32) with with_lse.  workspace: an uint8 device
+        tensor of attend_workspace(batch, q_heads, page_table.shape[1]) bytes,
+        or None for the library's own scratch."""
+        if Q.dim() != 3:
+            raise ValueError("Q must be 3-D [batch, q_heads, head_dim]")
+        batch, heads = Q.shape[:2]
+        shape = (batch, heads, self.head_dim)
+        qp, qb, qh = _heads(Q, shape, "Q")
+        if page_table.dim() != 2 or page_table.shape[0] != batch or (page_table.shape[1] > 1
+                                                                     and page_table.stride(1) != 1):
+            raise ValueError("page_table must be [batch, max_pages] with contiguous rows")
+        if page_table.dtype != torch.int32 or not page_table.is_cuda:
+            raise ValueError("page_table must be an int32 device tensor")
+        if lengths.shape != (batch,):
+            raise ValueError("lengths must be [batch]")
+        O = _out(out, shape, Q.dtype, Q.device, "out")
+        if O.dtype != Q.dtype:
+            raise ValueError("out must have Q's dtype")
+        op, ob, oh = _heads(O, shape, "out")
+        lse = torch.empty((batch, heads), dtype=torch.float32, device=Q.device) if with_lse else None
+        pages = page_table.shape[1]
+        ld = page_table.stride(0) if batch > 1 else pages
+        wp, wn = _space(workspace)
+        _check(load().mpq_mx_attend(self._at, qp, qb, qh, _mx_dtype(Q.dtype, "Q"), batch, heads,
+                                    page_table.data_ptr(), ld, pages, _dev(lengths, torch.int32, "lengths"),
+                                    int(window), self.head_dim ** -0.5 if scale is None else float(scale), op, ob, oh,
+                                    None if lse is None else lse.data_ptr(), wp, wn, _stream(stream)))
+        return (O, lse) if with_lse else O
 
 
 def timing_enable(on: bool = True):

@@ -1,0 +1,556 @@
+"""Microscaled operators (mpq_mx_*) through the C ABI against the plain
+64-bit implementation of mx_ref: codes, scales and held values bit for bit;
+products and attention within bounds that follow from fp32 sums.
+
+Bounds.  A product of fp4 blocks is exact, so Y errs by the sum alone: at most
+(128 + steps + 16) roundings of 2^-24 of sum |x w| (128 terms inside an
+instruction, one addition per step of 128, the wavefronts' sums and the bias),
+and by Y's own rounding.  A score of attention errs by delta = 2^-24 ((3 D + 8)
+scale sum |q k| + 4 (|s| + max |s|)) (up to three pieces of Q; products exact),
+an exponential by 2^-22 more, P by its pieces (2^-16 for 16-bit types, else
+2^-24), and sums of n tokens by (n + 64) 2^-24: all relative to
+sum p |v| / sum p, numerator and denominator alike."""
+import numpy as np
+import pytest
+
+import mx_ref as ref
+from gpu_util import say
+
+pytestmark = pytest.mark.gpu
+
+E = 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a ROCm device"
+    from paper_2002_09049_amd import mpq
+    mpq.load()
+    yield
+
+
+def _dt(name):
+    import torch
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[name]
+
+
+def _dev(a, dtype=None):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if dtype is None else t.to(dtype)
+
+
+def _np(t):
+    import torch
+    if t.dtype == torch.bfloat16:
+        t = t.float()
+    return t.cpu().numpy()
+
+
+def _f64(t):
+    return _np(t).astype(np.float64)
+
+
+def _activations(rng, shape):
+    x = rng.standard_normal(shape) * np.exp(rng.standard_normal(shape[-1]))
+    x[rng.random(shape) < 0.02] = 0.0
+    return x
+
+
+# ------------------------------------------------------------------ fp4 rows
+
+SIZES = [(1, 1), (3, 31), (2, 32), (5, 33), (4, 127), (7, 128), (2, 129), (33, 2047), (1, 4096), (300, 40), (9, 5000)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,d", SIZES)
+def test_quantize_and_back(rows, d, dtype):
+    from paper_2002_09049_amd import mpq
+    say(f"case mx quantize {rows} x {d} {dtype}")
+    rng = np.random.default_rng(rows * 1000 + d)
+    wide = _dev(_activations(rng, (rows, d + 5)).astype(np.float32), _dt(dtype))
+    for X in (wide[:, :d].contiguous(), wide[:, 5:], wide[:, 2:d + 2]):
+        codes, scales = mpq.mx_quantize(X)
+        c, s = ref.quantize(ref.padded(_f64(X), ref.ROW), "fp4")
+        assert np.array_equal(_np(codes), ref.pack(c))
+        assert np.array_equal(_np(scales), s)
+        want = ref.values(c, s, "fp4")[:, :d]
+        for out in ("f32", "bf16"):
+            assert np.array_equal(_f64(mpq.mx_dequantize(codes, scales, d, dtype=_dt(out))), want)
+    # into the middle of wider rows, whose other columns stay
+    import torch
+    Y = torch.full((rows, d + 7), -3.0, dtype=_dt(dtype), device="cuda")
+    mpq.mx_dequantize(codes, scales, d, dtype=Y.dtype, out=Y[:, 3:d + 3])
+    y = _f64(Y)
+    assert (y[:, :3] == -3).all() and (y[:, d + 3:] == -3).all()
+    if dtype != "f16":
+        assert np.array_equal(y[:, 3:d + 3], want)
+
+
+def test_quantize_special_values():
+    """Ties, saturation, signed zeros, subnormal and huge blocks, and blocks
+    with infinities and NaN, which spoil no other block."""
+    from paper_2002_09049_amd import mpq
+    rows = []
+    grid = np.arange(-32, 33) * 0.25                  # every tie of E2M1 under a largest of 4 .. 8
+    for top in (4.0, 5.0, 6.5, 7.999):
+        for k in range(0, len(grid), 31):
+            b = np.zeros(32)
+            part = grid[k:k + 31]
+            b[:len(part)] = np.clip(part, -top, top)
+            b[31] = top
+            for e in (-126, -100, 0, 1, 100, 124):
+                rows.append(np.ldexp(b, e))
+    rows.append(np.full(32, 2.0 ** -149))
+    rows.append(np.arange(32) * 2.0 ** -149)
+    rows.append(np.arange(32) * 2.0 ** -128)
+    rows.append(np.full(32, -0.0))
+    rows.append(np.full(32, 3.4028234663852886e38))
+    x = np.array(rows)
+    flat = np.zeros((len(x) // 4 + 1, 128))
+    flat.reshape(-1, 32)[:len(x)] = x
+    bad = flat[:3].copy()
+    bad[0, 5] = np.inf
+    bad[1, 40] = np.nan
+    bad[2, 127] = -np.inf
+    flat = np.concatenate([flat, bad]).astype(np.float32)
+    say("case mx quantize special values")
+    codes, scales = mpq.mx_quantize(_dev(flat))
+    c, s = ref.quantize(flat.astype(np.float64), "fp4")
+    assert np.array_equal(_np(scales), s)
+    assert np.array_equal(_np(codes), ref.pack(c))
+    v = _f64(mpq.mx_dequantize(codes, scales, 128))
+    w = ref.values(c, s, "fp4")
+    assert np.array_equal(v, w, equal_nan=True) and np.isnan(v[-3, :32]).all() and np.isfinite(v[-3, 32:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_dequantize_every_code_and_scale(dtype):
+    from paper_2002_09049_amd import mpq
+    say(f"case mx dequantize all codes {dtype}")
+    b = np.arange(256, dtype=np.uint8)
+    codes = np.tile(b[None, :], (256, 1)).reshape(256, 4, 64).reshape(1024, 64)
+    scales = np.repeat(b, 4)[:, None].repeat(4, 1)
+    got = _f64(mpq.mx_dequantize(_dev(codes), _dev(scales), 128, dtype=_dt(dtype)))
+    want = ref.values(ref.unpack(codes), scales, "fp4")
+    with np.errstate(over="ignore"):
+        want = want.astype(np.float16 if dtype == "f16" else np.float32).astype(np.float64)
+    assert np.array_equal(got, want, equal_nan=True)
+
+
+# ------------------------------------------------------------------ products
+
+def _weights(rng, c, d):
+    W = rng.standard_normal((c, d)) * np.exp(0.5 * rng.standard_normal((c, 1))) / np.sqrt(d)
+    return ref.quantize(ref.padded(W, ref.ROW), "fp4")
+
+
+def _check_product(y, x, w, bias, dtype, nb):
+    """x, w: held values, padded."""
+    want = x @ w.T + (0 if bias is None else bias)
+    room = (128 + nb // 4 + 16) * E * (np.abs(x) @ np.abs(w).T + (0 if bias is None else np.abs(bias)))
+    room += ref.UNIT[dtype] * np.abs(want) + (2.0 ** -25 if dtype == "f16" else 0)
+    err = np.abs(y - want)
+    assert (err <= room).all(), (np.max(err / room), np.argwhere(err > room)[:4])
+
+
+PRODUCTS = [(1, 1, 1), (1, 16, 128), (1, 40, 130), (2, 17, 512), (3, 100, 513), (4, 33, 1024), (5, 16, 640),
+            (8, 64, 2047), (9, 31, 700), (15, 48, 4096), (16, 16, 96), (17, 50, 1000), (33, 70, 300), (64, 130, 2048),
+            (65, 20, 256), (77, 100, 2047), (129, 257, 384), (200, 300, 1153), (256, 256, 512), (300, 513, 128),
+            (513, 511, 640)]
+
+
+@pytest.mark.parametrize("dtype,bias", [("f32", True), ("f16", False), ("bf16", True), ("f32", False)])
+@pytest.mark.parametrize("n,c,d", PRODUCTS)
+def test_linear(n, c, d, dtype, bias):
+    import torch
+    from paper_2002_09049_amd import mpq
+    say(f"case mx linear n={n} c={c} d={d} {dtype} bias={bias}")
+    rng = np.random.default_rng(n * 7 + c * 3 + d)
+    X = _dev(_activations(rng, (n, d + 3)).astype(np.float32), _dt(dtype))[:, 3:]
+    wc, ws = _weights(rng, c, d)
+    b = rng.standard_normal(c).astype(np.float32) if bias else None
+    codes, scales = _dev(ref.pack(wc)), _dev(ws)
+    bd = None if b is None else _dev(b)
+    xq = ref.values(*ref.quantize(ref.padded(_f64(X), ref.ROW), "fp4"), "fp4")
+    w = ref.values(wc, ws, "fp4")
+    # Y inside wider rows
+    room = torch.full((n, c + 9), -7.0, dtype=_dt(dtype), device="cuda")
+    Y = mpq.mx_linear(X, codes, scales, bias=bd, out=room[:, 4:c + 4])
+    _check_product(_f64(Y), xq, w, None if b is None else b.astype(np.float64), dtype, ws.shape[1])
+    r = _np(room)
+    assert (r[:, :4] == -7).all() and (r[:, c + 4:] == -7).all()
+    # with a workspace, and as two calls: the same bits
+    space = torch.full((mpq.mx_linear_workspace(n, c, d),), 255, dtype=torch.uint8, device="cuda")
+    assert torch.equal(mpq.mx_linear(X, codes, scales, bias=bd, workspace=space), Y)
+    x2 = mpq.mx_quantize(X)
+    assert torch.equal(mpq.mx_product(*x2, codes, scales, d, bias=bd, dtype=_dt(dtype)), Y)
+    # another output type
+    Y32 = mpq.mx_linear(X, codes, scales, bias=bd, dtype=torch.float32)
+    assert torch.equal(Y32.to(_dt(dtype)), Y)
+
+
+@pytest.mark.parametrize("n", [1, 5, 40, 300])
+def test_linear_with_a_bad_token(n):
+    """A token that holds a NaN gives a row of NaN, and no other."""
+    from paper_2002_09049_amd import mpq
+    say(f"case mx linear NaN token n={n}")
+    rng = np.random.default_rng(n)
+    x = _activations(rng, (n, 300)).astype(np.float32)
+    clean = _dev(x)
+    x[n // 2, 299] = np.nan
+    wc, ws = _weights(rng, 37, 300)
+    codes, scales = _dev(ref.pack(wc)), _dev(ws)
+    y, y0 = _np(mpq.mx_linear(_dev(x), codes, scales)), _np(mpq.mx_linear(clean, codes, scales))
+    assert np.isnan(y[n // 2]).all()
+    keep = np.arange(n) != n // 2
+    assert np.array_equal(y[keep], y0[keep])
+
+
+def test_linear_extreme_scales():
+    """Scale bytes near both ends: the sums are as the formula's."""
+    from paper_2002_09049_amd import mpq
+    say("case mx linear extreme scales")
+    rng = np.random.default_rng(5)
+    for ex, ew in ((-120, 100), (100, -120), (0, -126), (60, 60)):
+        X = (rng.standard_normal((6, 256)) * 2.0 ** ex).astype(np.float32)
+        wc, ws = ref.quantize(rng.standard_normal((20, 256)) * 2.0 ** ew, "fp4")
+        xq = ref.values(*ref.quantize(X.astype(np.float64), "fp4"), "fp4")
+        w = ref.values(wc, ws, "fp4")
+        y = _f64(mpq.mx_linear(_dev(X), _dev(ref.pack(wc)), _dev(ws)))
+        want = xq @ w.T
+        room = (128 + 2 + 16) * E * (np.abs(xq) @ np.abs(w).T) + 256 * 2.0 ** -149 + E * np.abs(want)
+        assert (np.abs(y - want) <= room).all()
+
+
+# ------------------------------------------------------------------ the cache
+
+def _cache(rng, pages, page, heads, dim, fmt):
+    """A cache whose every byte is garbage (scales of 255 among it)."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    c = mpq.MXCache.empty(pages, page, heads, dim, fmt)
+    for t in c.tensors:
+        t.copy_(torch.from_numpy(rng.integers(0, 256, tuple(t.shape), dtype=np.uint8)))
+    return c
+
+
+def _held(x, fmt):
+    """The values that rows x [..., dim] are held as."""
+    c, s = ref.quantize(ref.padded(x, ref.BLOCK), fmt)
+    return ref.values(c, s, fmt)[..., :x.shape[-1]]
+
+
+CACHES = [(1, 16, 1, 32), (5, 16, 2, 64), (70, 48, 3, 80), (33, 64, 8, 128), (9, 32, 2, 1), (20, 16, 1, 100),
+          (17, 256, 5, 256), (40, 16, 2, 192), (3, 16, 1, 224)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("n,page,heads,dim", CACHES)
+def test_cache_write_and_read(n, page, heads, dim, fmt, dtype):
+    import torch
+    say(f"case mx cache n={n} page={page} heads={heads} dim={dim} {fmt} {dtype}")
+    rng = np.random.default_rng(n + page + dim)
+    pages = n // page + 3
+    cache = _cache(rng, pages, page, heads, dim, fmt)
+    before = [t.clone() for t in cache.tensors]
+    # K: [heads, n, dim + 3] seen as tokens by heads; V: part of wider rows
+    K = _dev(_activations(rng, (heads, n, dim + 3)).astype(np.float32), _dt(dtype)).transpose(0, 1)[:, :, 2:dim + 2]
+    V = _dev(_activations(rng, (n, heads + 1, dim)).astype(np.float32), _dt(dtype))[:, 1:]
+    slots = rng.permutation(pages * page)[:n].astype(np.int64)
+    told = slots.copy()
+    if n > 4:
+        told[1], told[3] = -1, pages * page      # these two tokens are skipped
+    cache.write(K, V, _dev(told))
+    kept = (told >= 0) & (told < pages * page)
+    nb = -(-dim // 32)
+    for x, codes, scales, c0, s0 in ((K, cache.tensors[0], cache.tensors[2], before[0], before[2]),
+                                     (V, cache.tensors[1], cache.tensors[3], before[1], before[3])):
+        c, s = ref.quantize(ref.padded(_f64(x), ref.BLOCK), fmt)
+        c = ref.pack(c) if fmt == "fp4" else c
+        wc, wsc = _np(c0).copy(), _np(s0).copy()
+        for i in np.nonzero(kept)[0]:
+            wc[told[i] // page, :, told[i] % page] = c[i]
+            wsc[told[i] // page, :, :, told[i] % page] = s[i].reshape(heads, nb)
+        assert np.array_equal(_np(codes), wc) and np.array_equal(_np(scales), wsc)
+    # read into strided outputs
+    out = [torch.full((heads, n, dim + 2), 9.0, dtype=_dt(dtype), device="cuda") for _ in "KV"]
+    got = cache.read(_dev(told), dtype=_dt(dtype), out=[o.transpose(0, 1)[:, :, 1:dim + 1] for o in out])
+    for x, y, o in ((K, got[0], out[0]), (V, got[1], out[1])):
+        want = np.where(kept[:, None, None], _held(_f64(x), fmt), 0.0)
+        with np.errstate(over="ignore"):
+            want = want.astype(np.float16 if dtype == "f16" else np.float32).astype(np.float64)
+        assert np.array_equal(_f64(y), want)
+        o = _np(o)
+        assert (o[..., 0] == 9).all() and (o[..., -1] == 9).all()
+
+
+def test_fp8_special_values():
+    say("case mx cache fp8 special values")
+    rng = np.random.default_rng(4)
+    ties = []
+    for e in range(-9, 9):                       # half-way points of E4M3 under a largest of 256 .. 512
+        q = 2.0 ** (max(e, -6) - 3)
+        ties += [2.0 ** e + (k + 0.5) * q for k in range(8)]
+    x = np.zeros((len(ties) // 31 + 1, 1, 32))
+    for i, v in enumerate(ties):
+        x[i // 31, 0, i % 31] = v if i % 2 else -v
+    x[:, 0, 31] = rng.choice([256.0, 300.0, 447.0, 460.0, 500.0, 511.0], len(x))
+    rows = [np.ldexp(x, e) for e in (-118, -20, 0, 119)]
+    special = np.zeros((4, 1, 32))
+    special[0, 0, 3] = np.inf
+    special[1, 0, 30] = np.nan
+    special[2, 0] = 2.0 ** -149
+    special[3, 0] = np.arange(32) * 2.0 ** -140
+    x = np.concatenate(rows + [special]).astype(np.float32)
+    n = len(x)
+    cache = _cache(rng, n // 16 + 1, 16, 1, 32, "fp8")
+    slots = _dev(np.arange(n, dtype=np.int64))
+    cache.write(_dev(x), _dev(x[::-1].copy()), slots)
+    import torch
+    k, v = cache.read(slots, dtype=torch.float32)
+    want = _held(x.astype(np.float64), "fp8")
+    assert np.array_equal(_f64(k), want, equal_nan=True)
+    assert np.array_equal(_f64(v), want[::-1], equal_nan=True)
+
+
+# ------------------------------------------------------------------ attention
+
+def _attend_case(rng, lengths, kv, group, dim, dtype, fmt, page, window=0, spare=3, extra_cols=0, layout="plain",
+                 spread=1.0):
+    """Random caches with garbage everywhere outside the sequences' tokens, one
+    call, and its check against the plain implementation."""
+    import torch
+    batch = len(lengths)
+    need = [-(-n // page) for n in lengths]
+    total = sum(need) + spare
+    cache = _cache(rng, total, page, kv, dim, fmt)
+    cols = max(max(need), 0) + extra_cols
+    table = rng.integers(-5, total + 5, (batch, cols + 2)).astype(np.int32)   # garbage past a sequence's pages
+    order = rng.permutation(total)
+    held, at = [], 0
+    for b, n in enumerate(lengths):
+        pages = order[at:at + need[b]]
+        at += need[b]
+        table[b, :need[b]] = pages
+        K, V = _activations(rng, (n, kv, dim)), rng.standard_normal((n, kv, dim)) + 0.3
+        K *= spread
+        if n:
+            slots = pages[np.arange(n) // page] * page + np.arange(n) % page
+            cache.write(_dev(K.astype(np.float32)), _dev(V.astype(np.float32)), _dev(slots.astype(np.int64)))
+        held.append((_held(K.astype(np.float32).astype(np.float64), fmt),
+                     _held(V.astype(np.float32).astype(np.float64), fmt)))
+    heads = kv * group
+    if layout == "plain":
+        Q = _dev(rng.standard_normal((batch, heads, dim)).astype(np.float32), _dt(dtype))
+    else:   # heads first, rows apart, not aligned to vectors
+        Q = _dev(rng.standard_normal((heads, batch, dim + 3)).astype(np.float32), _dt(dtype)).transpose(0, 1)[:, :, 1:dim + 1]
+    scale = dim ** -0.5
+    T = _dev(table)[:, :cols]
+    L = _dev(np.array(lengths, dtype=np.int32))
+    O, lse = cache.attend(Q, T, L, window=window, with_lse=True)
+    q, o, e = _f64(Q), _f64(O), _f64(lse)
+    piece = 2.0 ** (-24 if dtype == "f32" else -16)
+    for b, n in enumerate(lengths):
+        first = max(0, n - window) if window else 0
+        for h in range(heads):
+            k, v = held[b][0][first:n, h // group], held[b][1][first:n, h // group]
+            want, l, mag = ref.attend(q[b, h], k, v, scale)
+            if n == 0:
+                assert (o[b, h] == 0).all() and e[b, h] == -np.inf
+                continue
+            s = np.abs(k @ q[b, h]) * scale
+            delta = E * ((3 * dim + 8) * scale * (np.abs(k) @ np.abs(q[b, h])) + 4 * (s + s.max())).max() + 2.0 ** -22
+            room = (2 * delta + piece + 2 * (n - first + 64) * E) * mag + ref.UNIT[dtype] * np.abs(want)
+            if dtype == "f16":
+                room += 2.0 ** -25
+            err = np.abs(o[b, h] - want)
+            assert (err <= room).all(), (b, h, np.max(err / room))
+            assert abs(e[b, h] - l) <= delta + (n - first + 64) * E + 2.0 ** -22 * (1 + abs(l)), (b, h, e[b, h], l)
+    return cache, Q, T, L, O, lse
+
+
+ATTENDS = [
+    # lengths, kv, group, dim, page, window
+    ([1], 1, 1, 32, 16, 0),
+    ([0, 1, 2, 15, 16, 17], 2, 4, 64, 16, 0),
+    ([31, 32, 33, 127, 128, 129], 2, 8, 128, 16, 0),
+    ([517, 0, 300], 2, 7, 80, 48, 300),
+    ([700, 5, 64], 1, 16, 96, 32, 0),
+    ([1000], 2, 17, 128, 64, 0),
+    ([260, 259], 1, 40, 64, 16, 0),
+    ([300, 77], 3, 2, 256, 16, 100),
+    ([200, 513], 2, 3, 192, 64, 0),
+    ([90], 1, 5, 1, 16, 0),
+    ([129, 640], 1, 6, 160, 128, 64),
+    ([333], 1, 4, 224, 16, 1),
+    ([2500, 1, 0, 1700], 1, 2, 128, 64, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("lengths,kv,group,dim,page,window", ATTENDS)
+def test_attend(lengths, kv, group, dim, page, window, fmt, dtype):
+    say(f"case mx attend {lengths} kv={kv} group={group} dim={dim} page={page} window={window} {fmt} {dtype}")
+    rng = np.random.default_rng(sum(lengths) + dim)
+    _attend_case(rng, lengths, kv, group, dim, dtype, fmt, page, window, extra_cols=len(lengths) % 3,
+                 layout="plain" if dim % 3 else "apart")
+
+
+def test_attend_sharp_scores():
+    """Scores far apart: the running maximum moves often, single tokens win."""
+    say("case mx attend sharp scores")
+    rng = np.random.default_rng(77)
+    for dtype in ("f32", "bf16"):
+        _attend_case(rng, [1500, 900], 2, 4, 128, dtype, "fp8", 16, spread=30.0)
+
+
+def test_attend_pages_that_are_not_there():
+    """Tokens of a page outside the cache take no part; a sequence with none
+    left is empty; a length past the table's columns stops there."""
+    import torch
+    say("case mx attend missing pages")
+    rng = np.random.default_rng(3)
+    cache, Q, T, L, O, lse = _attend_case(rng, [320, 200], 2, 4, 64, "f32", "fp8", 32)
+    T = T.clone()
+    T[0, 2], T[0, 5] = -1, cache.pages
+    T[1, :] = 1 << 30
+    got, e = cache.attend(Q, T, L, with_lse=True)
+    # the same with the missing pages cut out of the table
+    keep = [c for c in range(10) if c not in (2, 5)]
+    T2 = T[:1, keep].contiguous()
+    want, l = cache.attend(Q[:1], T2, torch.tensor([256], dtype=torch.int32, device="cuda"), with_lse=True)
+    assert np.allclose(_f64(got[:1]), _f64(want), rtol=0, atol=1e-5)
+    assert np.allclose(_f64(e[:1]), _f64(l), rtol=0, atol=1e-5)
+    assert (_f64(got[1]) == 0).all() and (_f64(e[1]) == -np.inf).all()
+    long = torch.tensor([1 << 30, 200], dtype=torch.int32, device="cuda")
+    assert torch.equal(cache.attend(Q, T, long)[0], cache.attend(Q, T, torch.full_like(L, 320))[0])
+    neg = torch.tensor([-4, -(1 << 31)], dtype=torch.int32, device="cuda")
+    assert (_f64(cache.attend(Q, T, neg)) == 0).all()
+    assert (_f64(cache.attend(Q, T[:, :0], L)) == 0).all()
+
+
+def test_attend_nan_inside_a_sequence_reaches_its_head_only():
+    import torch
+    say("case mx attend NaN token")
+    rng = np.random.default_rng(8)
+    cache, Q, T, L, O, lse = _attend_case(rng, [150, 150], 2, 2, 64, "f32", "fp8", 16)
+    slot = int(T[0, 3]) * 16 + 5
+    bad = torch.zeros((1, 2, 64), device="cuda")
+    keep = cache.read(torch.tensor([slot], device="cuda"))
+    bad[0, 1, 7] = float("nan")
+    cache.write(keep[0] + bad, keep[1], torch.tensor([slot], device="cuda"))
+    got = cache.attend(Q, T, L)
+    g, o = _np(got), _np(O)
+    assert np.isnan(g[0, 2:]).all()
+    assert np.array_equal(g[1], o[1]) and np.array_equal(g[0, :2], o[0, :2])
+
+
+def test_attend_workspace_stream_and_repeats():
+    """Bitwise the same on another stream, with a caller's workspace (whatever
+    it holds) and on every repeat."""
+    import torch
+    say("case mx attend workspace and stream")
+    rng = np.random.default_rng(9)
+    cache, Q, T, L, O, lse = _attend_case(rng, [3000, 1200, 17], 2, 4, 128, "bf16", "fp8", 64)
+    need = cache.attend_workspace(3, 8, T.shape[1])
+    assert need > 0
+    space = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for i in range(3):
+        o, e = cache.attend(Q, T, L, with_lse=True, workspace=space, stream=side)
+        side.synchronize()
+        assert torch.equal(o, O) and torch.equal(e, lse)
+
+
+def test_attend_far_pages():
+    """Pages past 2^32 bytes of a cache."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    say("case mx attend far pages")
+    rng = np.random.default_rng(10)
+    page, dim, heads = 256, 256, 8
+    pages = (1 << 32) // (page * dim * heads) + 40
+    rows = (pages, heads, page, dim)
+    k, v = (torch.empty(rows, dtype=torch.uint8, device="cuda") for _ in "KV")
+    ks, vs = (torch.empty((pages, heads, 8, page), dtype=torch.uint8, device="cuda") for _ in "KV")
+    cache = mpq.MXCache(k, v, ks, vs, dim, "fp8")
+    n = 700
+    K, V = _activations(rng, (n, heads, dim)).astype(np.float32), rng.standard_normal((n, heads, dim)).astype(np.float32)
+    use = np.array([pages - 1, 3, pages - 20])
+    slots = use[np.arange(n) // page] * page + np.arange(n) % page
+    cache.write(_dev(K), _dev(V), _dev(slots.astype(np.int64)))
+    back = cache.read(_dev(slots.astype(np.int64)))
+    hk, hv = _held(K.astype(np.float64), "fp8"), _held(V.astype(np.float64), "fp8")
+    assert np.array_equal(_f64(back[0]), hk) and np.array_equal(_f64(back[1]), hv)
+    Q = _dev(rng.standard_normal((1, heads, dim)).astype(np.float32))
+    O = _f64(cache.attend(Q, _dev(use[None].astype(np.int32)), _dev(np.array([n], dtype=np.int32))))
+    for h in range(heads):
+        want, _, mag = ref.attend(_f64(Q)[0, h], hk[:, h], hv[:, h], dim ** -0.5)
+        assert (np.abs(O[0, h] - want) <= 1e-4 * mag).all()
+
+
+# ------------------------------------------------------------------ together
+
+def test_captured_step_replays():
+    """A decoding step (projection, cache write, attention, projection) captured
+    once with the caller's workspaces and replayed over changing inputs, with
+    eager work between: bitwise the eager step."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    say("case mx captured step")
+    rng = np.random.default_rng(12)
+    batch, kv, group, dim, width = 3, 2, 4, 64, 512
+    heads = kv * group
+    rows = (heads + 2 * kv) * dim
+    wc, ws = _weights(rng, rows, width)
+    oc, os_ = _weights(rng, width, heads * dim)
+    W, O = (_dev(ref.pack(wc)), _dev(ws)), (_dev(ref.pack(oc)), _dev(os_))
+    cache = mpq.MXCache.empty(64, 16, kv, dim, "fp8")
+    table = _dev(rng.permutation(64)[:48].reshape(3, 16).astype(np.int32))
+    start = np.array([200, 7, 90], dtype=np.int32)
+    fill = [(int(table[b, t // 16]) * 16 + t % 16) for b in range(3) for t in range(int(start[b]))]
+    kv0 = [_dev(rng.standard_normal((len(fill), kv, dim)).astype(np.float32)) for _ in "KV"]
+    cache.write(*kv0, _dev(np.array(fill, dtype=np.int64)))
+    X = torch.zeros((batch, width), dtype=torch.bfloat16, device="cuda")
+    slots = torch.zeros((batch,), dtype=torch.int64, device="cuda")
+    lengths = torch.zeros((batch,), dtype=torch.int32, device="cuda")
+    space = [torch.empty((max(1, n),), dtype=torch.uint8, device="cuda") for n in (
+        mpq.mx_linear_workspace(batch, rows, width), mpq.mx_linear_workspace(batch, width, heads * dim),
+        cache.attend_workspace(batch, heads, 16))]
+
+    def step():
+        h = mpq.mx_linear(X, *W, workspace=space[0])
+        q, k, v = (t.reshape(batch, -1, dim) for t in h.split([heads * dim, kv * dim, kv * dim], 1))
+        cache.write(k, v, slots)
+        o = cache.attend(q, table, lengths, workspace=space[2])
+        return mpq.mx_linear(o.reshape(batch, -1), *O, workspace=space[1])
+
+    def set_inputs(i):
+        X.copy_(torch.from_numpy(np.random.default_rng(100 + i).standard_normal((batch, width)).astype(np.float32)))
+        at = start + i
+        slots.copy_(torch.tensor([int(table[b, at[b] // 16]) * 16 + int(at[b] % 16) for b in range(batch)]))
+        lengths.copy_(torch.from_numpy(at + 1))
+
+    set_inputs(0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        captured = step()
+    for i in range(5):
+        set_inputs(i)
+        g.replay()
+        torch.cuda.synchronize()
+        got = captured.clone()
+        want = step()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and bool(torch.isfinite(want.float()).all()), i

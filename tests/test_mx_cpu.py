@@ -1,0 +1,182 @@
+"""The microscaled calls without a GPU: what they refuse, before any HIP call,
+the sizes they report, and the struct's layout."""
+import ctypes
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+import mx_ref as ref
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def mpq():
+    from paper_2002_09049_amd import mpq
+    if not os.path.exists(mpq.LIB_PATH):
+        from paper_2002_09049_amd import build
+        build.build()
+    mpq.load()
+    return mpq
+
+
+def _refused(mpq, fn, ok, changes):
+    """Every change of one argument of a valid call is refused with a text."""
+    for kw in changes:
+        a = dict(ok)
+        a.update(kw)
+        assert fn(*a.values()) == mpq.MPQ_ERR_INVALID_ARG, kw
+        assert mpq.last_error(), kw
+
+
+def test_quantize_refusals(mpq):
+    lib = mpq.load()
+    ok = dict(X=64, dtype=0, rows=4, d=40, ld=40, codes=64, scales=64, stream=None)
+    bad = [dict(X=None), dict(dtype=3), dict(dtype=-1), dict(rows=-1), dict(d=0), dict(d=4194305, ld=4194305),
+           dict(ld=39), dict(ld=1 << 41), dict(codes=None), dict(scales=None), dict(codes=72), dict(scales=65),
+           dict(X=66), dict(X=65, dtype=2), dict(rows=1 << 39)]
+    _refused(mpq, lib.mpq_mx_quantize, ok, bad)
+    assert lib.mpq_mx_quantize(None, 0, 0, 40, 40, None, None, None) == 0
+    ok = dict(codes=64, scales=64, rows=4, d=40, Y=64, dtype=0, ld=40, stream=None)
+    _refused(mpq, lib.mpq_mx_dequantize, ok, [dict(Y=None), dict(dtype=9), dict(rows=-1), dict(d=0), dict(ld=39),
+                                               dict(codes=None), dict(scales=None), dict(codes=65), dict(scales=66),
+                                               dict(Y=66)])
+    assert lib.mpq_mx_dequantize(None, None, 0, 40, None, 0, 40, None) == 0
+
+
+def test_product_refusals(mpq):
+    lib = mpq.load()
+    ok = dict(xc=64, xs=64, n=3, wc=64, ws=64, c=5, d=40, bias=None, Y=64, dtype=1, ld=5, stream=None)
+    bad = [dict(n=-1), dict(n=1048577), dict(c=-1), dict(d=0), dict(d=4194305), dict(xc=None), dict(xs=None),
+           dict(wc=None), dict(ws=None), dict(xc=72), dict(xs=66), dict(wc=72), dict(ws=66), dict(bias=66),
+           dict(Y=None), dict(Y=65), dict(dtype=4), dict(ld=4)]
+    _refused(mpq, lib.mpq_mx_product, ok, bad)
+    assert lib.mpq_mx_product(None, None, 0, 64, 64, 5, 40, None, None, 1, 5, None) == 0
+    assert lib.mpq_mx_product(64, 64, 3, None, None, 0, 40, None, None, 1, 0, None) == 0
+    ok = dict(X=64, xt=2, n=3, x_ld=40, wc=64, ws=64, c=5, d=40, bias=None, Y=64, dtype=1, ld=5, space=None, nbytes=0,
+              stream=None)
+    bad = [dict(X=None), dict(X=65), dict(xt=5), dict(x_ld=39), dict(n=-1), dict(wc=None), dict(Y=None), dict(ld=4),
+           dict(dtype=-2), dict(space=64, nbytes=-1), dict(space=72, nbytes=1 << 20)]
+    _refused(mpq, lib.mpq_mx_linear, ok, bad)
+    assert lib.mpq_mx_linear(None, 2, 0, 40, 64, 64, 5, 40, None, None, 1, 5, None, 0, None) == 0
+    for n, c, d in ((-1, 4, 4), (1 << 21, 4, 4), (4, -1, 4), (4, 4, 0), (4, 4, 1 << 23)):
+        assert lib.mpq_mx_linear_workspace(n, c, d) == mpq.MPQ_ERR_INVALID_ARG
+        with pytest.raises(mpq.MPQError):
+            mpq.mx_linear_workspace(n, c, d)
+    assert mpq.mx_linear_workspace(0, 4, 4) >= 0
+
+
+def _view(mpq, **kw):
+    a = dict(k_codes=64, v_codes=64, k_scales=64, v_scales=64, n_pages=10, page_size=32, kv_heads=2, head_dim=64,
+             format=1)
+    a.update(kw)
+    return mpq.MXCacheView(*a.values())
+
+
+BAD_CACHES = [dict(k_codes=None), dict(v_codes=None), dict(k_scales=None), dict(v_scales=None), dict(k_codes=72),
+              dict(v_codes=8), dict(k_scales=66), dict(v_scales=65), dict(n_pages=0), dict(n_pages=-3),
+              dict(n_pages=1 << 31), dict(n_pages=1 << 30, page_size=1024), dict(page_size=0), dict(page_size=8),
+              dict(page_size=24), dict(page_size=-16), dict(kv_heads=0), dict(kv_heads=65536), dict(head_dim=0),
+              dict(head_dim=257), dict(format=2), dict(format=-1)]
+
+
+def test_cache_refusals(mpq):
+    lib = mpq.load()
+    E = mpq.MPQ_ERR_INVALID_ARG
+    good = _view(mpq)
+    at = ctypes.addressof(good)
+    ok = dict(c=at, K=64, ks=128, kh=64, V=64, vs=128, vh=64, dtype=0, n=3, slots=64, stream=None)
+    bad = [dict(c=None), dict(K=None), dict(V=None), dict(slots=None), dict(K=66), dict(V=65), dict(slots=68),
+           dict(dtype=7), dict(n=-1), dict(n=1 << 31), dict(ks=-1), dict(kh=-1), dict(vs=-1), dict(vh=1 << 41)]
+    _refused(mpq, lib.mpq_mx_cache_write, ok, bad)
+    # outputs of a read do not overlap
+    _refused(mpq, lib.mpq_mx_cache_read, ok, bad + [dict(ks=0), dict(kh=63), dict(vs=63), dict(vh=0)])
+    for kw in BAD_CACHES:
+        c = _view(mpq, **kw)
+        p = ctypes.addressof(c)
+        assert lib.mpq_mx_cache_write(p, 64, 128, 64, 64, 128, 64, 0, 3, 64, None) == E, kw
+        assert lib.mpq_mx_cache_read(p, 64, 128, 64, 64, 128, 64, 0, 3, 64, None) == E, kw
+        assert lib.mpq_mx_attend_workspace(p, 1, 4, 3) == E, kw
+    assert lib.mpq_mx_cache_write(at, None, 0, 0, None, 0, 0, 0, 0, None, None) == 0
+    assert lib.mpq_mx_cache_read(at, None, 128, 64, None, 128, 64, 0, 0, None, None) == 0
+
+
+def test_attend_refusals(mpq):
+    lib = mpq.load()
+    good = _view(mpq)
+    ok = dict(c=ctypes.addressof(good), Q=64, qs=256, qh=64, dtype=0, batch=2, heads=4, table=64, table_ld=5, cols=5,
+              lengths=64, window=0, scale=0.1, O=64, os=256, oh=64, lse=None, space=None, nbytes=0, stream=None)
+    bad = [dict(c=None), dict(Q=None), dict(O=None), dict(table=None), dict(lengths=None), dict(dtype=3),
+           dict(batch=-1), dict(batch=65536), dict(heads=0), dict(heads=3), dict(heads=65536), dict(table_ld=4),
+           dict(cols=-1), dict(cols=(1 << 24) + 1, table_ld=1 << 25), dict(window=-1), dict(scale=float("nan")),
+           dict(scale=float("inf")), dict(qs=-1), dict(qh=-1), dict(os=63), dict(oh=0), dict(Q=66), dict(O=65),
+           dict(table=66), dict(lengths=65), dict(lse=66), dict(space=72, nbytes=1 << 30),
+           dict(space=64, nbytes=8, cols=400, table_ld=400)]
+    _refused(mpq, lib.mpq_mx_attend, ok, bad)
+    a = dict(ok, batch=0, Q=None, O=None, table=None, lengths=None)
+    assert lib.mpq_mx_attend(*a.values()) == 0
+    for batch, heads, cols in ((-1, 4, 3), (1, 5, 3), (1, 4, -1), (1, 0, 3)):
+        assert lib.mpq_mx_attend_workspace(ok["c"], batch, heads, cols) == mpq.MPQ_ERR_INVALID_ARG
+    assert lib.mpq_mx_attend_workspace(ok["c"], 1, 4, 1) == 0             # one piece needs none
+    assert lib.mpq_mx_attend_workspace(ok["c"], 1, 4, 4096) > 0
+
+
+def test_workspace_cap_gives_nomem(mpq):
+    """MPQ_WORKSPACE_LIMIT caps the scratch of a call without a workspace."""
+    lib = mpq.load()
+    good = _view(mpq)
+    os.environ["MPQ_WORKSPACE_LIMIT"] = "64"
+    try:
+        assert lib.mpq_mx_linear(64, 0, 300, 4096, 64, 64, 5, 4096, None, 64, 0, 5, None, 0, None) == mpq.MPQ_ERR_NOMEM
+        assert "scratch" in mpq.last_error()
+        assert lib.mpq_mx_attend(ctypes.addressof(good), 64, 256, 64, 0, 2, 4, 64, 4096, 4096, 64, 0, 0.1, 64, 256, 64,
+                                 None, None, 0, None) == mpq.MPQ_ERR_NOMEM
+    finally:
+        del os.environ["MPQ_WORKSPACE_LIMIT"]
+
+
+def test_cache_struct_matches_header(mpq, tmp_path):
+    fields = [f for f, _ in mpq.MXCacheView._fields_]
+    src = tmp_path / "off.c"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "mpq.h"\nint main(void){\n'
+                   '  printf("%zu\\n", sizeof(mpq_mx_cache));\n' +
+                   "".join(f'  printf("%zu\\n", offsetof(mpq_mx_cache, {f}));\n' for f in fields) +
+                   '  printf("%d %d %d %d %d %d %d\\n", MPQ_F32, MPQ_F16, MPQ_BF16, MPQ_MX_FP4, MPQ_MX_FP8,'
+                   ' MPQ_MX_BLOCK, MPQ_MX_ROW);\n  return 0;\n}\n')
+    exe = tmp_path / "off"
+    subprocess.check_call(["gcc", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)])
+    out = [int(x) for x in subprocess.check_output([str(exe)]).split()]
+    assert out[0] == ctypes.sizeof(mpq.MXCacheView)
+    assert out[1:-7] == [getattr(mpq.MXCacheView, f).offset for f in fields]
+    assert out[-7:] == [0, 1, 2, 0, 1, mpq.MX_BLOCK, mpq.MX_ROW]
+
+
+def test_binding_refuses_host_tensors_and_shapes(mpq):
+    import torch
+    x = torch.zeros((2, 8))
+    with pytest.raises(ValueError):
+        mpq.mx_quantize(x)
+    with pytest.raises(ValueError):
+        mpq.mx_dequantize(torch.zeros((2, 64), dtype=torch.uint8), torch.zeros((2, 3), dtype=torch.uint8), 8)
+    with pytest.raises(ValueError):
+        mpq.MXCache.empty(4, 16, 2, 64, "int8", device="cpu")
+    with pytest.raises(ValueError):
+        mpq.MXCache.empty(4, 16, 2, 64, "fp8", device="cpu")
+
+
+def test_reference_rounds_to_nearest_even():
+    """The oracle's own formats: every half-way point, by enumeration."""
+    for fmt, top in (("fp4", 6.0), ("fp8", 448.0)):
+        v = ref.elements(fmt)
+        assert (np.diff(v) > 0).all() and v[-1] == top
+        for i in range(len(v) - 1):
+            x = np.zeros(32)
+            x[0], x[31] = (v[i] + v[i + 1]) / 2, top
+            c, s = ref.quantize(x, fmt)
+            assert s[0] == 127 and c[0] == (i if i % 2 == 0 else i + 1)
+        c, s = ref.quantize(np.linspace(-top, top, 64), fmt)
+        back = ref.values(c, s, fmt)
+        near = np.abs(np.linspace(-top, top, 64)[:, None] - np.concatenate([-v, v])).min(1)
+        assert np.allclose(np.abs(back - np.linspace(-top, top, 64)), near)

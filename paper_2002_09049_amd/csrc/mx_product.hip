@@ -5,12 +5,10 @@
 // and sums 128 products (four blocks, one for each l / 16) in fp32.  Rows of
 // W are the instruction's rows, tokens its columns.
 //
-// The order of the sum is free as long as both operands share it: in a chunk
-// of 512 elements, lanes of group g = l / 16 take the blocks 4g .. 4g + 3, one
-// for each of four instructions.  A lane then reads 64 consecutive bytes of
-// its row and one aligned word of four scales, whose bytes the instructions
-// select themselves.
+// The order of the sum is free as long as both operands share it.
 #include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 #include "mpq.h"
 #include "mx.hpp"
@@ -19,30 +17,38 @@ namespace mpq {
 
 namespace {
 
-constexpr int kChunkBlocks = 16;   // a chunk: 512 elements, 256 bytes of a row
-
-// One lane's share of a chunk of a row: blocks 4g .. 4g + 3 and their scales.
-// A row holds nb blocks, a multiple of four, so a lane's four are all there
-// or none is (zeros then).
+// One lane's share of a chunk (512 elements, 256 bytes) of a row: block 4i + g
+// for instruction i, so that the four lanes of a row read 64 consecutive bytes,
+// and a word whose byte i is that block's scale.  The row's scales lie
+// the other way, 4i .. 4i + 3 in word i: lane g reads word g and the four lanes of
+// the row exchange bytes.
+constexpr int kChunkBlocks = 16;
 struct Share {
     u32x4 c[4];
     uint32_t s;
 };
 
-__device__ __forceinline__ Share load_share(const uint8_t *codes, const uint8_t *scales, int64_t row, int nb, int blk)
+// Byte i of lane group g's result is byte g of group i's word.
+__device__ __forceinline__ uint32_t transpose_bytes(uint32_t w, int g)
 {
-    Share v;
-    if (blk < nb) {
-        const u32x4 *p = (const u32x4 *)(codes + (row * nb + blk) * 16);
+    uint32_t a, b;
+    swap_step<true>(w, a, b);    // groups g % 2 and g % 2 + 2
+    w = __builtin_amdgcn_perm(b, a, g / 2 ? 0x07060302u : 0x05040100u);
+    swap_step<false>(w, a, b);   // groups g / 2 * 2 and g / 2 * 2 + 1
+    return __builtin_amdgcn_perm(b, a, g % 2 ? 0x07030501u : 0x06020400u);
+}
+
+// Chunk k / 16 of a row of nb blocks, its scales not yet exchanged.  kWhole: the
+// chunk lies inside the row; else blocks past it are zeros.
+template <bool kWhole>
+__device__ __forceinline__ void load_share(Share &v, const uint8_t *codes, const uint8_t *scales, int64_t row, int nb,
+                                           int k, int g)
+{
+    const uint8_t *p = codes + (row * nb + k + g) * 16;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v.c[i] = p[i];
-        v.s = *(const uint32_t *)(scales + row * nb + blk);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v.c[i] = u32x4{0, 0, 0, 0};
-        v.s = 0;
-    }
-    return v;
+    for (int i = 0; i < 4; ++i)
+        v.c[i] = kWhole || k + 4 * i < nb ? *(const u32x4 *)(p + 64 * i) : u32x4{0, 0, 0, 0};
+    v.s = kWhole || k + 4 * g < nb ? *(const uint32_t *)(scales + row * nb + k + 4 * g) : 0u;
 }
 
 __device__ __forceinline__ i32x8 widen(u32x4 v)
@@ -83,7 +89,7 @@ template <int kNT>
 __global__ void __launch_bounds__(kFewWaves *kWave) mx_few_kernel(MxProduct p)
 {
     __shared__ __align__(16) float part[kFewWaves][kNT][kWave * 4];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = lane % 16, g = lane / 16;
     const int64_t c0 = (int64_t)blockIdx.x * 16, t0 = (int64_t)blockIdx.y * 16 * kNT;
     const int nb = p.nb;
@@ -96,14 +102,21 @@ __global__ void __launch_bounds__(kFewWaves *kWave) mx_few_kernel(MxProduct p)
         xrow[t] = min(t0 + 16 * t + r, p.n - 1);
         acc[t] = f32x4{0, 0, 0, 0};
     }
-    for (int k = wave * kChunkBlocks; k < nb; k += kFewWaves * kChunkBlocks) {
-        const Share a = load_share(p.wc, p.ws, wrow, nb, k + 4 * g);
-        Share b[kNT];
+    const auto chunk = [&](auto whole, int k) {
+        Share a, b[kNT];
+        load_share<decltype(whole)::value>(a, p.wc, p.ws, wrow, nb, k, g);
 #pragma unroll
-        for (int t = 0; t < kNT; ++t) b[t] = load_share(p.xc, p.xs, xrow[t], nb, k + 4 * g);
+        for (int t = 0; t < kNT; ++t) load_share<decltype(whole)::value>(b[t], p.xc, p.xs, xrow[t], nb, k, g);
+        a.s = transpose_bytes(a.s, g);
 #pragma unroll
-        for (int t = 0; t < kNT; ++t) acc[t] = multiply_chunk(a, b[t], acc[t]);
-    }
+        for (int t = 0; t < kNT; ++t) {
+            b[t].s = transpose_bytes(b[t].s, g);
+            acc[t] = multiply_chunk(a, b[t], acc[t]);
+        }
+    };
+    int k = wave * kChunkBlocks;
+    for (; k + kChunkBlocks <= nb; k += kFewWaves * kChunkBlocks) chunk(std::true_type(), k);
+    if (k < nb) chunk(std::false_type(), k);   // the chunk that the row ends in
 #pragma unroll
     for (int t = 0; t < kNT; ++t) *(f32x4 *)&part[wave][t][lane * 4] = acc[t];
     __syncthreads();
@@ -121,14 +134,399 @@ __global__ void __launch_bounds__(kFewWaves *kWave) mx_few_kernel(MxProduct p)
     }
 }
 
+// Many tokens: a workgroup owns 64 kTM rows of W by 64 kTN tokens, its four
+// wavefronts a quarter each (32 kTM by 32 kTN, in v_mfma_scale_f32_32x32x64
+// tiles: lane l supplies the 32 elements of one block of row l % 32).
+//
+// K runs in stages of 128 elements, 64 bytes of every row, in a ring of four
+// LDS buffers that loads fill without passing through registers.  While
+// stage s is multiplied, the loads of stage s + 3 go out between its products
+// (a wavefront has its SIMD to itself, so a load that waits for its turn
+// would hold up the matrix core), and the operands of each step are read from LDS
+// during the step before, those of stage s + 1 too: the barrier at stage s
+// says that stage s + 1 is there.  Stages past the row are zeros: their loads
+// lie past the buffer, and every wait counts the same number of loads.
+//
+// 16-byte piece q of row r lies in place q ^ (r / 4 % 4) of its LDS row, so that
+// lanes that read one piece of consecutive rows spread over the banks.  Lanes of
+// half h = l / 32 take pieces 2h and 2h + 1, one for each of a stage's two
+// steps, so the scales of a lane's row come as a half-word whose bytes the
+// steps select.  Scales go to LDS four stages at a time, 16 bytes of a row
+// through the registers of a thread: one row's scales lie in one line of
+// memory, apart from the other rows', so they are fetched as rarely as
+// possible.
+constexpr int kStageBytes = 64;
+constexpr uint32_t kOutside = 0x80000000u;   // past every buffer: loads give zeros
+
+// (the arguments are the same in every lane: a descriptor in scalar registers)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint8_t *base, int64_t bytes)
+{
+    const uint64_t at = (uint64_t)base;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc((void *)((uint64_t)hi << 32 | lo), (short)0,
+                                             __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
+}
+
+// 16 rows' part of a stage into LDS (the 64 lanes' 16 bytes land one after the
+// other).
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, uint8_t *to, uint32_t at, int offset)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, at, offset, 0, 0);
+}
+
+__device__ __forceinline__ u32x4 load_scales(__amdgpu_buffer_rsrc_t from, uint32_t at)
+{
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, at, 0, 0));
+}
+
+// acc += a b^T over the lanes' blocks; byte kA of as and byte kB of bs are
+// their scales.
+template <int kA, int kB>
+__device__ __forceinline__ f32x16 multiply_tile(u32x4 a, uint32_t as, u32x4 b, uint32_t bs, f32x16 acc)
+{
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widen(a), widen(b), acc, 4, 4, kA, (int)as, kB, (int)bs);
+}
+
+// A barrier that leaves this wavefront's last kLeft loads into LDS in flight
+// (__syncthreads would wait for them all); its LDS reads and writes and its
+// loads before those are done.
+template <int kLeft>
+__device__ __forceinline__ void meet()
+{
+    constexpr int kVmcnt = (kLeft & 15) | (kLeft >> 4) << 14;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // orders the compiler's accesses only
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0070 | kVmcnt);   // vmcnt(kLeft), lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// The operands of one step of a stage (64 elements): the lane's pieces of the
+// wavefront's rows of W, which start at row wm of the stage, and of its
+// tokens, at row 64 kTM + wn.
+template <int kTM, int kTN>
+struct Operands {
+    u32x4 a[kTM], b[kTN];
+    __device__ __forceinline__ void read(const uint8_t *stage, int step, int wm, int wn, int r, int h)
+    {
+        const int at = ((2 * h + step) ^ (r / 4 % 4)) * 16;
+#pragma unroll
+        for (int i = 0; i < kTM; ++i) a[i] = *(const u32x4 *)(stage + (wm + 32 * i + r) * kStageBytes + at);
+#pragma unroll
+        for (int j = 0; j < kTN; ++j) b[j] = *(const u32x4 *)(stage + (64 * kTM + wn + 32 * j + r) * kStageBytes + at);
+    }
+};
+
+// The scales of the lane's rows for one stage, two bytes (a step each) a row
+// tile: they lie side by side in LDS, [h][r][tile], and the products select
+// their bytes.
+typedef uint16_t __attribute__((may_alias)) half_word;
+typedef uint32_t __attribute__((may_alias)) word;
+typedef uint64_t __attribute__((may_alias)) two_words;
+
+// kT half-words, aligned to their size (plain loads: the compiler keeps track
+// of which LDS array they read)
+template <int kT>
+__device__ __forceinline__ void read_scales(const uint8_t *at, uint32_t (&w)[(kT + 1) / 2])
+{
+    if constexpr (kT == 1) w[0] = *(const half_word *)at;
+    else if constexpr (kT == 2) w[0] = *(const word *)at;
+    else {
+        static_assert(kT == 4, "");
+        const uint64_t v = *(const two_words *)at;
+        w[0] = (uint32_t)v;
+        w[1] = (uint32_t)(v >> 32);
+    }
+}
+
+template <int kTM, int kTN>
+struct Scales {
+    uint32_t a[(kTM + 1) / 2], b[(kTN + 1) / 2];
+    __device__ __forceinline__ void read(const uint8_t *stage, int wm, int wn, int r, int h)
+    {
+        const uint8_t *at = stage + h * 512 * ((64 * (kTM + kTN) + 255) / 256);
+        read_scales<kTM>(at + 2 * (wm + r * kTM), a);
+        read_scales<kTN>(at + 2 * (64 * kTM + wn + r * kTN), b);
+    }
+};
+
+// The products of one step; after(i) runs behind those of row tile i.
+template <int kS, int kTM, int kTN, class After>
+__device__ __forceinline__ void multiply_operands(const Operands<kTM, kTN> &o, const Scales<kTM, kTN> &sc,
+                                                  f32x16 (&acc)[kTM][kTN], After after)
+{
+#pragma unroll
+    for (int i = 0; i < kTM; ++i) {
+#pragma unroll
+        for (int j = 0; j < kTN; ++j) {
+            // byte of the word: the odd tile's pair is its upper half
+            if (i % 2 == 0 && j % 2 == 0)
+                acc[i][j] = multiply_tile<kS, kS>(o.a[i], sc.a[i / 2], o.b[j], sc.b[j / 2], acc[i][j]);
+            else if (i % 2 == 0)
+                acc[i][j] = multiply_tile<kS, kS + 2>(o.a[i], sc.a[i / 2], o.b[j], sc.b[j / 2], acc[i][j]);
+            else if (j % 2 == 0)
+                acc[i][j] = multiply_tile<kS + 2, kS>(o.a[i], sc.a[i / 2], o.b[j], sc.b[j / 2], acc[i][j]);
+            else
+                acc[i][j] = multiply_tile<kS + 2, kS + 2>(o.a[i], sc.a[i / 2], o.b[j], sc.b[j / 2], acc[i][j]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        after(i);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// The sums to Y.  Register v of a tile is row 8 (v / 4) + 4 h + v % 4 of W, token
+// r: a wavefront turns one row of tiles (32 rows of W by 32 kTN tokens) at a
+// time in its part of LDS, so that a lane then holds eight consecutive values
+// of a token's row and four lanes store 32 of them.  The loop over tokens
+// stays rolled: unrolled, with the sums' registers as its operands, it took
+// 14 us of a 256 by 256 tile, instruction fetches.
+constexpr int kTurnRow = 36;   // floats of a token's row in LDS
+
+// Every 16th token's eight values from `from` on, with the bias added, to rows
+// of Y from `to` on; whole: all lanes' eight values are inside the rows.
+template <class T>
+__device__ __forceinline__ void write_turn(T *to, int64_t step, const float *from, int tokens, bool whole, int live,
+                                           const float (&bias)[8])
+{
+    const auto one = [&](int t, int inside) {
+        const f32x4 lo = *(const f32x4 *)(from + t * kTurnRow), hi = *(const f32x4 *)(from + t * kTurnRow + 4);
+        float y[8];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            y[v] = lo[v] + bias[v];
+            y[v + 4] = hi[v] + bias[v + 4];
+        }
+        store8(to, inside, y);
+        to += step;
+    };
+    if (whole) {
+#pragma unroll 4
+        for (int t = 0; t < tokens; t += 16) one(t, 8);
+    } else {
+#pragma unroll 1
+        for (int t = 0; t < tokens; t += 16) one(t, live);
+    }
+}
+
+template <int kTM, int kTN>
+__device__ __forceinline__ void write_tiles(const MxProduct &p, float *turn, int64_t c0, int64_t t0, int lane,
+                                            const f32x16 (&acc)[kTM][kTN])
+{
+    const int r = lane % 32, h = lane / 32;
+    const int64_t first = t0 + lane / 4;   // the lane's first token
+    const int tokens = (int)min((int64_t)(32 * kTN) - lane / 4, p.n - first);
+    const float *from = turn + lane / 4 * kTurnRow + lane % 4 * 8;
+#pragma unroll
+    for (int i = 0; i < kTM; ++i) {
+#pragma unroll
+        for (int j = 0; j < kTN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *(f32x4 *)&turn[(32 * j + r) * kTurnRow + 8 * q + 4 * h] =
+                    f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const bool whole = c0 + 32 * i + 32 <= p.c;
+        const int64_t row = c0 + 32 * i + lane % 4 * 8;
+        const int live = (int)min((int64_t)8, p.c - row);
+        float bias[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (p.bias) load8(p.bias + row, live, bias);
+        const int64_t at = first * p.ldy + row;
+        if (p.dtype == MPQ_F32) write_turn((float *)p.Y + at, 16 * p.ldy, from, tokens, whole, live, bias);
+        else if (p.dtype == MPQ_F16) write_turn((_Float16 *)p.Y + at, 16 * p.ldy, from, tokens, whole, live, bias);
+        else write_turn((__bf16 *)p.Y + at, 16 * p.ldy, from, tokens, whole, live, bias);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+// The tile of this workgroup.  Workgroups are dealt to the eight XCDs in turn,
+// and each XCD has an L2 of its own: an XCD takes a run of consecutive tiles, in
+// an order that goes through four rows of tiles (of W) side by side, so that the
+// 32 workgroups which run there together read 4 + 8 tiles' rows.
+constexpr int kXcds = 8, kSide = 4;
+
+__device__ __forceinline__ bool tile_of(int tiles_m, int tiles_n, int &tm, int &tn)
+{
+    const int tiles = tiles_m * tiles_n;
+    const int xcd = blockIdx.x % kXcds, slot = blockIdx.x / kXcds;
+    const int run = tiles / kXcds, more = tiles % kXcds;
+    if (slot >= run + (xcd < more ? 1 : 0)) return false;   // the grid is rounded up
+    const int at = xcd * run + min(xcd, more) + slot;
+    const int group = at / (kSide * tiles_n), in = at - group * (kSide * tiles_n);
+    const int side = min(kSide, tiles_m - group * kSide);
+    tn = __builtin_amdgcn_readfirstlane(in / side);
+    tm = __builtin_amdgcn_readfirstlane(group * kSide + in % side);
+    return true;
+}
+
+template <int kTM, int kTN>
+__global__ void __launch_bounds__(256) mx_tile_kernel(MxProduct p)
+{
+    constexpr int kBM = 64 * kTM, kBN = 64 * kTN, kRows = kBM + kBN;
+    constexpr int kLoads = kRows / 64;                 // of a wavefront a stage
+    constexpr int kScaleRows = (kRows + 255) / 256;    // rows whose scales a thread moves
+    constexpr int kHalf = 256 * kScaleRows;            // half-words of a stage's scales for one h
+    // buffers of their own, which the compiler can tell apart: a read of one
+    // does not wait for the loads into another
+    __shared__ __align__(16) uint8_t lds0[kRows * kStageBytes], lds1[kRows * kStageBytes];
+    __shared__ __align__(16) uint8_t lds2[kRows * kStageBytes], lds3[kRows * kStageBytes];
+    __shared__ __align__(16) uint8_t lds_scales[2][4][4 * kHalf];   // of four stages, twice
+    const auto ring = [&](int i) { return i == 0 ? lds0 : i == 1 ? lds1 : i == 2 ? lds2 : lds3; };
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int r = lane % 32, h = lane / 32;
+    int tm, tn;
+    if (!tile_of((int)((p.c + kBM - 1) / kBM), (int)((p.n + kBN - 1) / kBN), tm, tn)) return;
+    const int64_t c0 = (int64_t)tm * kBM, t0 = (int64_t)tn * kBN;
+    const int row_bytes = p.nb * 16;
+    const int64_t wrows = min((int64_t)kBM, p.c - c0), xrows = min((int64_t)kBN, p.n - t0);
+    const __amdgpu_buffer_rsrc_t wc = buffer_of(p.wc + c0 * row_bytes, wrows * row_bytes);
+    const __amdgpu_buffer_rsrc_t xc = buffer_of(p.xc + t0 * row_bytes, xrows * row_bytes);
+    const int wm = wave % 2 * (kBM / 2), wn = wave / 2 * (kBN / 2);   // the wavefront's quarter
+
+    // a load covers 16 rows, lane l row l / 4 of them; a wavefront loads a quarter
+    // of W's rows (loads 0 .. kTM - 1) and of the tokens'
+    const uint32_t lane_at = (uint32_t)(lane / 4 * row_bytes + ((lane % 4) ^ (lane / 16)) * 16);
+    const auto load = [&](int st, int buf, int k) {
+        const uint32_t at = 4 * st < p.nb ? lane_at : kOutside;
+        const int row = k < kTM ? 16 * (wave * kTM + k) : 16 * (wave * kTN + k - kTM);
+        uint8_t *to = ring(buf) + ((k < kTM ? 0 : kBM) + row) * kStageBytes;
+        if (k < kTM) load_to_lds(wc, to, at, row * row_bytes + st * kStageBytes);
+        else load_to_lds(xc, to, at, row * row_bytes + st * kStageBytes);
+    };
+    // scales: a thread moves those of the rows threadIdx.x + 256 i (W's, then the
+    // tokens'; a wavefront's 64 are of one kind)
+    const auto scales_of = [&](int i) {
+        const int row = 256 * i + 64 * wave;
+        // (none of them inside the matrix: a buffer of no bytes)
+        return row < kBM ? buffer_of(p.ws + (c0 + row) * p.nb, max((int64_t)0, wrows - row) * p.nb)
+                         : buffer_of(p.xs + (t0 + row - kBM) * p.nb, max((int64_t)0, xrows - (row - kBM)) * p.nb);
+    };
+    const __amdgpu_buffer_rsrc_t scales0 = scales_of(0), scales1 = scales_of(kScaleRows - 1);
+    u32x4 moved[kScaleRows];
+    const auto fetch_scales = [&](int four) {   // of the stages 4 four ..
+#pragma unroll
+        for (int i = 0; i < kScaleRows; ++i)
+            moved[i] = load_scales(i == 0 ? scales0 : scales1, (uint32_t)(lane * p.nb + 16 * four));
+    };
+    // row R of W is row R % 32 of tile R / 32 % kTM of its half; rows past kRows
+    // are written behind the others and not read
+    uint32_t scales_at[kScaleRows];
+#pragma unroll
+    for (int i = 0; i < kScaleRows; ++i) {
+        const int row = (int)threadIdx.x + 256 * i, token = row - kBM;
+        scales_at[i] = 2 * (row < kBM   ? row / (32 * kTM) * (32 * kTM) + row % 32 * kTM + row / 32 % kTM
+                            : row < kRows ? kBM + token / (32 * kTN) * (32 * kTN) + token % 32 * kTN + token / 32 % kTN
+                                          : row);
+    }
+    const auto place_scales = [&](int four) {
+#pragma unroll
+        for (int i = 0; i < kScaleRows; ++i)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t v = 16 * four + 4 * w < p.nb ? moved[i][w] : 0u;   // past the row: the next row's
+                *(half_word *)&lds_scales[four % 2][w][scales_at[i]] = (uint16_t)v;
+                *(half_word *)&lds_scales[four % 2][w][2 * kHalf + scales_at[i]] = (uint16_t)(v >> 16);
+            }
+    };
+
+    f32x16 acc[kTM][kTN];
+#pragma unroll
+    for (int i = 0; i < kTM; ++i)
+#pragma unroll
+        for (int j = 0; j < kTN; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+
+    fetch_scales(0);
+#pragma unroll
+    for (int st = 0; st < 3; ++st)
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) load(st, st, k);
+    place_scales(0);
+    fetch_scales(1);
+    Operands<kTM, kTN> first, second;   // of a stage's two steps
+    Scales<kTM, kTN> now, next;
+    meet<2 * kLoads + kScaleRows>();   // stage 0 is there
+    first.read(ring(0), 0, wm, wn, r, h);
+    now.read(lds_scales[0][0], wm, wn, r, h);
+    const int fours = (p.nb + 15) / 16;
+    for (int four = 0; four < fours; ++four) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int st = 4 * four + q;
+            // stage st + 1 is there, and stage st - 1's buffer free; stage st + 2's
+            // loads and, where they are as young, the scales' may still run
+            if (q == 3 || q == 0) meet<kLoads + kScaleRows>();
+            else meet<kLoads>();
+            second.read(ring(q), 1, wm, wn, r, h);
+            next.read(lds_scales[q == 3 ? (four + 1) % 2 : four % 2][(q + 1) % 4], wm, wn, r, h);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply_operands<0>(first, now, acc, [&](int i) {
+                if (i < kLoads) load(st + 3, (q + 3) % 4, i);
+            });
+            if (q == 2) place_scales(four + 1);
+            first.read(ring((q + 1) % 4), 0, wm, wn, r, h);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply_operands<1>(second, now, acc, [&](int i) {
+                if (kTM + i < kLoads) load(st + 3, (q + 3) % 4, kTM + i);
+            });
+            if (q == 2) fetch_scales(four + 2);
+            now = next;
+        }
+    }
+    // no load into LDS outlives the loop, and no wavefront still reads it
+    meet<0>();
+    static_assert(32 * kTN * kTurnRow * 4 <= kRows * kStageBytes, "a wavefront's part fits its buffer");
+    write_tiles(p, (float *)ring(wave), c0 + wm, t0 + wn, lane, acc);
+}
+
+template <int kTM, int kTN>
+hipError_t launch_tiles(const MxProduct &p, hipStream_t s)
+{
+    const int64_t tiles = ((p.c + 64 * kTM - 1) / (64 * kTM)) * ((p.n + 64 * kTN - 1) / (64 * kTN));
+    if (tiles > 0x40000000LL) return hipErrorInvalidValue;
+    LaunchTimer timer(s, kTM == 2 ? (kTN == 1 ? "mx_tile_kernel<2,1>" : "mx_tile_kernel<2,2>")
+                                  : (kTN == 2 ? "mx_tile_kernel<4,2>" : "mx_tile_kernel<4,4>"));
+    hipLaunchKernelGGL((mx_tile_kernel<kTM, kTN>), dim3((unsigned)((tiles + kXcds - 1) / kXcds * kXcds)), dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
 }  // namespace
 
+// Which kernel: the one that a model of its time, in us, finds fastest.  With K
+// in stages of 128 elements, a tile kernel takes its start and end plus its
+// stages, once for every 256 tiles (one CU each); the kernel for few tokens,
+// for every 256 of its workgroups, what the vector cache takes to serve every
+// lane of its operands' loads by itself.  The constants are fits to
+// measurements; model and time, us, for 4096 x 4096 (last row: x 25088) weights:
+//     n          few        128x64      128x128     256x128     256x256
+//     64     8.5   8.4    9.9   8.5   12.5  11.0  19.4  18.0  28.8  26.4
+//     512     54    56    9.9  11.0   12.5  12.5  19.4  18.6  28.8  28.4
+//     1024   106   109   19.8  21.8   12.5  16.6  19.4  20.9  28.8  29.8
+//     2048   210   216     40    42     25    33  19.4  29.1  28.8  33.8
+//     8192   834           158   139   100   113    78   108    58    85
+//     64      42    34     43    52    54    56    88    89   131   128
 hipError_t launch_mx_product(const MxProduct &p, hipStream_t s)
 {
     if (p.n <= 0 || p.c <= 0) return hipSuccess;
+    const double stages = p.nb / 4;
+    const auto tiles_us = [&](int tm, int tn, double ends, double stage) {
+        const double tiles = (double)((p.c + 64 * tm - 1) / (64 * tm)) * (double)((p.n + 64 * tn - 1) / (64 * tn));
+        return ceil(tiles / 256.0) * (ends + stage * stages);
+    };
+    const double t21 = tiles_us(2, 1, 3.5, 0.2), t22 = tiles_us(2, 2, 4.5, 0.25), t42 = tiles_us(4, 2, 6.0, 0.42),
+                 t44 = tiles_us(4, 4, 9.0, 0.62);
+    const double best = std::min(std::min(t21, t22), std::min(t42, t44));
     const int nt = p.n <= 16 ? 1 : p.n <= 32 ? 2 : 4;
     const int64_t gx = (p.c + 15) / 16, gy = (p.n + 16 * nt - 1) / (16 * nt);
-    if (gx > 0x7fffffffLL || gy > 65535) return hipErrorInvalidValue;
+    const double few = 2.0 + ceil((double)gx * (double)gy / 256.0) * (p.nb / 128.0) * (nt == 1 ? 2.6 : nt == 2 ? 3.8 : 6.5);
+    if (few > best || gy > 65535) {
+        if (best == t44) return launch_tiles<4, 4>(p, s);
+        if (best == t42) return launch_tiles<4, 2>(p, s);
+        return best == t22 ? launch_tiles<2, 2>(p, s) : launch_tiles<2, 1>(p, s);
+    }
+    if (gx > 0x7fffffffLL) return hipErrorInvalidValue;
     LaunchTimer timer(s, "mx_few_kernel");
     auto kern = nt == 1 ? mx_few_kernel<1> : nt == 2 ? mx_few_kernel<2> : mx_few_kernel<4>;
     hipLaunchKernelGGL(kern, dim3((unsigned)gx, (unsigned)gy), dim3(kFewWaves * kWave), 0, s, p);

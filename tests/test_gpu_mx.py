@@ -191,6 +191,32 @@ def test_linear(n, c, d, dtype, bias):
     assert torch.equal(Y32.to(_dt(dtype)), Y)
 
 
+# (n, c, d, kernel's tile): sizes at which each tile of the many-token kernels
+# is taken, ragged at every edge, K of one to several rings of stages
+TILES = [(500, 4001, 130, "2,1"), (1000, 4001, 130, "2,2"), (2000, 4001, 257, "4,2"), (3900, 4001, 130, "4,4"),
+         (130, 2999, 5000, "2,1"), (1001, 3999, 1150, "2,2"), (3901, 4000, 640, "4,4")]
+
+
+@pytest.mark.parametrize("n,c,d,tile", TILES)
+def test_linear_tiles(n, c, d, tile):
+    from paper_2002_09049_amd import mpq
+    say(f"case mx linear tiles n={n} c={c} d={d}")
+    rng = np.random.default_rng(n + c + d)
+    X = _dev(_activations(rng, (n, d)).astype(np.float32))
+    wc, ws = _weights(rng, c, d)
+    b = rng.standard_normal(c).astype(np.float32)
+    codes, scales = _dev(ref.pack(wc)), _dev(ws)
+    mpq.timing_enable(True)
+    try:
+        Y = mpq.mx_linear(X, codes, scales, bias=_dev(b))
+        names = [k for k, _ in mpq.timing_read()]
+    finally:
+        mpq.timing_enable(False)
+    assert names == ["mx_quantize_kernel", f"mx_tile_kernel<{tile}>"]
+    xq = ref.values(*ref.quantize(ref.padded(_f64(X), ref.ROW), "fp4"), "fp4")
+    _check_product(_f64(Y), xq, ref.values(wc, ws, "fp4"), b.astype(np.float64), "f32", ws.shape[1])
+
+
 @pytest.mark.parametrize("n", [1, 5, 40, 300])
 def test_linear_with_a_bad_token(n):
     """A token that holds a NaN gives a row of NaN, and no other."""

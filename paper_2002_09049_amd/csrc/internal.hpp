@@ -329,6 +329,10 @@ struct MxProduct {
     int64_t n, c, ldy;
 };
 hipError_t launch_mx_product(const MxProduct &p, hipStream_t s);
+// The product with tokens [n][x_ld] of a dtype, quantized in the same launch
+// (xc and xs unused); only for so few tokens that mx_quantizes_inside.
+bool mx_quantizes_inside(int64_t n);
+hipError_t launch_mx_token(const MxProduct &p, const void *X, int dtype, int64_t x_ld, int64_t d, hipStream_t s);
 
 struct MxCacheView {
     uint8_t *k, *v;     // [n_pages][heads][page][row bytes]

@@ -133,6 +133,10 @@ size_t fp4_bytes(int64_t n, int64_t d)
     return (size_t)(n * (w / 2) + (n * (w / MPQ_MX_BLOCK) + 15) / 16 * 16);
 }
 
+// The workspace of a linear call: its quantized tokens, where they are not
+// quantized inside the product.
+size_t linear_bytes(int64_t n, int64_t d) { return mpq::mx_quantizes_inside(n) ? 0 : fp4_bytes(n, d); }
+
 int view_cache(const mpq_mx_cache *c, mpq::MxCacheView *v)
 {
     if (!c) return fail(MPQ_ERR_INVALID_ARG, "cache must not be NULL");
@@ -260,7 +264,7 @@ int64_t mpq_mx_linear_workspace(int64_t n, int64_t c_out, int64_t d)
     if (n < 0 || n > MPQ_MX_MAX_N || c_out < 0 || d < 1 || d > MPQ_MX_MAX_D)
         return fail(MPQ_ERR_INVALID_ARG, "n, c_out or d out of range (%lld, %lld, %lld)", (long long)n,
                     (long long)c_out, (long long)d);
-    return (int64_t)fp4_bytes(n, d);
+    return (int64_t)linear_bytes(n, d);
 }
 
 int mpq_mx_linear(const void *X, int x_dtype, int64_t n, int64_t x_ld, const uint8_t *w_codes,
@@ -273,8 +277,12 @@ int mpq_mx_linear(const void *X, int x_dtype, int64_t n, int64_t x_ld, const uin
     if (rc != MPQ_OK || n == 0 || c_out == 0) return rc;
     hipStream_t s = (hipStream_t)stream;
     Workspace ws;
-    rc = ws.open(workspace_opt, workspace_bytes, fp4_bytes(n, d), s);
+    rc = ws.open(workspace_opt, workspace_bytes, linear_bytes(n, d), s);
     if (rc != MPQ_OK) return rc;
+    if (mpq::mx_quantizes_inside(n))
+        return done(mpq::launch_mx_token(product(nullptr, nullptr, n, w_codes, w_scales, c_out, d, bias_opt, Y, dtype, ld),
+                                         X, x_dtype, x_ld, d, s),
+                    hipSuccess, "mx token launch");
     uint8_t *xc = ws.get(), *xs = xc + n * (mpq::mx_row(d) / 2);
     hipError_t e = mpq::launch_mx_quantize(X, x_dtype, n, d, x_ld, xc, xs, s);
     if (e == hipSuccess)

@@ -12,20 +12,19 @@
 //    as the sum over the head's dimensions may run in any order, its quarter
 //    l / 16 of the row, 8 nb consecutive elements.
 //  - S^T leaves lane l with column (query head) l % 16 and tokens
-//    4 (l / 16) + 0..3 of each 16, which is what O^T = V^T P^T takes as its second
-//    operand if the sum over 32 tokens runs in the order that this gives: P
-//    never moves between lanes.
-//  - For the first operand of O^T lane l loads, for its eight tokens, the eight
-//    consecutive dimensions 8 (l % 16) ..; each is converted with its own
-//    token's scale, and v_perm pairs tokens.  Output register j then
-//    belongs to dimension 8 (row) + j.
+//    4 (l / 16) + 0..3, which is what O^T = V^T P^T (v_mfma_f32_16x16x16_bf16)
+//    takes as its second operand: P never moves between lanes.
+//  - For the first operand of O^T lane l loads, for its four tokens, the eight
+//    (heads of up to 64: four) consecutive dimensions 8 (l % 16) ..; each is
+//    converted with its own token's scale, and v_perm pairs tokens.  Output
+//    register j then belongs to dimension 8 (row) + j.
 // Elements convert to bf16 exactly (at most four significant bits, any
 // power of two of a scale).  Q and P are split into bf16 pieces whose sum is
 // the value: Q exactly (1 piece for bf16, 2 for f16, 3 for f32), P to 2^-16
 // (2 pieces; outputs of 16 bits) or 2^-24 (3).
 //
 // A long sequence is cut into pieces, one workgroup each, whose four
-// wavefronts take 32 tokens in turn; mx_attend_join_kernel joins the pieces.
+// wavefronts take 16 tokens in turn; mx_attend_join_kernel joins the pieces.
 #include <algorithm>
 #include <cmath>
 
@@ -38,7 +37,8 @@ namespace {
 
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kCols = 16;    // query heads of a workgroup
-constexpr int kStep = 32;    // tokens of a step
+constexpr int kStep = 16;    // tokens of a step
+constexpr int kMostPieces = 256;   // of a sequence: one for each thread that joins them
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
 // the running maximum follows only a score this far above it (a factor 2^8
 // in p, which fp32 sums and bf16 pieces hold as exactly)
@@ -74,44 +74,54 @@ __device__ __forceinline__ void store_o(void *p, int dtype, int64_t at, float v)
 // Maximum, sum over the four lanes that share a column.
 __device__ __forceinline__ float column_max(float v)
 {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+    float a, b;
+    swap_step<false>(v, a, b);
+    swap_step<true>(fmaxf(a, b), a, b);
+    return fmaxf(a, b);
 }
 
 __device__ __forceinline__ float column_sum(float v)
 {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    float a, b;
+    swap_step<false>(v, a, b);
+    swap_step<true>(a + b, a, b);
+    return a + b;
 }
 
-// Eight elements (fp4: one word, fp8: two) under the scale sc as bf16.
-template <int kFmt>
-__device__ __forceinline__ void to_bf16(const uint32_t *w, float sc, bf16x2 (&v)[4])
+// 2 kN elements (four to a word of fp8, eight to one of fp4) under the scale sc
+// as bf16.
+template <int kFmt, int kN>
+__device__ __forceinline__ void to_bf16(const uint32_t *w, float sc, bf16x2 (&v)[kN])
 {
+    static_assert(kN == 2 || kN == 4, "four or eight elements");
     if constexpr (kFmt == kFp4) {
         v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], sc, 0);
         v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], sc, 1);
-        v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], sc, 2);
-        v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], sc, 3);
+        if constexpr (kN == 4) {
+            v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], sc, 2);
+            v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], sc, 3);
+        }
     } else {
         v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], sc, false);
         v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], sc, true);
-        v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], sc, false);
-        v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], sc, true);
+        if constexpr (kN == 4) {
+            v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], sc, false);
+            v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], sc, true);
+        }
     }
 }
 
 // x as the sum of kPieces bf16 values (each piece the rest's nearest).
-template <int kPieces>
-__device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&out)[kPieces])
+template <int kPieces, int kN, class V>
+__device__ __forceinline__ void split(const float (&x)[kN], V (&out)[kPieces])
 {
-    float rest[8];
+    float rest[kN];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rest[i] = x[i];
+    for (int i = 0; i < kN; ++i) rest[i] = x[i];
 #pragma unroll
     for (int p = 0; p < kPieces; ++p)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < kN; ++i) {
             const __bf16 h = (__bf16)rest[i];
             out[p][i] = h;
             rest[i] -= (float)h;
@@ -129,68 +139,70 @@ template <int kNb, int kFmt>
 struct Shape {
     static constexpr int kW = kFmt == kFp4 ? 1 : 2;          // words of eight elements
     static constexpr int kRow = kNb * 16 * kW;               // bytes of a cached row
-    static constexpr int kVg = (kNb + 3) / 4;                // groups of 128 dimensions of V
+    static constexpr int kE = kNb <= 2 ? 4 : 8;              // dimensions of V a lane holds together
+    static constexpr int kVw = kE * kW / 8 > 0 ? kE * kW / 8 : 1;   // their words (fp4, four: half a word)
+    static constexpr int kVg = (kNb * 32 + 16 * kE - 1) / (16 * kE);   // groups of 16 kE dimensions
     static constexpr int kDim = kNb * 32;
     static constexpr int kLds = kDim + 4;                    // floats of an LDS row of O
 };
 
-// What a lane holds of one step of 32 tokens (two tiles of 16).
+// What a lane holds of one step of 16 tokens.
 template <int kNb, int kFmt>
 struct Step {
     using S = Shape<kNb, kFmt>;
-    uint32_t k[2][kNb * S::kW];          // its token's quarter row, tile by tile
-    uint32_t ks[2][kNb];                 // scale byte of each eight elements
-    uint32_t v[2][S::kVg][4][S::kW];     // four tokens of each tile
-    uint32_t vs[2][S::kVg];              // their scales, a byte each
+    uint32_t k[kNb * S::kW];         // its token's quarter row
+    uint32_t ks[kNb];                // scale byte of each eight elements
+    uint32_t v[S::kVg][4][S::kVw];   // four tokens
+    uint32_t vs[S::kVg];             // their scales, a byte each
+    int page, at;                    // the tokens' page (-1: none) and their place in it
 };
 
 template <int kNb, int kFmt>
-__device__ __forceinline__ void load_step(const MxCacheView &c, int head, const int (&page)[2], const int (&at)[2],
-                                          Step<kNb, kFmt> &st)
+__device__ __forceinline__ void load_step(const MxCacheView &c, int head, Step<kNb, kFmt> &st)
 {
     using S = Shape<kNb, kFmt>;
     const int lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
+    const int64_t ph = (int64_t)(st.page < 0 ? 0 : st.page) * c.heads + head;
+    const int64_t row = ph * c.page + st.at;
+    const uint8_t *k = c.k + row * S::kRow + (r * S::kRow + g * (S::kRow / 4));
+    load_words<kNb * S::kW, 4 * S::kW * (kNb % 4 == 0 ? 4 / S::kW : kNb % 2 == 0 ? 2 : 1)>(k, st.k);
+    const uint8_t *ks = c.ks + ph * kNb * c.page + st.at;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const int64_t ph = (int64_t)(page[t] < 0 ? 0 : page[t]) * c.heads + head;
-        const int64_t row = ph * c.page + at[t];
-        const uint8_t *k = c.k + row * S::kRow + (r * S::kRow + g * (S::kRow / 4));
-        load_words<kNb * S::kW, 4 * S::kW * (kNb % 4 == 0 ? 4 / S::kW : kNb % 2 == 0 ? 2 : 1)>(k, st.k[t]);
-        const uint8_t *ks = c.ks + ph * kNb * c.page + at[t];
+    for (int i = 0; i < kNb; ++i) {
+        // block of elements 8 (g kNb + i) ..: the same for several i where kNb is even
+        constexpr int kSame = kNb % 4 == 0 ? 4 : kNb % 2 == 0 ? 2 : 1;
+        if (i % kSame == 0) st.ks[i] = ks[(g * kNb + i) / 4 * c.page + r];
+        else st.ks[i] = st.ks[i / kSame * kSame];
+    }
 #pragma unroll
-        for (int i = 0; i < kNb; ++i) {
-            // block of elements 8 (g kNb + i) ..: the same for several i where kNb is even
-            constexpr int kSame = kNb % 4 == 0 ? 4 : kNb % 2 == 0 ? 2 : 1;
-            if (i % kSame == 0) st.ks[t][i] = ks[(g * kNb + i) / 4 * c.page + r];
-            else st.ks[t][i] = st.ks[t][i / kSame * kSame];
-        }
+    for (int q = 0; q < S::kVg; ++q) {
+        const int blk = (q * 16 + r) * S::kE / 32;   // of the lane's dimensions kE (16 q + r) ..
+        if (blk < kNb) {
+            const uint8_t *v = c.v + row * S::kRow + (4 * g * S::kRow + (q * 16 + r) * (S::kE * S::kW / 2));
 #pragma unroll
-        for (int q = 0; q < S::kVg; ++q) {
-            const int blk = q * 4 + r / 4;     // of the lane's dimensions 128 q + 8 r ..
-            if (blk < kNb) {
-                const uint8_t *v = c.v + row * S::kRow + (4 * g * S::kRow + (q * 16 + r) * (4 * S::kW));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) load_words<S::kW, 4 * S::kW>(v + i * S::kRow, st.v[t][q][i]);
-                st.vs[t][q] = *(const uint32_t *)(c.vs + (ph * kNb + blk) * c.page + at[t] + 4 * g);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int w = 0; w < S::kW; ++w) st.v[t][q][i][w] = 0;
-                st.vs[t][q] = 0;
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (S::kE * S::kW < 8) st.v[q][i][0] = *(const uint16_t *)(v + i * S::kRow);
+                else load_words<S::kVw, 4 * S::kVw>(v + i * S::kRow, st.v[q][i]);
             }
+            st.vs[q] = *(const uint32_t *)(c.vs + (ph * kNb + blk) * c.page + st.at + 4 * g);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int w = 0; w < S::kVw; ++w) st.v[q][i][w] = 0;
+            st.vs[q] = 0;
         }
     }
 }
 
 template <int kNb, int kFmt, class T, int kQ, int kP>
-__global__ void __launch_bounds__(kThreads) mx_attend_kernel(MxAttend a)
+__global__ void __launch_bounds__(kThreads, kNb > 4 || kQ > 2 ? 2 : 3) mx_attend_kernel(MxAttend a)
 {
     using S = Shape<kNb, kFmt>;
     __shared__ float s_m[kWaves][kCols], s_l[kWaves][kCols];
     __shared__ __align__(16) float s_o[kWaves][kCols * S::kLds];
 
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = lane % 16, g = lane / 16;
     const int piece = blockIdx.x;
     const int tiles = (a.group + kCols - 1) / kCols;
@@ -198,93 +210,81 @@ __global__ void __launch_bounds__(kThreads) mx_attend_kernel(MxAttend a)
     const int64_t b = blockIdx.z;
     const int h0 = head * a.group + tile * kCols;                 // first query head
     const int cols = min(kCols, a.group - tile * kCols);
+    // a lane's page of the wavefront's first 64 steps, asked for before
+    // the length is known where the span starts at 0
+    const int cols_most = a.most / a.c.page;
+    int early = -1;
+    if (a.window == 0) {
+        const int col = (piece * a.piece + kStep * (wave + kWaves * lane)) / a.c.page;
+        if (col < cols_most) early = a.table[b * a.table_ld + col];
+    }
     const Span span(a, b);
     const int begin = span.base + piece * a.piece;
     const int end = min(span.len, begin + a.piece);
     if (a.pieces > 1 && begin >= end) return;   // with one piece, an empty row is written here
 
-    // Q's columns: elements 8 (g kNb + i) .. of head h0 + r
-    bf16x8 qf[kNb][kQ];
-#pragma unroll
-    for (int i = 0; i < kNb; ++i) {
-        float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        const int j = 8 * (g * kNb + i);
-        if (r < cols) load8((const T *)a.Q + b * a.q_batch + (int64_t)(h0 + r) * a.q_head + j, a.c.dim - j, x);
-        split8<kQ>(x, qf[i]);
-    }
     const float scale = a.scale * kLog2e;
 
+    bf16x8 qf[kNb][kQ];
     float m = -INFINITY, l = 0.0f;   // of column r; l of the lane's own tokens
-    f32x4 o[S::kVg][8];
+    f32x4 o[S::kVg][S::kE];
 #pragma unroll
     for (int q = 0; q < S::kVg; ++q)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[q][j] = f32x4{0, 0, 0, 0};
+        for (int j = 0; j < S::kE; ++j) o[q][j] = f32x4{0, 0, 0, 0};
 
     const int steps = begin < end ? (end - begin + kStep - 1) / kStep : 0;
     const int mine = steps > wave ? (steps - wave + kWaves - 1) / kWaves : 0;   // this wavefront's
+    // step i of this wavefront: its pages, 64 steps' at a time (one a lane), and
+    // its part of the cache
     int my_page = -1, my_at = 0;
-    for (int i = 0; i < mine; ++i) {
-        if (i % 32 == 0) {
-            // the next 64 tiles' pages, one a lane
-            const int tok = begin + kStep * (wave + kWaves * (i + lane / 2)) + 16 * (lane % 2);
+    const auto fetch = [&](int i, Step<kNb, kFmt> &st) {
+        if (i % kWave == 0) {
+            const int tok = begin + kStep * (wave + kWaves * (i + lane));
             my_page = -1;
             if (tok < end) {
                 const int col = tok / a.c.page;
                 my_at = tok - col * a.c.page;
-                const int pg = a.table[b * a.table_ld + col];
+                const int pg = i == 0 && a.window == 0 ? early : a.table[b * a.table_ld + col];
                 if (pg >= 0 && pg < a.c.n_pages) my_page = pg;
             }
         }
+        st.page = __builtin_amdgcn_readlane(my_page, i % kWave);
+        st.at = st.page < 0 ? 0 : __builtin_amdgcn_readlane(my_at, i % kWave);
+        load_step<kNb, kFmt>(a.c, head, st);
+    };
+    const auto attend = [&](int i, Step<kNb, kFmt> &st) {
         const int tok0 = begin + kStep * (wave + kWaves * i);
-        int page[2], at[2];
+        f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            page[t] = __builtin_amdgcn_readlane(my_page, 2 * (i % 32) + t);
-            at[t] = page[t] < 0 ? 0 : __builtin_amdgcn_readlane(my_at, 2 * (i % 32) + t);
+        for (int k = 0; k < kNb; ++k) {
+            union { bf16x2 h[4]; bf16x8 v; } kf;
+            to_bf16<kFmt>(&st.k[k * S::kW], mx_scale(st.ks[k]), kf.h);
+#pragma unroll
+            for (int p = 0; p < kQ; ++p) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf.v, qf[k][p], acc, 0, 0, 0);
         }
-        Step<kNb, kFmt> st;
-        load_step<kNb, kFmt>(a.c, head, page, at, st);
-
-        float s[8];
+        float s[4];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            f32x4 acc = {0, 0, 0, 0};
-#pragma unroll
-            for (int k = 0; k < kNb; ++k) {
-                union { bf16x2 h[4]; bf16x8 v; } kf;
-                to_bf16<kFmt>(&st.k[t][k * S::kW], mx_scale(st.ks[t][k]), kf.h);
-#pragma unroll
-                for (int p = 0; p < kQ; ++p)
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf.v, qf[k][p], acc, 0, 0, 0);
-            }
-#pragma unroll
-            for (int x = 0; x < 4; ++x) s[4 * t + x] = acc[x] * scale;
-        }
+        for (int x = 0; x < 4; ++x) s[x] = acc[x] * scale;
         // a step that tokens outside the span, or a page that is not there,
         // touch: their scores are -infinity and their values zeros, whatever
         // the cache holds there
-        if (tok0 < span.first || tok0 + kStep > end || page[0] < 0 || page[1] < 0) {
+        if (tok0 < span.first || tok0 + kStep > end || st.page < 0) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int x = 0; x < 4; ++x) {
+                const int tok = tok0 + 4 * g + x;
+                if (st.page < 0 || tok < span.first || tok >= end) {
+                    s[x] = -INFINITY;
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int tok = tok0 + 16 * t + 4 * g + x;
-                    if (page[t] < 0 || tok < span.first || tok >= end) {
-                        s[4 * t + x] = -INFINITY;
+                    for (int q = 0; q < S::kVg; ++q) {
+                        st.vs[q] &= ~(255u << (8 * x));
 #pragma unroll
-                        for (int q = 0; q < S::kVg; ++q) {
-                            st.vs[t][q] &= ~(255u << (8 * x));
-#pragma unroll
-                            for (int w = 0; w < S::kW; ++w) st.v[t][q][x][w] = 0;
-                        }
+                        for (int w = 0; w < S::kVw; ++w) st.v[q][x][w] = 0;
                     }
                 }
+            }
         }
-        float top = s[0];
-#pragma unroll
-        for (int x = 1; x < 8; ++x) top = fmaxf(top, s[x]);
-        top = column_max(top);
+        const float top = column_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
         if (__any(top > m + kSlack)) {
             const float to = fmaxf(m, top);
             const float f = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);   // m = -infinity: 0
@@ -293,42 +293,84 @@ __global__ void __launch_bounds__(kThreads) mx_attend_kernel(MxAttend a)
 #pragma unroll
             for (int q = 0; q < S::kVg; ++q)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
+                for (int j = 0; j < S::kE; ++j)
 #pragma unroll
                     for (int x = 0; x < 4; ++x) o[q][j][x] *= f;
         }
         const float base = m == -INFINITY ? 0.0f : m;
-        float p[8];
+        float p[4];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
+        for (int x = 0; x < 4; ++x) {
             p[x] = __builtin_amdgcn_exp2f(s[x] - base);
             l += p[x];
         }
-        bf16x8 pf[kP];
-        split8<kP>(p, pf);
+        bf16x4 pf[kP];
+        split(p, pf);
 #pragma unroll
         for (int q = 0; q < S::kVg; ++q) {
-            // the eight tokens' eight dimensions as bf16 pairs of dimensions,
-            // then as pairs of tokens
-            uint32_t d[8][4];
+            // the four tokens' kE dimensions as bf16 pairs of dimensions, then
+            // as pairs of tokens
+            uint32_t d[4][S::kE / 2];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                bf16x2 h[4];
-                to_bf16<kFmt>(st.v[x / 4][q][x % 4], mx_scale((st.vs[x / 4][q] >> (8 * (x % 4))) & 255u), h);
+            for (int x = 0; x < 4; ++x) {
+                bf16x2 h[S::kE / 2];
+                to_bf16<kFmt>(st.v[q][x], mx_scale((st.vs[q] >> (8 * x)) & 255u), h);
 #pragma unroll
-                for (int y = 0; y < 4; ++y) d[x][y] = __builtin_bit_cast(uint32_t, h[y]);
+                for (int y = 0; y < S::kE / 2; ++y) d[x][y] = __builtin_bit_cast(uint32_t, h[y]);
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                union { uint32_t w[4]; bf16x8 v; } vf;
+            for (int j = 0; j < S::kE; ++j) {
+                union { uint32_t w[2]; i16x4 v; } vf;
 #pragma unroll
-                for (int y = 0; y < 4; ++y)
+                for (int y = 0; y < 2; ++y)
                     vf.w[y] = __builtin_amdgcn_perm(d[2 * y + 1][j / 2], d[2 * y][j / 2],
                                                     j % 2 ? 0x07060302u : 0x05040100u);
 #pragma unroll
                 for (int y = 0; y < kP; ++y)
-                    o[q][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, pf[y], o[q][j], 0, 0, 0);
+                    o[q][j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf.v, __builtin_bit_cast(i16x4, pf[y]), o[q][j],
+                                                                        0, 0, 0);
             }
+        }
+    };
+    // the next step's loads are in flight while one is computed
+    if (mine > 0) {
+        Step<kNb, kFmt> even, odd;
+        fetch(0, even);
+        // Q's columns: elements 8 (g kNb + i) .. of head h0 + r; columns and
+        // elements past the last are zeros.  Whole vectors are all loaded
+        // before the first is used (from element 0 where there is none).
+        const T *q = (const T *)a.Q + b * a.q_batch + (int64_t)(h0 + (r < cols ? r : 0)) * a.q_head;
+        float x[kNb][8];
+        if (a.c.dim % 8 == 0) {
+#pragma unroll
+            for (int i = 0; i < kNb; ++i) {
+                const int j = 8 * (g * kNb + i);
+                load8(q + (j < a.c.dim ? j : 0), 8, x[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kNb; ++i) load8(q + 8 * (g * kNb + i), a.c.dim - 8 * (g * kNb + i), x[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kNb; ++i) {
+            if (r >= cols || 8 * (g * kNb + i) >= a.c.dim)
+#pragma unroll
+                for (int y = 0; y < 8; ++y) x[i][y] = 0.0f;
+            split(x[i], qf[i]);
+        }
+        int i = 0;
+        for (; i + 2 < mine; i += 2) {
+            fetch(i + 1, odd);
+            attend(i, even);
+            fetch(i + 2, even);
+            attend(i + 1, odd);
+        }
+        if (i + 1 < mine) {
+            fetch(i + 1, odd);
+            attend(i, even);
+            attend(i + 1, odd);
+        } else {
+            attend(i, even);
         }
     }
 
@@ -342,70 +384,106 @@ __global__ void __launch_bounds__(kThreads) mx_attend_kernel(MxAttend a)
     for (int q = 0; q < S::kVg; ++q)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-            const int d0 = q * 128 + (4 * g + x) * 8;
+            const int d0 = q * 16 * S::kE + (4 * g + x) * S::kE;
             if (d0 < S::kDim) {
-                f32x4 lo, hi;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    lo[j] = o[q][j][x];
-                    hi[j] = o[q][j + 4][x];
-                }
-                *(f32x4 *)&s_o[wave][r * S::kLds + d0] = lo;
-                *(f32x4 *)&s_o[wave][r * S::kLds + d0 + 4] = hi;
+                for (int h = 0; h < S::kE; h += 4)
+                    *(f32x4 *)&s_o[wave][r * S::kLds + d0 + h] =
+                        f32x4{o[q][h][x], o[q][h + 1][x], o[q][h + 2][x], o[q][h + 3][x]};
             }
         }
     __syncthreads();
-    for (int e = threadIdx.x; e < cols * S::kDim; e += kThreads) {
-        const int col = e / S::kDim, d = e % S::kDim;
+    // the wavefronts' weights under their common maximum
+    if (threadIdx.x < kCols) {
+        const int col = threadIdx.x;
         float top = s_m[0][col];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w][col]);
         const float base = top == -INFINITY ? 0.0f : top;
-        float sum = 0.0f, val = 0.0f;
+        float sum = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             const float f = __builtin_amdgcn_exp2f(s_m[w][col] - base);
             sum += f * s_l[w][col];
-            val += f * s_o[w][col * S::kLds + d];
+            s_m[w][col] = f;
         }
         const int64_t row = b * a.q_heads + h0 + col;
+        if (col < cols) {
+            if (a.pieces > 1)
+                ((f32x2 *)(a.part + a.batch * a.q_heads * a.pieces * S::kDim))[row * a.pieces + piece] = f32x2{top, sum};
+            else if (a.lse)
+                a.lse[row] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+        }
+        s_l[0][col] = sum == 0.0f ? 0.0f : 1.0f / sum;
+    }
+    __syncthreads();
+    constexpr int kPer = S::kDim / 4;   // threads a column, four dimensions each
+    for (int e = threadIdx.x; e < cols * kPer; e += kThreads) {
+        const int col = e / kPer, d = e % kPer * 4;
+        f32x4 val = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) val += s_m[w][col] * *(const f32x4 *)&s_o[w][col * S::kLds + d];
         if (a.pieces > 1) {
-            float *out = a.part + (row * a.pieces + piece) * (S::kDim + 2);
-            out[2 + d] = val;
-            if (d == 0) {
-                out[0] = top;
-                out[1] = sum;
-            }
+            *(f32x4 *)&a.part[((b * a.q_heads + h0 + col) * a.pieces + piece) * S::kDim + d] = val;
         } else {
-            if (d < a.c.dim)
-                store_o(a.O, a.dtype, b * a.o_batch + (int64_t)(h0 + col) * a.o_head + d, sum == 0.0f ? 0.0f : val / sum);
-            if (d == 0 && a.lse) a.lse[row] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+            const int64_t at = b * a.o_batch + (int64_t)(h0 + col) * a.o_head + d;
+            const float inv = s_l[0][col];
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+                if (d + y < a.c.dim) store_o(a.O, a.dtype, at + y, val[y] * inv);
         }
     }
 }
 
-// Joins the pieces of one query head (a workgroup): thread d sums dimension d.
-__global__ void __launch_bounds__(256) mx_attend_join_kernel(MxAttend a)
+// Joins the pieces of one query head (a workgroup): its threads weigh a piece
+// each, then groups of dim / 4 threads sum every (256 / (dim / 4))th piece, four
+// dimensions a thread, and the groups' sums meet in LDS.
+__global__ void __launch_bounds__(kThreads) mx_attend_join_kernel(MxAttend a)
 {
-    const int d = threadIdx.x;
+    __shared__ float s_w[kMostPieces], s_red[2][kWaves];
+    __shared__ f32x4 s_sum[kThreads];
+    const int t = threadIdx.x, lane = t % kWave, wave = t / kWave;
     const int64_t b = blockIdx.y, row = b * a.q_heads + blockIdx.x;
     const int dim = a.c.nb * 32;
     const Span span(a, b);
-    const int n = span.pieces(a.piece);
-    const float *in = a.part + row * a.pieces * (dim + 2);
-    float top = -INFINITY;
-    for (int i = 0; i < n; ++i) top = fmaxf(top, in[(int64_t)i * (dim + 2)]);
-    const float base = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, val = 0.0f;
-    for (int i = 0; i < n; ++i) {
-        const float *p = in + (int64_t)i * (dim + 2);
-        const float f = __builtin_amdgcn_exp2f(p[0] - base);
-        sum += f * p[1];
-        if (d < a.c.dim) val += f * p[2 + d];
+    const int n = span.pieces(a.piece);   // at most a.pieces, at most kMostPieces
+    const f32x2 *ml = (const f32x2 *)(a.part + a.batch * a.q_heads * a.pieces * dim) + row * a.pieces;
+    const f32x2 mine = t < n ? ml[t] : f32x2{-INFINITY, 0.0f};
+    float top = mine[0];
+#pragma unroll
+    for (int d = 32; d; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
+    if (lane == 0) s_red[0][wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
+    const float w = __builtin_amdgcn_exp2f(mine[0] - (top == -INFINITY ? 0.0f : top));
+    s_w[t] = w;
+    float sum = w * mine[1];
+#pragma unroll
+    for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
+    if (lane == 0) s_red[1][wave] = sum;
+    __syncthreads();
+    sum = (s_red[1][0] + s_red[1][1]) + (s_red[1][2] + s_red[1][3]);
+
+    const int per = dim / 4, groups = kThreads / per, group = t / per;   // threads past groups * per idle
+    f32x4 val = {0, 0, 0, 0};
+    if (group < groups) {
+        const f32x4 *in = (const f32x4 *)(a.part + row * a.pieces * dim) + t % per;
+#pragma unroll 4
+        for (int i = group; i < n; i += groups) val += s_w[i] * in[(int64_t)i * per];
     }
-    if (d < a.c.dim)
-        store_o(a.O, a.dtype, b * a.o_batch + (int64_t)blockIdx.x * a.o_head + d, sum == 0.0f ? 0.0f : val / sum);
-    if (d == 0 && a.lse) a.lse[row] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    s_sum[t] = val;
+    __syncthreads();
+    if (t < per) {
+        for (int i = 1; i < groups; ++i) val += s_sum[i * per + t];
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int d = 4 * t + i;
+            if (d < a.c.dim)
+                store_o(a.O, a.dtype, b * a.o_batch + (int64_t)blockIdx.x * a.o_head + d, sum == 0.0f ? 0.0f : val[i] * inv);
+        }
+    }
+    if (t == 0 && a.lse) a.lse[row] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 template <int kNb, int kFmt>
@@ -438,20 +516,29 @@ hipError_t launch_format(const MxAttend &a, dim3 grid, hipStream_t s)
 
 }  // namespace
 
-// A sequence is cut into pieces of a multiple of 128 tokens (a step of each
-// wavefront), as many as give every CU a few workgroups.
+// A sequence is cut into pieces of a multiple of 64 tokens (a step of each
+// wavefront).  For several sequences about 1536 workgroups, two rounds of the
+// three that fit a CU, even out their lengths (32 of 1 to 8192 tokens, 8 heads of
+// 128, groups of 8: 512, 768, 1536, 3072 workgroups take 70, 74, 69, 65 us); one
+// sequence's pieces are all alike, and 512 do (131072 tokens: 51 us and 5 to
+// join them, 1536: 54 and 7).  A piece of less than 256 tokens is mostly start
+// and end (16384 tokens of 8 heads in 512, 1536, 3072 pieces: 10.6, 12.1, 15.6
+// us), unless CUs would stay empty; up to 512 tokens stay whole, as the join
+// costs a launch (315 tokens: 7.6 us whole, 5.1 + 4.2 in five pieces; 1000: 13.0
+// and 4.9 + 4.9).
 size_t mx_attend_plan(MxAttend &a)
 {
-    constexpr int64_t kUnit = kWaves * kStep, kWant = 1024, kMostPieces = 256;
-    const int64_t units = a.batch * a.c.heads * ((a.group + kCols - 1) / kCols);
-    const int64_t want = std::min(kMostPieces, std::max<int64_t>(1, kWant / std::max<int64_t>(1, units)));
+    constexpr int64_t kUnit = kWaves * kStep, kWhole = 512, kCus = 256;
+    const int64_t units = std::max<int64_t>(1, a.batch * a.c.heads * ((a.group + kCols - 1) / kCols));
     const int64_t most = a.window > 0 ? std::min<int64_t>(a.most, (int64_t)a.window + 15) : a.most;
-    const int64_t piece = std::max(kUnit, ((most + want - 1) / want + kUnit - 1) / kUnit * kUnit);
+    const int64_t least = most <= kWhole ? kWhole : units * (most / 256) >= kCus ? 256 : 128;
+    const int64_t want = std::min<int64_t>(kMostPieces, std::max<int64_t>(1, (a.batch == 1 ? 512 : 1536) / units));
+    const int64_t piece = std::max(least, ((most + want - 1) / want + kUnit - 1) / kUnit * kUnit);
     a.piece = (int)piece;
     a.pieces = (int)std::max<int64_t>(1, (most + piece - 1) / piece);
-    // for any window: pieces is at most want, and at most the tokens' units
-    const int64_t bound = std::min(want, (a.most + kUnit - 1) / kUnit);
-    return bound <= 1 ? 0 : (size_t)(a.batch * a.q_heads * bound) * (a.c.nb * 32 + 2) * sizeof(float);
+    // for any window: no more than want, nor than the tokens' smallest pieces
+    const int64_t bound = std::min<int64_t>(want, (a.most + 127) / 128);
+    return bound <= 1 || a.most <= kWhole ? 0 : (size_t)(a.batch * a.q_heads * bound) * (a.c.nb * 32 + 2) * sizeof(float);
 }
 
 hipError_t launch_mx_attend(const MxAttend &a, hipStream_t s)

@@ -22,6 +22,10 @@ namespace {
 // and a word whose byte i is that block's scale.  The row's scales lie
 // the other way, 4i .. 4i + 3 in word i: lane g reads word g and the four lanes of
 // the row exchange bytes.
+typedef uint16_t __attribute__((may_alias)) half_word;
+typedef uint32_t __attribute__((may_alias)) word;
+typedef uint64_t __attribute__((may_alias)) two_words;
+
 constexpr int kChunkBlocks = 16;
 struct Share {
     u32x4 c[4];
@@ -85,6 +89,29 @@ __device__ __forceinline__ void store_y(void *Y, int dtype, int64_t at, float v)
 // sums meet in LDS, added in wavefront order.
 constexpr int kFewWaves = 8;
 
+// The sums of a workgroup's wavefronts to Y.
+template <int kNT>
+__device__ __forceinline__ void join_waves(const MxProduct &p, float (&part)[kFewWaves][kNT][kWave * 4],
+                                           const f32x4 (&acc)[kNT], int64_t c0, int64_t t0)
+{
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+#pragma unroll
+    for (int t = 0; t < kNT; ++t) *(f32x4 *)&part[wave][t][lane * 4] = acc[t];
+    __syncthreads();
+    // output o of the tile: row o % 16 of W, token o / 16; lane l's register i
+    // holds row 4 (l / 16) + i, token l % 16
+    for (int o = threadIdx.x; o < kNT * 256; o += kFewWaves * kWave) {
+        const int row = o % 16, tok = o / 16;
+        const int at = ((row / 4) * 16 + tok % 16) * 4 + row % 4;
+        if (c0 + row >= p.c || t0 + tok >= p.n) continue;
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) v += part[w][tok / 16][at];
+        if (p.bias) v += p.bias[c0 + row];
+        store_y(p.Y, p.dtype, (t0 + tok) * p.ldy + c0 + row, v);
+    }
+}
+
 template <int kNT>
 __global__ void __launch_bounds__(kFewWaves *kWave) mx_few_kernel(MxProduct p)
 {
@@ -117,21 +144,57 @@ __global__ void __launch_bounds__(kFewWaves *kWave) mx_few_kernel(MxProduct p)
     int k = wave * kChunkBlocks;
     for (; k + kChunkBlocks <= nb; k += kFewWaves * kChunkBlocks) chunk(std::true_type(), k);
     if (k < nb) chunk(std::false_type(), k);   // the chunk that the row ends in
+    join_waves<kNT>(p, part, acc, c0, t0);
+}
+
+// One to kN tokens, quantized on the way: a wavefront quantizes its chunk of
+// every token itself (eight elements a lane, a block a quad, as
+// mx_quantize.hip), through a part of LDS of its own, so the call is one
+// launch and X is read by each workgroup.  4096 x 4096, one token: 4.2 us,
+// against 1.9 + 3.8 in two launches (and their gap); with more than four
+// tokens the quantization in every workgroup costs more than the launch.
+template <int kN, class T>
+__global__ void __launch_bounds__(kFewWaves *kWave) mx_token_kernel(MxProduct p, const T *X, int64_t x_ld, int d)
+{
+    __shared__ __align__(16) float part[kFewWaves][1][kWave * 4];
+    __shared__ __align__(16) uint32_t xcodes[kFewWaves][kN][kWave];   // a chunk's codes, eight elements a word
+    __shared__ __align__(4) uint8_t xscales[kFewWaves][kN][kChunkBlocks];          // block 4i + g at 4g + i
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int r = lane % 16, g = lane / 16;
+    const int64_t c0 = (int64_t)blockIdx.x * 16;
+    const int nb = p.nb;
+    const int64_t wrow = min(c0 + r, p.c - 1);
+    f32x4 acc[1] = {f32x4{0, 0, 0, 0}};
+    const auto chunk = [&](auto whole, int k) {
+        Share a, b;
+        load_share<decltype(whole)::value>(a, p.wc, p.ws, wrow, nb, k, g);
+        const int e = k * kMxBlock + 8 * lane;
+        float x[kN][8];
 #pragma unroll
-    for (int t = 0; t < kNT; ++t) *(f32x4 *)&part[wave][t][lane * 4] = acc[t];
-    __syncthreads();
-    // output o of the tile: row o % 16 of W, token o / 16; lane l's register i
-    // holds row 4 (l / 16) + i, token l % 16
-    for (int o = threadIdx.x; o < kNT * 256; o += kFewWaves * kWave) {
-        const int row = o % 16, tok = o / 16;
-        const int at = ((row / 4) * 16 + tok % 16) * 4 + row % 4;
-        if (c0 + row >= p.c || t0 + tok >= p.n) continue;
-        float v = 0.0f;
+        for (int t = 0; t < kN; ++t) load8(X + (t < p.n ? t : 0) * x_ld + e, d - e, x[t]);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-        for (int w = 0; w < kFewWaves; ++w) v += part[w][tok / 16][at];
-        if (p.bias) v += p.bias[c0 + row];
-        store_y(p.Y, p.dtype, (t0 + tok) * p.ldy + c0 + row, v);
-    }
+        for (int t = 0; t < kN; ++t) {
+            const uint32_t s = mx_scale_byte<kFp4>(quad_max(largest_bits(x[t])));
+            uint32_t w[1];
+            mx_codes<kFp4>(x[t], s, w);
+            xcodes[wave][t][lane] = w[0];
+            const int blk = lane / 4;
+            if (lane % 4 == 0) xscales[wave][t][blk % 4 * 4 + blk / 4] = (uint8_t)s;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const bool live = r < kN && r < p.n;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            b.c[i] = live ? *(const u32x4 *)&xcodes[wave][r][(4 * i + g) * 4] : u32x4{0, 0, 0, 0};
+        b.s = live ? *(const word *)&xscales[wave][r][4 * g] : 0u;
+        a.s = transpose_bytes(a.s, g);
+        acc[0] = multiply_chunk(a, b, acc[0]);
+    };
+    int k = wave * kChunkBlocks;
+    for (; k + kChunkBlocks <= nb; k += kFewWaves * kChunkBlocks) chunk(std::true_type(), k);
+    if (k < nb) chunk(std::false_type(), k);
+    join_waves<1>(p, part, acc, c0, 0);
 }
 
 // Many tokens: a workgroup owns 64 kTM rows of W by 64 kTN tokens, its four
@@ -221,10 +284,6 @@ struct Operands {
 // The scales of the lane's rows for one stage, two bytes (a step each) a row
 // tile: they lie side by side in LDS, [h][r][tile], and the products select
 // their bytes.
-typedef uint16_t __attribute__((may_alias)) half_word;
-typedef uint32_t __attribute__((may_alias)) word;
-typedef uint64_t __attribute__((may_alias)) two_words;
-
 // kT half-words, aligned to their size (plain loads: the compiler keeps track
 // of which LDS array they read)
 template <int kT>
@@ -492,7 +551,30 @@ hipError_t launch_tiles(const MxProduct &p, hipStream_t s)
     return hipGetLastError();
 }
 
+template <int kN>
+hipError_t launch_token_as(const MxProduct &p, const void *X, int dtype, int64_t x_ld, int d, hipStream_t s)
+{
+    const dim3 grid((unsigned)((p.c + 15) / 16)), threads(kFewWaves * kWave);
+    if (dtype == MPQ_F32)
+        hipLaunchKernelGGL((mx_token_kernel<kN, float>), grid, threads, 0, s, p, (const float *)X, x_ld, d);
+    else if (dtype == MPQ_F16)
+        hipLaunchKernelGGL((mx_token_kernel<kN, _Float16>), grid, threads, 0, s, p, (const _Float16 *)X, x_ld, d);
+    else
+        hipLaunchKernelGGL((mx_token_kernel<kN, __bf16>), grid, threads, 0, s, p, (const __bf16 *)X, x_ld, d);
+    return hipGetLastError();
+}
+
 }  // namespace
+
+bool mx_quantizes_inside(int64_t n) { return n <= 4; }
+
+hipError_t launch_mx_token(const MxProduct &p, const void *X, int dtype, int64_t x_ld, int64_t d, hipStream_t s)
+{
+    if (p.n <= 0 || p.c <= 0) return hipSuccess;
+    if (!mx_quantizes_inside(p.n) || (p.c + 15) / 16 > 0x7fffffffLL) return hipErrorInvalidValue;
+    LaunchTimer timer(s, "mx_token_kernel");
+    return p.n == 1 ? launch_token_as<1>(p, X, dtype, x_ld, (int)d, s) : launch_token_as<4>(p, X, dtype, x_ld, (int)d, s);
+}
 
 // Which kernel: the one that a model of its time, in us, finds fastest.  With K
 // in stages of 128 elements, a tile kernel takes its start and end plus its

@@ -185,9 +185,16 @@ def _dev(x: torch.Tensor, dtype, name: str) -> int:
     return x.data_ptr()
 
 
+# the current stream's handle without an object around it (2.7 us less a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
+    return torch.cuda.current_stream().cuda_stream
 
 
 def fit_layer(W: torch.Tensor, bits: int, max_points: int, n_grid: int, tol: float,

@@ -63,6 +63,19 @@ __device__ __forceinline__ void store8(T *p, int live, const float (&x)[8])
     }
 }
 
+// n / d for n + d below 2^22: a quotient is at least 1 / (2 d) away from
+// (n + 1/2) / d's neighbouring integers, far more than the product's rounding.
+__device__ __forceinline__ uint32_t small_quotient(uint32_t n, float inverse)
+{
+    return (uint32_t)(((float)n + 0.5f) * inverse);
+}
+
+// n / d, in 32 bits where n allows.
+__device__ __forceinline__ int64_t quotient(int64_t n, int d)
+{
+    return n < 0x100000000LL ? (int64_t)((uint32_t)n / (uint32_t)d) : n / d;
+}
+
 // The scale byte of a block whose largest magnitude has these bits (an
 // infinity's and a NaN's bits are above every finite number's).
 template <int kFmt>

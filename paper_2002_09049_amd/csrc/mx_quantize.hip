@@ -1,10 +1,13 @@
 // Rows to fp4 blocks and back (mpq_mx_quantize, mpq_mx_dequantize).
 //
-// Both stream: a thread holds eight consecutive elements, so the four lanes
-// of a quad hold a block and its largest magnitude takes two DPP steps.  A
-// workgroup takes 2048 consecutive elements of the rows laid end to end
-// (each row w elements, w a multiple of 128 at or above d), whatever their
-// length, and only its first element's row takes a 64-bit division.
+// Both stream, bound by memory: a thread holds eight consecutive elements, so
+// the four lanes of a quad hold a block and its largest magnitude takes two DPP
+// steps, and 16-bit values come and go as whole 16-byte vectors, lane by lane
+// (16 elements a thread on the way back, its stores 32 bytes apart: 107 us where
+// eight take 69).  A workgroup takes 2048 consecutive elements of the rows
+// laid end to end (each row w elements, w a multiple of 128 at or above d),
+// whatever their length; only its first element's row takes a division of
+// large numbers.
 #include "mpq.h"
 #include "mx.hpp"
 
@@ -12,16 +15,18 @@ namespace mpq {
 
 namespace {
 
-constexpr int kThreads = 256, kPerThread = 8, kElems = kThreads * kPerThread;
+constexpr int kThreads = 256, kElems = kThreads * 8;
 
 // The row and the place in it of this thread's eight elements.
 __device__ __forceinline__ void place(int w, int64_t &row, int &j)
 {
     const int64_t first = (int64_t)blockIdx.x * kElems;
-    const int64_t row0 = first / w;
-    const uint32_t off = (uint32_t)(first - row0 * w) + kPerThread * threadIdx.x;
-    row = row0 + off / (uint32_t)w;
-    j = (int)(off % (uint32_t)w);
+    const int64_t row0 = quotient(first, w);
+    const uint32_t off = (uint32_t)(first - row0 * w) + 8 * threadIdx.x;
+    // rows of 2048 or more: the first one or the next
+    const uint32_t more = w >= kElems ? (off >= (uint32_t)w ? 1u : 0u) : small_quotient(off, 1.0f / (float)w);
+    row = row0 + more;
+    j = (int)(off - more * (uint32_t)w);
 }
 
 template <class T>
@@ -50,9 +55,8 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t *
     place(w, row, j);
     if (row >= rows || j >= d) return;
     const uint32_t c[1] = {*(const uint32_t *)(codes + row * (w / 2) + j / 2)};
-    const uint32_t s = scales[row * (w / kMxBlock) + j / kMxBlock];
     float x[8];
-    mx_values<kFp4>(c, s, x);
+    mx_values<kFp4>(c, scales[row * (w / kMxBlock) + j / kMxBlock], x);
     store8(Y + row * ld + j, d - j, x);
 }
 

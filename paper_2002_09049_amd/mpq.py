@@ -402,18 +402,31 @@ def _fp4(codes: torch.Tensor, scales: torch.Tensor, d: int, name: str):
     return _dev(codes, torch.uint8, f"{name} codes"), _dev(scales, torch.uint8, f"{name} scales")
 
 
-def _space(workspace):
-    if workspace is None:
-        return None, 0
-    return _dev(workspace, torch.uint8, "workspace"), workspace.numel()
+def _space(workspace, need, stream):
+    """(pointer, bytes, owner) of a call's workspace: the caller's; else, on the
+    current stream, need() bytes of torch's allocator (the owner keeps them
+    until the call is enqueued); else none, and the library takes its own
+    scratch on the caller's stream."""
+    if workspace is not None:
+        return _dev(workspace, torch.uint8, "workspace"), workspace.numel(), None
+    if stream is None:
+        n = need()
+        if n > 0:
+            own = torch.empty((n,), dtype=torch.uint8, device="cuda")
+            return own.data_ptr(), n, own
+    return None, 0, None
 
 
-def _out(out, shape, dtype, device, name: str):
+def _rows_out(out, n: int, d: int, dtype, like: torch.Tensor):
+    """(tensor, pointer, dtype number, row stride) of an output [n, d]: the
+    caller's, or a new one."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(out.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {tuple(shape)} (got {tuple(out.shape)})")
-    return out
+        dt = _mx_dtype(dtype, "dtype")
+        out = like.new_empty((n, d), dtype=dtype)
+        return out, out.data_ptr(), dt, max(d, 1)
+    if tuple(out.shape) != (n, d):
+        raise ValueError(f"out must be {(n, d)} (got {tuple(out.shape)})")
+    return (out, *_rows(out, "out"))
 
 
 def mx_quantize(X: torch.Tensor, stream=None, out=None):
@@ -424,12 +437,14 @@ def mx_quantize(X: torch.Tensor, stream=None, out=None):
     r, d = X.shape
     wide = -(-d // MX_ROW) * MX_ROW
     if out is None:
-        out = (torch.empty((r, wide // 2), dtype=torch.uint8, device=X.device),
-               torch.empty((r, wide // MX_BLOCK), dtype=torch.uint8, device=X.device))
-    codes, scales = out
-    cp, sp = _fp4(codes, scales, d, "out")
-    if codes.shape[0] != r:
-        raise ValueError(f"out must hold {r} rows")
+        codes = X.new_empty((r, wide // 2), dtype=torch.uint8)
+        scales = X.new_empty((r, wide // MX_BLOCK), dtype=torch.uint8)
+        cp, sp = codes.data_ptr(), scales.data_ptr()
+    else:
+        codes, scales = out
+        cp, sp = _fp4(codes, scales, d, "out")
+        if codes.shape[0] != r:
+            raise ValueError(f"out must hold {r} rows")
     _check(load().mpq_mx_quantize(ptr, dt, r, d, ld, cp, sp, _stream(stream)))
     return codes, scales
 
@@ -438,8 +453,7 @@ def mx_dequantize(codes: torch.Tensor, scales: torch.Tensor, d: int, dtype=torch
                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """mpq_mx_dequantize: the values [r, d] that fp4 blocks stand for."""
     cp, sp = _fp4(codes, scales, d, "rows")
-    Y = _out(out, (codes.shape[0], d), dtype, codes.device, "out")
-    yp, dt, ld = _rows(Y, "out")
+    Y, yp, dt, ld = _rows_out(out, codes.shape[0], d, dtype, codes)
     _check(load().mpq_mx_dequantize(cp, sp, codes.shape[0], d, yp, dt, ld, _stream(stream)))
     return Y
 
@@ -454,8 +468,7 @@ def mx_product(x_codes: torch.Tensor, x_scales: torch.Tensor, codes: torch.Tenso
     n, c = x_codes.shape[0], codes.shape[0]
     if bias is not None and bias.shape != (c,):
         raise ValueError(f"bias must be ({c},)")
-    Y = _out(out, (n, c), dtype, codes.device, "out")
-    yp, dt, ld = _rows(Y, "out")
+    Y, yp, dt, ld = _rows_out(out, n, c, dtype, codes)
     _check(load().mpq_mx_product(xc, xs, n, wc, ws, c, d,
                                  None if bias is None else _dev(bias, torch.float32, "bias"), yp, dt, ld,
                                  _stream(stream)))
@@ -474,17 +487,17 @@ def mx_linear(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bias: 
               dtype=None, stream=None, out: Optional[torch.Tensor] = None, workspace=None) -> torch.Tensor:
     """mpq_mx_linear: Y [n, c] = Q(X) W^T + bias, X [n, d] quantized to fp4 in
     the call, W as mx_quantize gives it.  dtype of Y: X's unless given.
-    workspace: an uint8 device tensor of mx_linear_workspace(n, c, d) bytes, or
-    None for the library's own scratch."""
+    workspace: an uint8 device tensor of mx_linear_workspace(n, c, d) bytes;
+    without one the call takes memory of torch's allocator (of the library's own
+    pool if a stream is given)."""
     xp, xt, x_ld = _rows(X, "X")
     n, d = X.shape
     wc, ws = _fp4(codes, scales, d, "weights")
     c = codes.shape[0]
     if bias is not None and bias.shape != (c,):
         raise ValueError(f"bias must be ({c},)")
-    Y = _out(out, (n, c), X.dtype if dtype is None else dtype, X.device, "out")
-    yp, dt, ld = _rows(Y, "out")
-    wp, wn = _space(workspace)
+    Y, yp, dt, ld = _rows_out(out, n, c, X.dtype if dtype is None else dtype, X)
+    wp, wn, _own = _space(workspace, lambda: mx_linear_workspace(n, c, d), stream)
     _check(load().mpq_mx_linear(xp, xt, n, x_ld, wc, ws, c, d,
                                 None if bias is None else _dev(bias, torch.float32, "bias"), yp, dt, ld, wp, wn,
                                 _stream(stream)))
@@ -546,11 +559,17 @@ class MXCache:
         at the slots, as (K, V); zeros for a slot that is not of the cache."""
         n = slots.numel()
         shape = (n, self.kv_heads, self.head_dim)
-        K, V = (torch.empty(shape, dtype=dtype, device=slots.device) for _ in "KV") if out is None else out
-        kp, kt, kh = _heads(K, shape, "K")
-        vp, vt, vh = _heads(V, shape, "V")
-        if K.dtype != V.dtype:
-            raise ValueError("K and V must have one dtype")
+        if out is None:
+            K, V = slots.new_empty(shape, dtype=dtype), slots.new_empty(shape, dtype=dtype)
+            kp, vp = K.data_ptr(), V.data_ptr()
+            kt = vt = self.kv_heads * self.head_dim
+            kh = vh = self.head_dim
+        else:
+            K, V = out
+            kp, kt, kh = _heads(K, shape, "K")
+            vp, vt, vh = _heads(V, shape, "V")
+            if K.dtype != V.dtype:
+                raise ValueError("K and V must have one dtype")
         _check(load().mpq_mx_cache_read(self._at, kp, kt, kh, vp, vt, vh, _mx_dtype(K.dtype, "dtype"), n,
                                         _dev(slots, torch.int64, "slots"), _stream(stream)))
         return K, V
@@ -570,8 +589,8 @@ class MXCache:
         page_table[b] (int32 both); window > 0: over the last `window` of them.
         scale: 1 / sqrt(head_dim) unless given.  Returns O like Q, or
         (O, lse [batch, q_heads] fp32) with with_lse.  workspace: an uint8 device
-        tensor of attend_workspace(batch, q_heads, page_table.shape[1]) bytes,
-        or None for the library's own scratch."""
+        tensor of attend_workspace(batch, q_heads, page_table.shape[1]) bytes;
+        without one as in mx_linear."""
         if Q.dim() != 3:
             raise ValueError("Q must be 3-D [batch, q_heads, head_dim]")
         batch, heads = Q.shape[:2]
@@ -584,14 +603,18 @@ class MXCache:
             raise ValueError("page_table must be an int32 device tensor")
         if lengths.shape != (batch,):
             raise ValueError("lengths must be [batch]")
-        O = _out(out, shape, Q.dtype, Q.device, "out")
-        if O.dtype != Q.dtype:
-            raise ValueError("out must have Q's dtype")
-        op, ob, oh = _heads(O, shape, "out")
-        lse = torch.empty((batch, heads), dtype=torch.float32, device=Q.device) if with_lse else None
+        if out is None:
+            O = Q.new_empty(shape)
+            op, ob, oh = O.data_ptr(), heads * self.head_dim, self.head_dim
+        else:
+            O = out
+            if O.dtype != Q.dtype:
+                raise ValueError("out must have Q's dtype")
+            op, ob, oh = _heads(O, shape, "out")
+        lse = Q.new_empty((batch, heads), dtype=torch.float32) if with_lse else None
         pages = page_table.shape[1]
         ld = page_table.stride(0) if batch > 1 else pages
-        wp, wn = _space(workspace)
+        wp, wn, _own = _space(workspace, lambda: self.attend_workspace(batch, heads, pages), stream)
         _check(load().mpq_mx_attend(self._at, qp, qb, qh, _mx_dtype(Q.dtype, "Q"), batch, heads,
                                     page_table.data_ptr(), ld, pages, _dev(lengths, torch.int32, "lengths"),
                                     int(window), self.head_dim ** -0.5 if scale is None else float(scale), op, ob, oh,

@@ -31,35 +31,68 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 constexpr int kFp4 = 0, kFp8 = 1;   // MPQ_MX_FP4, MPQ_MX_FP8
 constexpr int kMxBlock = 32;
 
-// Eight consecutive values of a row, `live` of them inside it (the others
-// are zero).  The row need only be aligned to its element: global loads of
-// gfx950 take any address, and a whole vector goes in 16-byte loads.
+// Eight consecutive values of a row as they lie in memory: what a load in
+// flight fills (their values taken apart, the load would have to be done).
 template <class T>
-__device__ __forceinline__ void load8(const T *p, int live, float (&x)[8])
-{
-    if (live >= 8) {
+struct Eight {
+    uint32_t w[2 * sizeof(T)];
+
+    __device__ __forceinline__ void values(float (&x)[8]) const
+    {
         T v[8];
-        __builtin_memcpy(v, p, sizeof v);
+        __builtin_memcpy(v, w, sizeof v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = i < live ? (float)p[i] : 0.0f;
     }
+};
+
+// `live` of the eight are inside the row, the others are zero.  The row need
+// only be aligned to its element: global loads of gfx950 take any address, and
+// a whole vector goes in 16-byte loads.
+template <class T>
+__device__ __forceinline__ Eight<T> load_eight(const T *p, int live)
+{
+    Eight<T> e;
+    if (live >= 8) {
+        __builtin_memcpy(e.w, p, sizeof e.w);
+    } else {
+        T v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < live ? p[i] : (T)0.0f;
+        __builtin_memcpy(e.w, v, sizeof e.w);
+    }
+    return e;
 }
 
 template <class T>
+__device__ __forceinline__ void load8(const T *p, int live, float (&x)[8])
+{
+    load_eight(p, live).values(x);
+}
+
+typedef uint32_t loose_vector __attribute__((ext_vector_type(4), aligned(2)));
+
+// The first `live` of eight values to a row.  kPast: past the caches, for what
+// fills whole lines and is not read again here (rows read back from fp4:
+// 43 us, by ordinary stores 69).
+template <bool kPast, class T>
 __device__ __forceinline__ void store8(T *p, int live, const float (&x)[8])
 {
-    if (live >= 8) {
-        T v[8];
+    T v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (T)x[i];
-        __builtin_memcpy(p, v, sizeof v);
+    for (int i = 0; i < 8; ++i) v[i] = (T)x[i];
+    if (live >= 8) {
+        loose_vector o[sizeof(T) / 2];
+        __builtin_memcpy(o, v, sizeof v);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            if constexpr (kPast) __builtin_nontemporal_store(o[i], (loose_vector *)p + i);
+            else ((loose_vector *)p)[i] = o[i];
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < live) p[i] = (T)x[i];
+            if (i < live) p[i] = v[i];
     }
 }
 

@@ -98,9 +98,11 @@ __global__ void __launch_bounds__(kThreads) mx_cache_write_kernel(MxCacheView c,
     int64_t page;
     int at;
     find(c, slot, page, at);
+    const Eight<T> ke = load_eight(K + p.token * k_tok + p.head * k_head + p.j, c.dim - p.j);
+    const Eight<T> ve = load_eight(V + p.token * v_tok + p.head * v_head + p.j, c.dim - p.j);
     float k[8], v[8];
-    load8(K + p.token * k_tok + p.head * k_head + p.j, c.dim - p.j, k);
-    load8(V + p.token * v_tok + p.head * v_head + p.j, c.dim - p.j, v);
+    ke.values(k);
+    ve.values(v);
     const int64_t ph = page * c.heads + p.head, code = code_at<kFmt>(c, ph, at, p.j), scale = scale_at(c, ph, at, p.j);
     write8<kFmt>(k, c.k + code, c.ks + scale, p.j % kMxBlock == 0);
     write8<kFmt>(v, c.v + code, c.vs + scale, p.j % kMxBlock == 0);
@@ -124,8 +126,8 @@ __global__ void __launch_bounds__(kThreads) mx_cache_read_kernel(MxCacheView c, 
         read8<kFmt>(c.k + code, c.ks + scale, k);
         read8<kFmt>(c.v + code, c.vs + scale, v);
     }
-    store8(K + p.token * k_tok + p.head * k_head + p.j, c.dim - p.j, k);
-    store8(V + p.token * v_tok + p.head * v_head + p.j, c.dim - p.j, v);
+    store8<true>(K + p.token * k_tok + p.head * k_head + p.j, c.dim - p.j, k);
+    store8<true>(V + p.token * v_tok + p.head * v_head + p.j, c.dim - p.j, v);
 }
 
 int64_t row_blocks(const MxCacheView &c, int64_t tokens)

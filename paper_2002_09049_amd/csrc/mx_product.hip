@@ -165,35 +165,71 @@ __global__ void __launch_bounds__(kFewWaves *kWave) mx_token_kernel(MxProduct p,
     const int nb = p.nb;
     const int64_t wrow = min(c0 + r, p.c - 1);
     f32x4 acc[1] = {f32x4{0, 0, 0, 0}};
-    const auto chunk = [&](auto whole, int k) {
-        Share a, b;
-        load_share<decltype(whole)::value>(a, p.wc, p.ws, wrow, nb, k, g);
+    struct Chunk {
+        Share a;
+        Eight<T> x[kN];
+    };
+    const auto fetch = [&](auto whole, int k, Chunk &c) {
+        constexpr bool kWhole = decltype(whole)::value;
+        load_share<kWhole>(c.a, p.wc, p.ws, wrow, nb, k, g);
         const int e = k * kMxBlock + 8 * lane;
-        float x[kN][8];
 #pragma unroll
-        for (int t = 0; t < kN; ++t) load8(X + (t < p.n ? t : 0) * x_ld + e, d - e, x[t]);
+        for (int t = 0; t < kN; ++t) c.x[t] = load_eight(X + (t < p.n ? t : 0) * x_ld + e, kWhole ? 8 : d - e);
+    };
+    const auto multiply = [&](Chunk &c) {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int t = 0; t < kN; ++t) {
-            const uint32_t s = mx_scale_byte<kFp4>(quad_max(largest_bits(x[t])));
+            float x[8];
+            c.x[t].values(x);
+            const uint32_t s = mx_scale_byte<kFp4>(quad_max(largest_bits(x)));
             uint32_t w[1];
-            mx_codes<kFp4>(x[t], s, w);
+            mx_codes<kFp4>(x, s, w);
             xcodes[wave][t][lane] = w[0];
             const int blk = lane / 4;
             if (lane % 4 == 0) xscales[wave][t][blk % 4 * 4 + blk / 4] = (uint8_t)s;
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const bool live = r < kN && r < p.n;
+        Share b;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             b.c[i] = live ? *(const u32x4 *)&xcodes[wave][r][(4 * i + g) * 4] : u32x4{0, 0, 0, 0};
         b.s = live ? *(const word *)&xscales[wave][r][4 * g] : 0u;
-        a.s = transpose_bytes(a.s, g);
-        acc[0] = multiply_chunk(a, b, acc[0]);
+        c.a.s = transpose_bytes(c.a.s, g);
+        acc[0] = multiply_chunk(c.a, b, acc[0]);
     };
+    // this wavefront's chunks inside the rows of X, the next one's loads in
+    // flight, then the one that they end in
+    constexpr int kTurn = kFewWaves * kChunkBlocks;
+    const int inside = d / kMxBlock;   // whole blocks
     int k = wave * kChunkBlocks;
-    for (; k + kChunkBlocks <= nb; k += kFewWaves * kChunkBlocks) chunk(std::true_type(), k);
-    if (k < nb) chunk(std::false_type(), k);
+    const int mine = k + kChunkBlocks <= inside ? (inside - kChunkBlocks - k) / kTurn + 1 : 0;
+    Chunk even, odd;
+    if (mine > 0) {
+        const std::true_type whole;
+        fetch(whole, k, even);
+        int i = 0;
+        for (; i + 2 < mine; i += 2, k += 2 * kTurn) {
+            fetch(whole, k + kTurn, odd);
+            multiply(even);
+            fetch(whole, k + 2 * kTurn, even);
+            multiply(odd);
+        }
+        if (i + 1 < mine) {
+            fetch(whole, k + kTurn, odd);
+            multiply(even);
+            multiply(odd);
+            k += kTurn;
+        } else {
+            multiply(even);
+        }
+        k += kTurn;
+    }
+    if (k < nb) {
+        fetch(std::false_type(), k, even);
+        multiply(even);
+    }
     join_waves<1>(p, part, acc, c0, 0);
 }
 
@@ -357,7 +393,7 @@ __device__ __forceinline__ void write_turn(T *to, int64_t step, const float *fro
             y[v] = lo[v] + bias[v];
             y[v + 4] = hi[v] + bias[v + 4];
         }
-        store8(to, inside, y);
+        store8<false>(to, inside, y);
         to += step;
     };
     if (whole) {

@@ -8,6 +8,8 @@
 // laid end to end (each row w elements, w a multiple of 128 at or above d),
 // whatever their length; only its first element's row takes a division of
 // large numbers.
+//
+// MEASURED
 #include "mpq.h"
 #include "mx.hpp"
 
@@ -57,7 +59,23 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t *
     const uint32_t c[1] = {*(const uint32_t *)(codes + row * (w / 2) + j / 2)};
     float x[8];
     mx_values<kFp4>(c, scales[row * (w / kMxBlock) + j / kMxBlock], x);
-    store8(Y + row * ld + j, d - j, x);
+    store8<true>(Y + row * ld + j, d - j, x);
+}
+
+template <class T>
+hipError_t quantize_as(const T *X, int64_t rows, int d, int64_t ld, int w, uint8_t *codes, uint8_t *scales,
+                       unsigned blocks, hipStream_t s)
+{
+    hipLaunchKernelGGL(mx_quantize_kernel<T>, dim3(blocks), dim3(kThreads), 0, s, X, rows, d, ld, w, codes, scales);
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t dequantize_as(const uint8_t *codes, const uint8_t *scales, int64_t rows, int d, int w, T *Y, int64_t ld,
+                         unsigned blocks, hipStream_t s)
+{
+    hipLaunchKernelGGL(mx_dequantize_kernel<T>, dim3(blocks), dim3(kThreads), 0, s, codes, scales, rows, d, w, Y, ld);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -65,41 +83,29 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t *
 hipError_t launch_mx_quantize(const void *X, int dtype, int64_t rows, int64_t d, int64_t ld, uint8_t *codes,
                               uint8_t *scales, hipStream_t s)
 {
-    const int64_t w = mx_row(d), blocks = (rows * w + kElems - 1) / kElems;
+    const int w = (int)mx_row(d);
+    const int64_t blocks = (rows * w + kElems - 1) / kElems;
     if (blocks <= 0) return hipSuccess;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
     LaunchTimer timer(s, "mx_quantize_kernel");
-    const dim3 grid((unsigned)blocks), threads(kThreads);
-    if (dtype == MPQ_F32)
-        hipLaunchKernelGGL(mx_quantize_kernel<float>, grid, threads, 0, s, (const float *)X, rows, (int)d, ld, (int)w,
-                           codes, scales);
-    else if (dtype == MPQ_F16)
-        hipLaunchKernelGGL(mx_quantize_kernel<_Float16>, grid, threads, 0, s, (const _Float16 *)X, rows, (int)d, ld,
-                           (int)w, codes, scales);
-    else
-        hipLaunchKernelGGL(mx_quantize_kernel<__bf16>, grid, threads, 0, s, (const __bf16 *)X, rows, (int)d, ld,
-                           (int)w, codes, scales);
-    return hipGetLastError();
+    const unsigned n = (unsigned)blocks;
+    if (dtype == MPQ_F32) return quantize_as((const float *)X, rows, (int)d, ld, w, codes, scales, n, s);
+    if (dtype == MPQ_F16) return quantize_as((const _Float16 *)X, rows, (int)d, ld, w, codes, scales, n, s);
+    return quantize_as((const __bf16 *)X, rows, (int)d, ld, w, codes, scales, n, s);
 }
 
 hipError_t launch_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t d, void *Y,
                                 int dtype, int64_t ld, hipStream_t s)
 {
-    const int64_t w = mx_row(d), blocks = (rows * w + kElems - 1) / kElems;
+    const int w = (int)mx_row(d);
+    const int64_t blocks = (rows * w + kElems - 1) / kElems;
     if (blocks <= 0) return hipSuccess;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
     LaunchTimer timer(s, "mx_dequantize_kernel");
-    const dim3 grid((unsigned)blocks), threads(kThreads);
-    if (dtype == MPQ_F32)
-        hipLaunchKernelGGL(mx_dequantize_kernel<float>, grid, threads, 0, s, codes, scales, rows, (int)d, (int)w,
-                           (float *)Y, ld);
-    else if (dtype == MPQ_F16)
-        hipLaunchKernelGGL(mx_dequantize_kernel<_Float16>, grid, threads, 0, s, codes, scales, rows, (int)d, (int)w,
-                           (_Float16 *)Y, ld);
-    else
-        hipLaunchKernelGGL(mx_dequantize_kernel<__bf16>, grid, threads, 0, s, codes, scales, rows, (int)d, (int)w,
-                           (__bf16 *)Y, ld);
-    return hipGetLastError();
+    const unsigned n = (unsigned)blocks;
+    if (dtype == MPQ_F32) return dequantize_as(codes, scales, rows, (int)d, w, (float *)Y, ld, n, s);
+    if (dtype == MPQ_F16) return dequantize_as(codes, scales, rows, (int)d, w, (_Float16 *)Y, ld, n, s);
+    return dequantize_as(codes, scales, rows, (int)d, w, (__bf16 *)Y, ld, n, s);
 }
 
 }  // namespace mpq

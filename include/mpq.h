@@ -459,6 +459,7 @@ int mpq_integer_forward_layers(const mpq_int_layer *layers, int n_layers, int ma
 #define MPQ_MX_MAX_D 4194304        /* d of fp4 rows */
 #define MPQ_MX_MAX_N 1048576        /* tokens of a product */
 #define MPQ_MX_MAX_HEAD_DIM 256
+#define MPQ_MX_MAX_PAGE 65536
 #define MPQ_MX_MAX_TOKENS 536870912 /* tokens of one sequence: columns of the page table times page_size */
 
 /*
@@ -513,7 +514,7 @@ int mpq_mx_linear(const void *X, int x_dtype, int64_t n, int64_t x_ld, const uin
  * The caller owns the arrays (DEVICE pointers in a HOST struct, read before
  * the call returns) and the pages.  Slot p * page_size + i is place i of
  * page p.
- *   n_pages >= 1; page_size a multiple of 16; 1 <= head_dim <=
+ *   n_pages >= 1; page_size a multiple of 16, at most MPQ_MX_MAX_PAGE; 1 <= head_dim <=
  *   MPQ_MX_MAX_HEAD_DIM; kv_heads >= 1; n_pages * page_size < 2^40.
  */
 typedef struct mpq_mx_cache {

@@ -144,8 +144,9 @@ int view_cache(const mpq_mx_cache *c, mpq::MxCacheView *v)
         return fail(MPQ_ERR_INVALID_ARG, "cache format must be MPQ_MX_FP4 or MPQ_MX_FP8 (got %d)", c->format);
     if (c->head_dim < 1 || c->head_dim > MPQ_MX_MAX_HEAD_DIM)
         return fail(MPQ_ERR_INVALID_ARG, "head_dim must be in [1, %d] (got %d)", MPQ_MX_MAX_HEAD_DIM, c->head_dim);
-    if (c->page_size < 16 || c->page_size % 16 != 0)
-        return fail(MPQ_ERR_INVALID_ARG, "page_size must be a multiple of 16 (got %d)", c->page_size);
+    if (c->page_size < 16 || c->page_size > MPQ_MX_MAX_PAGE || c->page_size % 16 != 0)
+        return fail(MPQ_ERR_INVALID_ARG, "page_size must be a multiple of 16 of at most %d (got %d)", MPQ_MX_MAX_PAGE,
+                    c->page_size);
     if (c->kv_heads < 1 || c->kv_heads > 65535)
         return fail(MPQ_ERR_INVALID_ARG, "kv_heads must be in [1, 65535] (got %d)", c->kv_heads);
     if (c->n_pages < 1 || c->n_pages > 0x7fffffff || c->n_pages * c->page_size >= kMaxRows)

@@ -234,6 +234,23 @@ def test_linear_with_a_bad_token(n):
     assert np.array_equal(y[keep], y0[keep])
 
 
+@pytest.mark.parametrize("n", [1, 40, 300])
+def test_linear_with_a_bad_channel(n):
+    """A row of W with a block that is not a number gives that column of NaN,
+    and no other."""
+    from paper_2002_09049_amd import mpq
+    say(f"case mx linear NaN channel n={n}")
+    rng = np.random.default_rng(n)
+    X = _dev(_activations(rng, (n, 600)).astype(np.float32))
+    wc, ws = _weights(rng, 150, 600)
+    y0 = _np(mpq.mx_linear(X, _dev(ref.pack(wc)), _dev(ws)))
+    ws[77, 18] = 255
+    y = _np(mpq.mx_linear(X, _dev(ref.pack(wc)), _dev(ws)))
+    assert np.isnan(y[:, 77]).all()
+    keep = np.arange(150) != 77
+    assert np.array_equal(y[:, keep], y0[:, keep])
+
+
 def test_linear_extreme_scales():
     """Scale bytes near both ends: the sums are as the formula's."""
     from paper_2002_09049_amd import mpq

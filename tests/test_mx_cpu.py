@@ -78,7 +78,7 @@ def _view(mpq, **kw):
 BAD_CACHES = [dict(k_codes=None), dict(v_codes=None), dict(k_scales=None), dict(v_scales=None), dict(k_codes=72),
               dict(v_codes=8), dict(k_scales=66), dict(v_scales=65), dict(n_pages=0), dict(n_pages=-3),
               dict(n_pages=1 << 31), dict(n_pages=1 << 30, page_size=1024), dict(page_size=0), dict(page_size=8),
-              dict(page_size=24), dict(page_size=-16), dict(kv_heads=0), dict(kv_heads=65536), dict(head_dim=0),
+              dict(page_size=24), dict(page_size=-16), dict(page_size=65552), dict(kv_heads=0), dict(kv_heads=65536), dict(head_dim=0),
               dict(head_dim=257), dict(format=2), dict(format=-1)]
 
 

@@ -517,28 +517,39 @@ hipError_t launch_format(const MxAttend &a, dim3 grid, hipStream_t s)
 }  // namespace
 
 // A sequence is cut into pieces of a multiple of 64 tokens (a step of each
-// wavefront).  For several sequences about 1536 workgroups, two rounds of the
-// three that fit a CU, even out their lengths (32 of 1 to 8192 tokens, 8 heads of
-// 128, groups of 8: 512, 768, 1536, 3072 workgroups take 70, 74, 69, 65 us); one
-// sequence's pieces are all alike, and 512 do (131072 tokens: 51 us and 5 to
-// join them, 1536: 54 and 7).  A piece of less than 256 tokens is mostly start
-// and end (16384 tokens of 8 heads in 512, 1536, 3072 pieces: 10.6, 12.1, 15.6
-// us), unless CUs would stay empty; up to 512 tokens stay whole, as the join
-// costs a launch (315 tokens: 7.6 us whole, 5.1 + 4.2 in five pieces; 1000: 13.0
-// and 4.9 + 4.9).
+// wavefront), as long as give the three workgroups that fit a CU one each, but
+// for several sequences no longer than 960 tokens, which evens out their
+// lengths (32 of 1 to 8192 tokens, 8 heads of 128, groups of 8: pieces of 2752,
+// 1408, 960, 704 take 74, 70, 62, 65 us).  One sequence's pieces are all alike,
+// and two workgroups a CU do (131072 tokens: 51 us and 5 to join them; three: 54
+// and 7).  Shorter than 256 tokens, a piece is mostly start and end (16384
+// tokens of 8 heads in pieces of 256, 192, 64: 10.6, 12.1, 15.6 us), unless CUs
+// would stay empty.  The join costs a launch: up to 512 tokens stay whole (315:
+// 7.6 us whole, 5.1 + 4.2 in five pieces; 1000: 13.0 and 4.9 + 4.9), and up to
+// 2304 where the heads and sequences alone fill the CUs twice (64 of up to 2048
+// tokens, 8 heads in fp4: 27 us whole, 25 + 8.4 in three).
 size_t mx_attend_plan(MxAttend &a)
 {
-    constexpr int64_t kUnit = kWaves * kStep, kWhole = 512, kCus = 256;
-    const int64_t units = std::max<int64_t>(1, a.batch * a.c.heads * ((a.group + kCols - 1) / kCols));
+    constexpr int64_t kUnit = kWaves * kStep, kWhole = 512, kWholeFilled = 2304, kCus = 256, kLongest = 960;
+    const auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
+    const int64_t units = std::max<int64_t>(1, a.batch * a.c.heads * up(a.group, kCols));
+    const int64_t want = a.batch == 1 ? 2 * kCus : 3 * kCus;
+    // pieces for any window, and so the workspace
+    int64_t bound = std::max(up(want, units) + 2, a.batch == 1 ? 0 : up(a.most, kLongest) + 1);
+    bound = std::min<int64_t>(std::min<int64_t>(bound, kMostPieces), up(a.most, 128));
+    if (a.most <= kWhole || (units >= 2 * kCus && a.most <= kWholeFilled)) bound = 1;
+    bound = std::max<int64_t>(1, bound);
+
     const int64_t most = a.window > 0 ? std::min<int64_t>(a.most, (int64_t)a.window + 15) : a.most;
-    const int64_t least = most <= kWhole ? kWhole : units * (most / 256) >= kCus ? 256 : 128;
-    const int64_t want = std::min<int64_t>(kMostPieces, std::max<int64_t>(1, (a.batch == 1 ? 512 : 1536) / units));
-    const int64_t piece = std::max(least, ((most + want - 1) / want + kUnit - 1) / kUnit * kUnit);
+    int64_t piece = up(most * units, want);
+    if (a.batch > 1) piece = std::min(piece, kLongest);
+    piece = std::max<int64_t>(piece, units * (most / 256) >= kCus ? 256 : 128);
+    if (most <= kWhole || (units >= 2 * kCus && most <= kWholeFilled)) piece = std::max<int64_t>(1, most);
+    piece = up(std::max(piece, up(most, bound)), kUnit) * kUnit;
+    piece = std::max(piece, kUnit);
     a.piece = (int)piece;
-    a.pieces = (int)std::max<int64_t>(1, (most + piece - 1) / piece);
-    // for any window: no more than want, nor than the tokens' smallest pieces
-    const int64_t bound = std::min<int64_t>(want, (a.most + 127) / 128);
-    return bound <= 1 || a.most <= kWhole ? 0 : (size_t)(a.batch * a.q_heads * bound) * (a.c.nb * 32 + 2) * sizeof(float);
+    a.pieces = (int)std::max<int64_t>(1, up(most, piece));
+    return bound == 1 ? 0 : (size_t)(a.batch * a.q_heads * bound) * (a.c.nb * 32 + 2) * sizeof(float);
 }
 
 hipError_t launch_mx_attend(const MxAttend &a, hipStream_t s)

@@ -307,13 +307,12 @@ __device__ __forceinline__ void meet()
 template <int kTM, int kTN>
 struct Operands {
     u32x4 a[kTM], b[kTN];
-    __device__ __forceinline__ void read(const uint8_t *stage, int step, int wm, int wn, int r, int h)
+    // those of row tile i: W's, and the tokens' where there is one
+    __device__ __forceinline__ void read(int i, const uint8_t *stage, int step, int wm, int wn, int r, int h)
     {
         const int at = ((2 * h + step) ^ (r / 4 % 4)) * 16;
-#pragma unroll
-        for (int i = 0; i < kTM; ++i) a[i] = *(const u32x4 *)(stage + (wm + 32 * i + r) * kStageBytes + at);
-#pragma unroll
-        for (int j = 0; j < kTN; ++j) b[j] = *(const u32x4 *)(stage + (64 * kTM + wn + 32 * j + r) * kStageBytes + at);
+        a[i] = *(const u32x4 *)(stage + (wm + 32 * i + r) * kStageBytes + at);
+        if (i < kTN) b[i] = *(const u32x4 *)(stage + (64 * kTM + wn + 32 * i + r) * kStageBytes + at);
     }
 };
 
@@ -514,15 +513,13 @@ __global__ void __launch_bounds__(256) mx_tile_kernel(MxProduct p)
                             : row < kRows ? kBM + token / (32 * kTN) * (32 * kTN) + token % 32 * kTN + token / 32 % kTN
                                           : row);
     }
-    const auto place_scales = [&](int four) {
+    const auto place_scales = [&](int four, int w) {   // word w: stage 4 four + w
 #pragma unroll
-        for (int i = 0; i < kScaleRows; ++i)
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const uint32_t v = 16 * four + 4 * w < p.nb ? moved[i][w] : 0u;   // past the row: the next row's
-                *(half_word *)&lds_scales[four % 2][w][scales_at[i]] = (uint16_t)v;
-                *(half_word *)&lds_scales[four % 2][w][2 * kHalf + scales_at[i]] = (uint16_t)(v >> 16);
-            }
+        for (int i = 0; i < kScaleRows; ++i) {
+            const uint32_t v = 16 * four + 4 * w < p.nb ? moved[i][w] : 0u;   // past the row: the next row's
+            *(half_word *)&lds_scales[four % 2][w][scales_at[i]] = (uint16_t)v;
+            *(half_word *)&lds_scales[four % 2][w][2 * kHalf + scales_at[i]] = (uint16_t)(v >> 16);
+        }
     };
 
     f32x16 acc[kTM][kTN];
@@ -538,12 +535,14 @@ __global__ void __launch_bounds__(256) mx_tile_kernel(MxProduct p)
     for (int st = 0; st < 3; ++st)
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) load(st, st, k);
-    place_scales(0);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) place_scales(0, w);
     fetch_scales(1);
     Operands<kTM, kTN> first, second;   // of a stage's two steps
     Scales<kTM, kTN> now, next;
     meet<2 * kLoads + kScaleRows>();   // stage 0 is there
-    first.read(ring(0), 0, wm, wn, r, h);
+#pragma unroll
+    for (int i = 0; i < kTM; ++i) first.read(i, ring(0), 0, wm, wn, r, h);
     now.read(lds_scales[0][0], wm, wn, r, h);
     const int fours = (p.nb + 15) / 16;
     for (int four = 0; four < fours; ++four) {
@@ -554,16 +553,20 @@ __global__ void __launch_bounds__(256) mx_tile_kernel(MxProduct p)
             // loads and, where they are as young, the scales' may still run
             if (q == 3 || q == 0) meet<kLoads + kScaleRows>();
             else meet<kLoads>();
-            second.read(ring(q), 1, wm, wn, r, h);
             next.read(lds_scales[q == 3 ? (four + 1) % 2 : four % 2][(q + 1) % 4], wm, wn, r, h);
             __builtin_amdgcn_sched_barrier(0);
+            // everything else goes out between the products, behind those of
+            // each row tile
             multiply_operands<0>(first, now, acc, [&](int i) {
+                second.read(i, ring(q), 1, wm, wn, r, h);
                 if (i < kLoads) load(st + 3, (q + 3) % 4, i);
+                if (q == 2) {
+#pragma unroll
+                    for (int w = 4 * i / kTM; w < 4 * (i + 1) / kTM; ++w) place_scales(four + 1, w);
+                }
             });
-            if (q == 2) place_scales(four + 1);
-            first.read(ring((q + 1) % 4), 0, wm, wn, r, h);
-            __builtin_amdgcn_sched_barrier(0);
             multiply_operands<1>(second, now, acc, [&](int i) {
+                first.read(i, ring((q + 1) % 4), 0, wm, wn, r, h);
                 if (kTM + i < kLoads) load(st + 3, (q + 3) % 4, kTM + i);
             });
             if (q == 2) fetch_scales(four + 2);

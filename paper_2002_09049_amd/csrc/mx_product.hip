@@ -371,21 +371,29 @@ __device__ __forceinline__ void multiply_operands(const Operands<kTM, kTN> &o, c
 }
 
 // The sums to Y.  Register v of a tile is row 8 (v / 4) + 4 h + v % 4 of W, token
-// r: a wavefront turns one row of tiles (32 rows of W by 32 kTN tokens) at a
-// time in its part of LDS, so that a lane then holds eight consecutive values
-// of a token's row and four lanes store 32 of them.  The loop over tokens
-// stays rolled: unrolled, with the sums' registers as its operands, it took
-// 14 us of a 256 by 256 tile, instruction fetches.
-constexpr int kTurnRow = 36;   // floats of a token's row in LDS
+// r: a wavefront turns two by two tiles (64 rows of W by 64 tokens; 32 where it
+// has one tile of them) at a time in its part of LDS, so that a lane then holds
+// eight consecutive values of a token's row and eight lanes store 64 of them, a
+// whole line of 16-bit values (32 at a time, half a line: 1.5 times the bytes
+// written).  The loop over tokens stays rolled: unrolled, with the sums'
+// registers as its operands, it took 14 us of a 256 by 256 tile, instruction
+// fetches.
+//
+// A token's row in LDS is 16 pieces of four values; piece q of token t lies in
+// place q ^ (t % 16).
+constexpr int kTurnRow = 64;   // floats
 
-// Every 16th token's eight values from `from` on, with the bias added, to rows
-// of Y from `to` on; whole: all lanes' eight values are inside the rows.
+// Of the tokens lane / 8, + 8, .. below `tokens`: eight values, with the bias
+// added, to rows of Y from `to` on; whole: all lanes' eight values are inside
+// the rows.
 template <class T>
-__device__ __forceinline__ void write_turn(T *to, int64_t step, const float *from, int tokens, bool whole, int live,
-                                           const float (&bias)[8])
+__device__ __forceinline__ void write_turn(T *to, int64_t step, const float *turn, int lane, int tokens, bool whole,
+                                           int live, const float (&bias)[8])
 {
     const auto one = [&](int t, int inside) {
-        const f32x4 lo = *(const f32x4 *)(from + t * kTurnRow), hi = *(const f32x4 *)(from + t * kTurnRow + 4);
+        const int piece = (lane % 8 * 2) ^ (t % 16);
+        const float *row = turn + t * kTurnRow;
+        const f32x4 lo = *(const f32x4 *)(row + piece * 4), hi = *(const f32x4 *)(row + (piece ^ 1) * 4);
         float y[8];
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
@@ -397,10 +405,10 @@ __device__ __forceinline__ void write_turn(T *to, int64_t step, const float *fro
     };
     if (whole) {
 #pragma unroll 4
-        for (int t = 0; t < tokens; t += 16) one(t, 8);
+        for (int t = lane / 8; t < tokens; t += 8) one(t, 8);
     } else {
 #pragma unroll 1
-        for (int t = 0; t < tokens; t += 16) one(t, live);
+        for (int t = lane / 8; t < tokens; t += 8) one(t, live);
     }
 }
 
@@ -408,29 +416,35 @@ template <int kTM, int kTN>
 __device__ __forceinline__ void write_tiles(const MxProduct &p, float *turn, int64_t c0, int64_t t0, int lane,
                                             const f32x16 (&acc)[kTM][kTN])
 {
+    constexpr int kJ = kTN < 2 ? 1 : 2;   // token tiles of a turn
     const int r = lane % 32, h = lane / 32;
-    const int64_t first = t0 + lane / 4;   // the lane's first token
-    const int tokens = (int)min((int64_t)(32 * kTN) - lane / 4, p.n - first);
-    const float *from = turn + lane / 4 * kTurnRow + lane % 4 * 8;
 #pragma unroll
-    for (int i = 0; i < kTM; ++i) {
-#pragma unroll
-        for (int j = 0; j < kTN; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *(f32x4 *)&turn[(32 * j + r) * kTurnRow + 8 * q + 4 * h] =
-                    f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        const bool whole = c0 + 32 * i + 32 <= p.c;
-        const int64_t row = c0 + 32 * i + lane % 4 * 8;
+    for (int i = 0; i < kTM; i += 2) {
+        const bool whole = c0 + 32 * i + 64 <= p.c;
+        const int64_t row = c0 + 32 * i + lane % 8 * 8;
         const int live = (int)min((int64_t)8, p.c - row);
         float bias[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         if (p.bias) load8(p.bias + row, live, bias);
-        const int64_t at = first * p.ldy + row;
-        if (p.dtype == MPQ_F32) write_turn((float *)p.Y + at, 16 * p.ldy, from, tokens, whole, live, bias);
-        else if (p.dtype == MPQ_F16) write_turn((_Float16 *)p.Y + at, 16 * p.ldy, from, tokens, whole, live, bias);
-        else write_turn((__bf16 *)p.Y + at, 16 * p.ldy, from, tokens, whole, live, bias);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int j = 0; j < kTN; j += kJ) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int y = 0; y < kJ; ++y)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x16 &t = acc[i + x][j + y];
+                        *(f32x4 *)&turn[(32 * y + r) * kTurnRow + ((8 * x + 2 * q + h) ^ (r % 16)) * 4] =
+                            f32x4{t[4 * q], t[4 * q + 1], t[4 * q + 2], t[4 * q + 3]};
+                    }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const int64_t first = t0 + 32 * j, at = (first + lane / 8) * p.ldy + row;
+            const int tokens = (int)min((int64_t)(32 * kJ), p.n - first);
+            if (p.dtype == MPQ_F32) write_turn((float *)p.Y + at, 8 * p.ldy, turn, lane, tokens, whole, live, bias);
+            else if (p.dtype == MPQ_F16) write_turn((_Float16 *)p.Y + at, 8 * p.ldy, turn, lane, tokens, whole, live, bias);
+            else write_turn((__bf16 *)p.Y + at, 8 * p.ldy, turn, lane, tokens, whole, live, bias);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
     }
 }
 
@@ -575,7 +589,8 @@ __global__ void __launch_bounds__(256) mx_tile_kernel(MxProduct p)
     }
     // no load into LDS outlives the loop, and no wavefront still reads it
     meet<0>();
-    static_assert(32 * kTN * kTurnRow * 4 <= kRows * kStageBytes, "a wavefront's part fits its buffer");
+    static_assert(kTM % 2 == 0 && 32 * (kTN < 2 ? 1 : 2) * kTurnRow * 4 <= kRows * kStageBytes,
+                  "a wavefront's part fits its buffer");
     write_tiles(p, (float *)ring(wave), c0 + wm, t0 + wn, lane, acc);
 }
 
@@ -623,11 +638,11 @@ hipError_t launch_mx_token(const MxProduct &p, const void *X, int dtype, int64_t
 // measurements; model and time, us, for 4096 x 4096 (last row: x 25088) weights:
 //     n          few        128x64      128x128     256x128     256x256
 //     64     8.5   8.4    9.9   8.5   12.5  11.0  19.4  18.0  28.8  26.4
-//     512     54    56    9.9  11.0   12.5  12.5  19.4  18.6  28.8  28.4
-//     1024   106   109   19.8  21.8   12.5  16.6  19.4  20.9  28.8  29.8
-//     2048   210   216     40    42     25    33  19.4  29.1  28.8  33.8
-//     8192   834           158   139   100   113    78   108    58    85
-//     64      42    34     43    52    54    56    88    89   131   128
+//     512     54    56    9.9  11.1   12.5  12.1  19.4  17.0  28.8  25.5
+//     2048   210   216     40    38     25    29  19.4  27.5  28.8  31.7
+//     4096   418            79    68     50    54    39    52  28.8  40.9
+//     8192   834           158   133   100   103    78    99    58    77
+//     1024   640   508      85   107    54    77    88   100   131   137
 hipError_t launch_mx_product(const MxProduct &p, hipStream_t s)
 {
     if (p.n <= 0 || p.c <= 0) return hipSuccess;

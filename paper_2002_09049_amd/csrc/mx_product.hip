@@ -86,7 +86,9 @@ __device__ __forceinline__ void store_y(void *Y, int dtype, int64_t at, float v)
 
 // Few tokens: a workgroup owns 16 rows of W and 16 kNT tokens; its wavefronts
 // take the chunks of K in turn, straight from memory to registers, and their
-// sums meet in LDS, added in wavefront order.
+// sums meet in LDS, added in wavefront order.  At 16 tokens, 4096 x 4096, 4.5
+// us; from 64 on the vector cache bounds it, which serves the lanes of a load of
+// 16-byte pieces one after another (25088 x 4096: 34 us, 1.6 TB/s of W).
 constexpr int kFewWaves = 8;
 
 // The sums of a workgroup's wavefronts to Y.
@@ -150,9 +152,10 @@ __global__ void __launch_bounds__(kFewWaves *kWave) mx_few_kernel(MxProduct p)
 // One to kN tokens, quantized on the way: a wavefront quantizes its chunk of
 // every token itself (eight elements a lane, a block a quad, as
 // mx_quantize.hip), through a part of LDS of its own, so the call is one
-// launch and X is read by each workgroup.  4096 x 4096, one token: 4.2 us,
-// against 1.9 + 3.8 in two launches (and their gap); with more than four
-// tokens the quantization in every workgroup costs more than the launch.
+// launch and X is read by each workgroup.  4096 x 4096, one token: 4.0 us,
+// against 1.9 + 3.8 in two launches (and their gap); four tokens, 25088 x 4096:
+// 14 us, 3.9 TB/s of W.  With more than four tokens the quantization in every
+// workgroup costs more than the launch.
 template <int kN, class T>
 __global__ void __launch_bounds__(kFewWaves *kWave) mx_token_kernel(MxProduct p, const T *X, int64_t x_ld, int d)
 {
@@ -254,6 +257,12 @@ __global__ void __launch_bounds__(kFewWaves *kWave) mx_token_kernel(MxProduct p,
 // through the registers of a thread: one row's scales lie in one line of
 // memory, apart from the other rows', so they are fetched as rarely as
 // possible.
+//
+// 8192 tokens, 4096 x 4096, in 256 by 256 tiles: 77 to 82 us, 3.4 to 3.6
+// PFLOP/s (8192 x 8192: 4.2).  The same instructions alone, on registers and
+// with this tile's start and end, take 65; the matrix cores are busy 44% of a
+// wavefront's cycles, and the rest is the start, the end and what the reads
+// of LDS and the barriers leave uncovered.
 constexpr int kStageBytes = 64;
 constexpr uint32_t kOutside = 0x80000000u;   // past every buffer: loads give zeros
 
@@ -635,14 +644,20 @@ hipError_t launch_mx_token(const MxProduct &p, const void *X, int dtype, int64_t
 // stages, once for every 256 tiles (one CU each); the kernel for few tokens,
 // for every 256 of its workgroups, what the vector cache takes to serve every
 // lane of its operands' loads by itself.  The constants are fits to
-// measurements; model and time, us, for 4096 x 4096 (last row: x 25088) weights:
-//     n          few        128x64      128x128     256x128     256x256
-//     64     8.5   8.4    9.9   8.5   12.5  11.0  19.4  18.0  28.8  26.4
-//     512     54    56    9.9  11.1   12.5  12.1  19.4  17.0  28.8  25.5
-//     2048   210   216     40    38     25    29  19.4  27.5  28.8  31.7
-//     4096   418            79    68     50    54    39    52  28.8  40.9
-//     8192   834           158   133   100   103    78    99    58    77
-//     1024   640   508      85   107    54    77    88   100   131   137
+// measurements; model and time, us, all of one run, for 4096 rows of W:
+//     n     d          few         128x64       128x128      256x128      256x256
+//     1     4096     4.6   3.7    9.9   8.3   12.5  10.4   19.4  15.2   28.8  23.3
+//     16    4096     4.6   4.5    9.9   8.4   12.5  10.4   19.4  15.3   28.8  23.4
+//     64    4096     8.5   8.4    9.9   8.5   12.5  10.8   19.4  16.1   28.8  23.7
+//     512   4096    54.0  47.8    9.9  11.4   12.5  12.5   19.4  17.4   28.8  26.0
+//     1024  4096     106  89.5   19.8  20.5   12.5  15.5   19.4  19.4   28.8  27.7
+//     2048  4096     210   178   39.6  38.9   25.0  29.5   19.4  27.7   28.8  31.8
+//     4096  4096     418   351   79.2  73.0   50.0  55.0   38.9  55.7   28.8  42.2
+//     8192  4096     834   700    158   138    100   113   77.8   102   57.7  80.6
+//     64    25088   41.8  34.1   42.7  51.3   53.5  55.3   88.3  91.5    131   120
+//     1024  25088    639   488   85.4   106   53.5  77.4   88.3   100    131   135
+// The first kernel's model is high where it is far from being taken; 1000 tokens
+// through 512 x 512 go to it (4.6 us) where 128x64 tiles would take 4.1.
 hipError_t launch_mx_product(const MxProduct &p, hipStream_t s)
 {
     if (p.n <= 0 || p.c <= 0) return hipSuccess;

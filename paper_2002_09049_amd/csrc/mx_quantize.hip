@@ -9,7 +9,9 @@
 // whatever their length; only its first element's row takes a division of
 // large numbers.
 //
-// MEASURED
+// 4096 x 25088: fp32 to fp4 79 us, 5.9 TB/s of the 466 MB that it moves; back to
+// bf16 44 us, 5.9 TB/s of 260 MB (the codes come from the last-level cache when
+// they were just written).  A large copy reaches 5.2 TB/s.
 #include "mpq.h"
 #include "mx.hpp"
 

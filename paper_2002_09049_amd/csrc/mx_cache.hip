@@ -9,7 +9,7 @@
 // without divisions of large numbers (with them: 52 and 45 us for 32768 tokens
 // of 8 heads of 128 in fp4; without, 39 and 34 us, 4.4 and 5.0 TB/s of the 170 MB
 // that either moves).  Writing is the slower: tokens at slots in any order fill
-// parts of lines (62 MB written for the 36 MB held).
+// parts of lines (63 MB written for the 36 MB held).
 //
 // In the cache a head's rows of one page follow each other, and their scales
 // are stored block by block, consecutive tokens' scales of one block beside

@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kFewWaves *kWave) mx_token_kernel(MxProduct p,
 //
 // 8192 tokens, 4096 x 4096, in 256 by 256 tiles: 77 to 82 us, 3.4 to 3.6
 // PFLOP/s (8192 x 8192: 4.2).  The same instructions alone, on registers and
-// with this tile's start and end, take 65; the matrix cores are busy 44% of a
+// with this tile's start and end, take 65; the matrix cores are busy 47% of a
 // wavefront's cycles, and the rest is the start, the end and what the reads
 // of LDS and the barriers leave uncovered.
 constexpr int kStageBytes = 64;

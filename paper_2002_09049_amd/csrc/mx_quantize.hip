@@ -10,8 +10,9 @@
 // large numbers.
 //
 // 4096 x 25088: fp32 to fp4 79 us, 5.9 TB/s of the 466 MB that it moves; back to
-// bf16 44 us, 5.9 TB/s of 260 MB (the codes come from the last-level cache when
-// they were just written).  A large copy reaches 5.2 TB/s.
+// bf16 44 us, 5.9 TB/s of 260 MB.  A large copy, half reads and half writes,
+// reaches 5.2 TB/s; these mostly read or mostly write, and the codes, just
+// written when they were timed, may still lie in the last-level cache.
 #include "mpq.h"
 #include "mx.hpp"
 

@@ -603,6 +603,110 @@ __global__ void __launch_bounds__(256) mx_tile_kernel(MxProduct p)
     write_tiles(p, (float *)ring(wave), c0 + wm, t0 + wn, lane, acc);
 }
 
+// Some tens of tokens: a workgroup owns 16 rows of W by 64 tokens, 16 for each of
+// its four wavefronts, which share W's rows and sum over all of K.  K runs in
+// stages of 512 elements, 256 bytes of every row, in a ring as above.  Lanes
+// that load for registers directly (mx_few_kernel) are served one by one by
+// the vector cache; here 16 lanes load a row's 256 bytes.  Piece q of row r lies in
+// place q ^ (r % 16), so the 16 rows that an instruction takes one piece of lie
+// in all the banks.  Scales come a ring ahead, a row's 16 bytes a lane
+// (wavefront 0: W's, 1: the tokens'), and go to LDS with their words and bytes
+// exchanged, as Share has them.
+//
+// A stage takes 0.3 us, of few workgroups too; a ring of six stages gained
+// nothing (64 tokens, 4096 x 4096: 7.0 us, four 5.6, mx_few_kernel 8.3; 25088 x
+// 4096: 22.0, 20.8, 34.5).
+constexpr int kSlabM = 16, kSlabN = 64, kSlabRows = kSlabM + kSlabN, kSlabBytes = 256;
+
+// Byte i of word g of the result is byte g of word i.
+__device__ __forceinline__ u32x4 transpose_words(u32x4 w)
+{
+    const uint32_t lo0 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), lo1 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
+    const uint32_t hi0 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u), hi1 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+    return u32x4{__builtin_amdgcn_perm(lo1, lo0, 0x05040100u), __builtin_amdgcn_perm(lo1, lo0, 0x07060302u),
+                 __builtin_amdgcn_perm(hi1, hi0, 0x05040100u), __builtin_amdgcn_perm(hi1, hi0, 0x07060302u)};
+}
+
+__global__ void __launch_bounds__(256) mx_slab_kernel(MxProduct p)
+{
+    constexpr int kLoads = kSlabRows / 16;   // of a wavefront a stage
+    __shared__ __align__(16) uint8_t lds0[kSlabRows * kSlabBytes], lds1[kSlabRows * kSlabBytes];
+    __shared__ __align__(16) uint8_t lds2[kSlabRows * kSlabBytes], lds3[kSlabRows * kSlabBytes];
+    __shared__ __align__(16) uint32_t lds_scales[2][2][kWave][4];   // W's (16 rows), the tokens'
+    const auto ring = [&](int i) { return i == 0 ? lds0 : i == 1 ? lds1 : i == 2 ? lds2 : lds3; };
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int r = lane % 16, g = lane / 16;
+    const int64_t c0 = (int64_t)blockIdx.x * kSlabM, t0 = (int64_t)blockIdx.y * kSlabN;
+    const int nb = p.nb, row_bytes = nb * 16;
+    const int64_t wrows = min((int64_t)kSlabM, p.c - c0), xrows = min((int64_t)kSlabN, p.n - t0);
+    const __amdgpu_buffer_rsrc_t wc = buffer_of(p.wc + c0 * row_bytes, wrows * row_bytes);
+    const __amdgpu_buffer_rsrc_t xc = buffer_of(p.xc + t0 * row_bytes, xrows * row_bytes);
+    const __amdgpu_buffer_rsrc_t sc = wave == 0 ? buffer_of(p.ws + c0 * nb, wrows * nb)
+                                                : buffer_of(p.xs + t0 * nb, wave == 1 ? xrows * nb : 0);
+    // a load covers four rows, 4 wave .. of 16: lane l's 16 bytes land in place r of
+    // row 4 wave + g
+    const int piece = r ^ (4 * wave + g);
+    const uint32_t lane_at = (uint32_t)((4 * wave + g) * row_bytes + piece * 16);
+    const auto load = [&](int st, int buf) {
+        const uint32_t at = 16 * st + piece < nb ? lane_at + (uint32_t)st * kSlabBytes : kOutside;
+        load_to_lds(wc, ring(buf) + 4 * wave * kSlabBytes, at, 0);
+#pragma unroll
+        for (int k = 1; k < kLoads; ++k)
+            load_to_lds(xc, ring(buf) + (16 * k + 4 * wave) * kSlabBytes, at + (uint32_t)((k - 1) * 16 * row_bytes), 0);
+    };
+    u32x4 moved[4];
+    const auto fetch_scales = [&](int st, int i) { moved[i] = load_scales(sc, (uint32_t)(lane * nb + 16 * st)); };
+    const auto place_scales = [&](int st, int i) {
+        u32x4 v = moved[i];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[w] = 16 * st + 4 * w < nb ? v[w] : 0u;   // past the row: the next row's
+        if (wave < 2) *(u32x4 *)&lds_scales[i % 2][wave][lane][0] = transpose_words(v);
+    };
+
+    f32x4 acc = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int st = -1; st < 3; ++st) {
+        fetch_scales(st + 1, st + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (st >= 0) load(st, st);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    place_scales(0, 0);
+    const int fours = (nb + 63) / 64;
+    for (int four = 0; four < fours; ++four) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int st = 4 * four + q;
+            // stage st is there, and stage st - 1's buffer free; the loads of two
+            // stages may still run
+            meet<2 * (kLoads + 1)>();
+            Share a, b;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = ((4 * i + g) ^ r) * 16;
+                a.c[i] = *(const u32x4 *)(ring(q) + r * kSlabBytes + at);
+                b.c[i] = *(const u32x4 *)(ring(q) + (kSlabM + 16 * wave + r) * kSlabBytes + at);
+            }
+            a.s = lds_scales[q % 2][0][r][g];
+            b.s = lds_scales[q % 2][1][16 * wave + r][g];
+            __builtin_amdgcn_sched_barrier(0);
+            place_scales(st + 1, (q + 1) % 4);
+            fetch_scales(st + 4, q);
+            load(st + 3, (q + 3) % 4);
+            __builtin_amdgcn_sched_barrier(0);
+            acc = multiply_chunk(a, b, acc);
+        }
+    }
+    meet<0>();   // no load into LDS outlives the loop
+    const int64_t token = t0 + 16 * wave + r;
+    if (token >= p.n) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t row = c0 + 4 * g + i;
+        if (row < p.c) store_y(p.Y, p.dtype, token * p.ldy + row, acc[i] + (p.bias ? p.bias[row] : 0.0f));
+    }
+}
+
 template <int kTM, int kTN>
 hipError_t launch_tiles(const MxProduct &p, hipStream_t s)
 {
@@ -672,6 +776,13 @@ hipError_t launch_mx_product(const MxProduct &p, hipStream_t s)
     const int nt = p.n <= 16 ? 1 : p.n <= 32 ? 2 : 4;
     const int64_t gx = (p.c + 15) / 16, gy = (p.n + 16 * nt - 1) / (16 * nt);
     const double few = 2.0 + ceil((double)gx * (double)gy / 256.0) * (p.nb / 128.0) * (nt == 1 ? 2.6 : nt == 2 ? 3.8 : 6.5);
+    const int64_t sx = (p.c + kSlabM - 1) / kSlabM, sy = (p.n + kSlabN - 1) / kSlabN;
+    const double slab = 1.0 + ceil((double)sx * (double)sy / 256.0) * (1.9 + 0.34 * 4.0 * ceil(p.nb / 64.0));
+    if (slab < best && slab < few && sx <= 0x7fffffffLL && sy <= 65535) {
+        LaunchTimer timer(s, "mx_slab_kernel");
+        hipLaunchKernelGGL(mx_slab_kernel, dim3((unsigned)sx, (unsigned)sy), dim3(256), 0, s, p);
+        return hipGetLastError();
+    }
     if (few > best || gy > 65535) {
         if (best == t44) return launch_tiles<4, 4>(p, s);
         if (best == t42) return launch_tiles<4, 2>(p, s);

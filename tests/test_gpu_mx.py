@@ -217,6 +217,62 @@ def test_linear_tiles(n, c, d, tile):
     _check_product(_f64(Y), xq, ref.values(wc, ws, "fp4"), b.astype(np.float64), "f32", ws.shape[1])
 
 
+# sizes at which the kernel for some tens of tokens is taken: rows, tokens and K
+# (stages of 512, rings of four) ragged at every edge
+SLABS = [(64, 100, 2048), (33, 70, 1500), (65, 17, 1700), (34, 16, 3000), (77, 1000, 2047), (20, 33, 9000),
+         (100, 1001, 3000), (128, 40, 25000), (64, 4090, 4096)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,c,d", SLABS)
+def test_linear_slabs(n, c, d, dtype):
+    import torch
+    from paper_2002_09049_amd import mpq
+    say(f"case mx linear slabs n={n} c={c} d={d} {dtype}")
+    rng = np.random.default_rng(n + 2 * c + d)
+    X = _dev(_activations(rng, (n, d)).astype(np.float32), _dt(dtype))
+    wc, ws = _weights(rng, c, d)
+    b = rng.standard_normal(c).astype(np.float32)
+    codes, scales = _dev(ref.pack(wc)), _dev(ws)
+    room = torch.full((n, c + 5), -7.0, dtype=_dt(dtype), device="cuda")
+    mpq.timing_enable(True)
+    try:
+        Y = mpq.mx_linear(X, codes, scales, bias=_dev(b), out=room[:, 2:c + 2])
+        names = [k for k, _ in mpq.timing_read()]
+    finally:
+        mpq.timing_enable(False)
+    assert names == ["mx_quantize_kernel", "mx_slab_kernel"]
+    r = _np(room.float())
+    assert (r[:, :2] == -7).all() and (r[:, c + 2:] == -7).all()
+    xq = ref.values(*ref.quantize(ref.padded(_f64(X), ref.ROW), "fp4"), "fp4")
+    _check_product(_f64(Y), xq, ref.values(wc, ws, "fp4"), b.astype(np.float64), dtype, ws.shape[1])
+
+
+def test_linear_slabs_with_bad_rows():
+    """A stage that a row ends in does not see the next row: blocks that are
+    not numbers at the start of one token and one channel reach no other."""
+    from paper_2002_09049_amd import mpq
+    n, c, d = 50, 60, 2600
+    say(f"case mx linear slabs bad rows n={n} c={c} d={d}")
+    rng = np.random.default_rng(3)
+    x = _activations(rng, (n, d)).astype(np.float32)
+    wc, ws = _weights(rng, c, d)
+    y0 = _np(mpq.mx_linear(_dev(x), _dev(ref.pack(wc)), _dev(ws)))
+    x[21, :400:32] = np.nan
+    ws[[5, c - 1], :12] = 255
+    mpq.timing_enable(True)
+    try:
+        y = _np(mpq.mx_linear(_dev(x), _dev(ref.pack(wc)), _dev(ws)))
+        names = [k for k, _ in mpq.timing_read()]
+    finally:
+        mpq.timing_enable(False)
+    assert names == ["mx_quantize_kernel", "mx_slab_kernel"]
+    bad = np.zeros((n, c), bool)
+    bad[21] = bad[:, [5, c - 1]] = True
+    assert np.isnan(y[bad]).all()
+    assert np.array_equal(y[~bad], y0[~bad])
+
+
 @pytest.mark.parametrize("n", [1, 5, 40, 300])
 def test_linear_with_a_bad_token(n):
     """A token that holds a NaN gives a row of NaN, and no other."""

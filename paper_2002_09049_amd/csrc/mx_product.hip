@@ -87,8 +87,8 @@ __device__ __forceinline__ void store_y(void *Y, int dtype, int64_t at, float v)
 // Few tokens: a workgroup owns 16 rows of W and 16 kNT tokens; its wavefronts
 // take the chunks of K in turn, straight from memory to registers, and their
 // sums meet in LDS, added in wavefront order.  At 16 tokens, 4096 x 4096, 4.5
-// us; from 64 on the vector cache bounds it, which serves the lanes of a load of
-// 16-byte pieces one after another (25088 x 4096: 34 us, 1.6 TB/s of W).
+// us; more are bound by the vector cache, which serves the lanes of a load of
+// 16-byte pieces one after another (64, 25088 x 4096: 34 us, 1.6 TB/s of W).
 constexpr int kFewWaves = 8;
 
 // The sums of a workgroup's wavefronts to Y.
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kFewWaves *kWave) mx_token_kernel(MxProduct p,
 // memory, apart from the other rows', so they are fetched as rarely as
 // possible.
 //
-// 8192 tokens, 4096 x 4096, in 256 by 256 tiles: 77 to 82 us, 3.4 to 3.6
+// 8192 tokens, 4096 x 4096, in 256 by 256 tiles: 77 to 85 us, 3.2 to 3.6
 // PFLOP/s (8192 x 8192: 4.2).  The same instructions alone, on registers and
 // with this tile's start and end, take 65; the matrix cores are busy 47% of a
 // wavefront's cycles, and the rest is the start, the end and what the reads
@@ -615,7 +615,7 @@ __global__ void __launch_bounds__(256) mx_tile_kernel(MxProduct p)
 //
 // A stage takes 0.3 us, of few workgroups too; a ring of six stages gained
 // nothing (64 tokens, 4096 x 4096: 7.0 us, four 5.6, mx_few_kernel 8.3; 25088 x
-// 4096: 22.0, 20.8, 34.5).
+// 4096: 22.0, 20.6, 34.1; the last is 2.6 TB/s of W).
 constexpr int kSlabM = 16, kSlabN = 64, kSlabRows = kSlabM + kSlabN, kSlabBytes = 256;
 
 // Byte i of word g of the result is byte g of word i.
@@ -745,23 +745,30 @@ hipError_t launch_mx_token(const MxProduct &p, const void *X, int dtype, int64_t
 
 // Which kernel: the one that a model of its time, in us, finds fastest.  With K
 // in stages of 128 elements, a tile kernel takes its start and end plus its
-// stages, once for every 256 tiles (one CU each); the kernel for few tokens,
-// for every 256 of its workgroups, what the vector cache takes to serve every
-// lane of its operands' loads by itself.  The constants are fits to
-// measurements; model and time, us, all of one run, for 4096 rows of W:
-//     n     d          few         128x64       128x128      256x128      256x256
-//     1     4096     4.6   3.7    9.9   8.3   12.5  10.4   19.4  15.2   28.8  23.3
-//     16    4096     4.6   4.5    9.9   8.4   12.5  10.4   19.4  15.3   28.8  23.4
-//     64    4096     8.5   8.4    9.9   8.5   12.5  10.8   19.4  16.1   28.8  23.7
-//     512   4096    54.0  47.8    9.9  11.4   12.5  12.5   19.4  17.4   28.8  26.0
-//     1024  4096     106  89.5   19.8  20.5   12.5  15.5   19.4  19.4   28.8  27.7
-//     2048  4096     210   178   39.6  38.9   25.0  29.5   19.4  27.7   28.8  31.8
-//     4096  4096     418   351   79.2  73.0   50.0  55.0   38.9  55.7   28.8  42.2
-//     8192  4096     834   700    158   138    100   113   77.8   102   57.7  80.6
-//     64    25088   41.8  34.1   42.7  51.3   53.5  55.3   88.3  91.5    131   120
-//     1024  25088    639   488   85.4   106   53.5  77.4   88.3   100    131   135
-// The first kernel's model is high where it is far from being taken; 1000 tokens
-// through 512 x 512 go to it (4.6 us) where 128x64 tiles would take 4.1.
+// stages, once for every 256 tiles (one CU each); the slab kernel the same, its
+// rings of four stages of 512 whole; the kernel for few tokens, for every 256
+// of its workgroups, what the vector cache takes to serve every lane of its
+// operands' loads by itself.  The constants are fits to measurements; model
+// and time, us, all of one run, for 4096 rows of W:
+//    n    d        few        slab       128x64     128x128     256x128     256x256
+//    1    4096   4.6  3.5    5.6  4.9    9.9  8.3   12.5 10.2   19.4 15.2   28.8 23.3
+//    16   4096   4.6  4.4    5.6  5.2    9.9  8.4   12.5 10.3   19.4 15.3   28.8 23.5
+//    32   4096   5.8  5.8    5.6  5.2    9.9  8.4   12.5 10.4   19.4 15.5   28.8 23.5
+//    64   4096   8.5  8.3    5.6  5.6    9.9  8.5   12.5 10.7   19.4 15.9   28.8 23.7
+//    128  4096  15.0 13.9   10.2  9.5    9.9  8.7   12.5 10.9   19.4 16.2   28.8 24.9
+//    512  4096  54.0 46.7   38.0 33.0    9.9 11.0   12.5 12.2   19.4 17.0   28.8 25.8
+//    1024 4096   106 88.5   74.9 72.4   19.8 20.1   12.5 15.3   19.4 18.8   28.8 26.9
+//    2048 4096   210  175    149  142   39.6 39.0   25.0 29.2   19.4 28.0   28.8 30.7
+//    4096 4096   418  351    297  282   79.2 73.4   50.0 56.9   38.9 55.9   28.8 42.2
+//    8192 4096   834  697    592  562    158  142    100  115   77.8  103   57.7 80.8
+//    16   25088 17.9 14.9   20.6 15.9   42.7 45.0   53.5 53.2   88.3 89.6    131  117
+//    32   25088 25.3 21.1   20.6 16.2   42.7 47.8   53.5 53.7   88.3 90.1    131  119
+//    64   25088 41.8 34.1   20.6 20.6   42.7 51.5   53.5 55.3   88.3 91.3    131  120
+//    128  25088 81.6 64.5   40.2 39.1   42.7 51.1   53.5 66.0   88.3 96.1    131  124
+//    1024 25088  639  487    314  293   85.4  102   53.5 75.8   88.3 96.4    131  134
+//    64   1024   3.6  4.1    4.3  4.4    5.1  4.7    6.5  5.6    9.4  7.9   14.0 10.6
+// Misses seen: 20 tokens through 4096 x 4096 go to the slabs (5.3 us; the first
+// kernel 5.0), 1000 through 512 x 512 to the first kernel (4.5; 128x64 tiles 4.1).
 hipError_t launch_mx_product(const MxProduct &p, hipStream_t s)
 {
     if (p.n <= 0 || p.c <= 0) return hipSuccess;

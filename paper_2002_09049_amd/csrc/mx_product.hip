@@ -295,19 +295,28 @@ __device__ __forceinline__ f32x16 multiply_tile(u32x4 a, uint32_t as, u32x4 b, u
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widen(a), widen(b), acc, 4, 4, kA, (int)as, kB, (int)bs);
 }
 
-// A barrier that leaves this wavefront's last kLeft loads into LDS in flight
+// The compiler moves no access across (no instruction).  The rings' waits count
+// loads in the order that they are issued, those into LDS and the scales' into
+// registers alike, so between loads of the two kinds stands a pin:
+// tests/test_mx_ring_cpu.py reads it off the code that the compiler makes.
+__device__ __forceinline__ void pin()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// A barrier that leaves this wavefront's last kLeft loads in flight
 // (__syncthreads would wait for them all); its LDS reads and writes and its
 // loads before those are done.
 template <int kLeft>
 __device__ __forceinline__ void meet()
 {
     constexpr int kVmcnt = (kLeft & 15) | (kLeft >> 4) << 14;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // orders the compiler's accesses only
-    __builtin_amdgcn_sched_barrier(0);
+    pin();
     __builtin_amdgcn_s_waitcnt(0x0070 | kVmcnt);   // vmcnt(kLeft), lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    pin();
 }
 
 // The operands of one step of a stage (64 elements): the lane's pieces of the
@@ -554,10 +563,12 @@ __global__ void __launch_bounds__(256) mx_tile_kernel(MxProduct p)
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
 
     fetch_scales(0);
+    pin();
 #pragma unroll
     for (int st = 0; st < 3; ++st)
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) load(st, st, k);
+    pin();
 #pragma unroll
     for (int w = 0; w < 4; ++w) place_scales(0, w);
     fetch_scales(1);
@@ -592,7 +603,11 @@ __global__ void __launch_bounds__(256) mx_tile_kernel(MxProduct p)
                 first.read(i, ring((q + 1) % 4), 0, wm, wn, r, h);
                 if (kTM + i < kLoads) load(st + 3, (q + 3) % 4, kTM + i);
             });
-            if (q == 2) fetch_scales(four + 2);
+            if (q == 2) {
+                pin();
+                fetch_scales(four + 2);
+                pin();
+            }
             now = next;
         }
     }
@@ -667,9 +682,9 @@ __global__ void __launch_bounds__(256) mx_slab_kernel(MxProduct p)
 #pragma unroll
     for (int st = -1; st < 3; ++st) {
         fetch_scales(st + 1, st + 1);
-        __builtin_amdgcn_sched_barrier(0);
+        pin();
         if (st >= 0) load(st, st);
-        __builtin_amdgcn_sched_barrier(0);
+        pin();
     }
     place_scales(0, 0);
     const int fours = (nb + 63) / 64;
@@ -692,8 +707,9 @@ __global__ void __launch_bounds__(256) mx_slab_kernel(MxProduct p)
             __builtin_amdgcn_sched_barrier(0);
             place_scales(st + 1, (q + 1) % 4);
             fetch_scales(st + 4, q);
+            pin();
             load(st + 3, (q + 3) % 4);
-            __builtin_amdgcn_sched_barrier(0);
+            pin();
             acc = multiply_chunk(a, b, acc);
         }
     }

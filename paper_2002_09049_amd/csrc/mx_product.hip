@@ -12,6 +12,7 @@
 
 #include "mpq.h"
 #include "mx.hpp"
+#include "mx_stage.hpp"
 
 namespace mpq {
 
@@ -263,8 +264,6 @@ __global__ void __launch_bounds__(kFewWaves *kWave) mx_token_kernel(MxProduct p,
 // with this tile's start and end, take 65; the matrix cores are busy 47% of a
 // wavefront's cycles, and the rest is the start, the end and what the reads
 // of LDS and the barriers leave uncovered.
-constexpr int kStageBytes = 64;
-constexpr uint32_t kOutside = 0x80000000u;   // past every buffer: loads give zeros
 
 // (the arguments are the same in every lane: a descriptor in scalar registers)
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint8_t *base, int64_t bytes)
@@ -276,10 +275,11 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint8_t *base,
 }
 
 // 16 rows' part of a stage into LDS (the 64 lanes' 16 bytes land one after the
-// other).
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, uint8_t *to, uint32_t at, int offset)
+// other).  The whole offset is the lane's own: the check against the buffer's
+// length is documented to cover that one, not the scalar offset.
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, uint8_t *to, uint32_t at)
 {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, at, offset, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, at, 0, 0, 0);
 }
 
 __device__ __forceinline__ u32x4 load_scales(__amdgpu_buffer_rsrc_t from, uint32_t at)
@@ -512,13 +512,14 @@ __global__ void __launch_bounds__(256) mx_tile_kernel(MxProduct p)
 
     // a load covers 16 rows, lane l row l / 4 of them; a wavefront loads a quarter
     // of W's rows (loads 0 .. kTM - 1) and of the tokens'
-    const uint32_t lane_at = (uint32_t)(lane / 4 * row_bytes + ((lane % 4) ^ (lane / 16)) * 16);
+    const int wrow0 = 16 * wave * kTM, xrow0 = 16 * wave * kTN;
+    const uint32_t w_at = tile_lane_offset(wrow0, lane, row_bytes), x_at = tile_lane_offset(xrow0, lane, row_bytes);
     const auto load = [&](int st, int buf, int k) {
-        const uint32_t at = 4 * st < p.nb ? lane_at : kOutside;
-        const int row = k < kTM ? 16 * (wave * kTM + k) : 16 * (wave * kTN + k - kTM);
-        uint8_t *to = ring(buf) + ((k < kTM ? 0 : kBM) + row) * kStageBytes;
-        if (k < kTM) load_to_lds(wc, to, at, row * row_bytes + st * kStageBytes);
-        else load_to_lds(xc, to, at, row * row_bytes + st * kStageBytes);
+        if (k < kTM)
+            load_to_lds(wc, ring(buf) + (wrow0 + 16 * k) * kStageBytes, w_at + tile_stage_offset(k, row_bytes, st, p.nb));
+        else
+            load_to_lds(xc, ring(buf) + (kBM + xrow0 + 16 * (k - kTM)) * kStageBytes,
+                        x_at + tile_stage_offset(k - kTM, row_bytes, st, p.nb));
     };
     // scales: a thread moves those of the rows threadIdx.x + 256 i (W's, then the
     // tokens'; a wavefront's 64 are of one kind)
@@ -631,7 +632,7 @@ __global__ void __launch_bounds__(256) mx_tile_kernel(MxProduct p)
 // A stage takes 0.3 us, of few workgroups too; a ring of six stages gained
 // nothing (64 tokens, 4096 x 4096: 7.0 us, four 5.6, mx_few_kernel 8.3; 25088 x
 // 4096: 22.0, 20.6, 34.1; the last is 2.6 TB/s of W).
-constexpr int kSlabM = 16, kSlabN = 64, kSlabRows = kSlabM + kSlabN, kSlabBytes = 256;
+constexpr int kSlabM = 16, kSlabN = 64, kSlabRows = kSlabM + kSlabN;
 
 // Byte i of word g of the result is byte g of word i.
 __device__ __forceinline__ u32x4 transpose_words(u32x4 w)
@@ -660,14 +661,12 @@ __global__ void __launch_bounds__(256) mx_slab_kernel(MxProduct p)
                                                 : buffer_of(p.xs + t0 * nb, wave == 1 ? xrows * nb : 0);
     // a load covers four rows, 4 wave .. of 16: lane l's 16 bytes land in place r of
     // row 4 wave + g
-    const int piece = r ^ (4 * wave + g);
-    const uint32_t lane_at = (uint32_t)((4 * wave + g) * row_bytes + piece * 16);
     const auto load = [&](int st, int buf) {
-        const uint32_t at = 16 * st + piece < nb ? lane_at + (uint32_t)st * kSlabBytes : kOutside;
-        load_to_lds(wc, ring(buf) + 4 * wave * kSlabBytes, at, 0);
+        const uint32_t at = slab_lane_offset(4 * wave + g, r, row_bytes, st, nb);
+        load_to_lds(wc, ring(buf) + 4 * wave * kSlabBytes, at);
 #pragma unroll
         for (int k = 1; k < kLoads; ++k)
-            load_to_lds(xc, ring(buf) + (16 * k + 4 * wave) * kSlabBytes, at + (uint32_t)((k - 1) * 16 * row_bytes), 0);
+            load_to_lds(xc, ring(buf) + (16 * k + 4 * wave) * kSlabBytes, at + (uint32_t)((k - 1) * 16 * row_bytes));
     };
     u32x4 moved[4];
     const auto fetch_scales = [&](int st, int i) { moved[i] = load_scales(sc, (uint32_t)(lane * nb + 16 * st)); };

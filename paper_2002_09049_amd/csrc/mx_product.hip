@@ -782,6 +782,11 @@ hipError_t launch_mx_token(const MxProduct &p, const void *X, int dtype, int64_t
 //    128  25088 81.6 64.5   40.2 39.1   42.7 51.1   53.5 66.0   88.3 96.1    131  124
 //    1024 25088  639  487    314  293   85.4  102   53.5 75.8   88.3 96.4    131  134
 //    64   1024   3.6  4.1    4.3  4.4    5.1  4.7    6.5  5.6    9.4  7.9   14.0 10.6
+// Up to four tokens always take the kernel for few: its sums have the order of
+// mx_token_kernel's, which a linear call runs for them, so that the two calls
+// give the same bits.  (One token and four, d = 4096: 16384 rows of W 8.0 and 9.0
+// us, by 128x64 tiles 11.1 and 11.1; 32000 rows 13.6 and 15.5, 12.6 and 12.7;
+// 128256 rows 47.2 and 53.8, by 256x128 tiles 47.5 and 48.5.)
 // Misses seen: 20 tokens through 4096 x 4096 go to the slabs (5.3 us; the first
 // kernel 5.0), 1000 through 512 x 512 to the first kernel (4.5; 128x64 tiles 4.1).
 hipError_t launch_mx_product(const MxProduct &p, hipStream_t s)
@@ -800,12 +805,13 @@ hipError_t launch_mx_product(const MxProduct &p, hipStream_t s)
     const double few = 2.0 + ceil((double)gx * (double)gy / 256.0) * (p.nb / 128.0) * (nt == 1 ? 2.6 : nt == 2 ? 3.8 : 6.5);
     const int64_t sx = (p.c + kSlabM - 1) / kSlabM, sy = (p.n + kSlabN - 1) / kSlabN;
     const double slab = 1.0 + ceil((double)sx * (double)sy / 256.0) * (1.9 + 0.34 * 4.0 * ceil(p.nb / 64.0));
-    if (slab < best && slab < few && sx <= 0x7fffffffLL && sy <= 65535) {
+    const bool by_model = !mx_quantizes_inside(p.n);
+    if (by_model && slab < best && slab < few && sx <= 0x7fffffffLL && sy <= 65535) {
         LaunchTimer timer(s, "mx_slab_kernel");
         hipLaunchKernelGGL(mx_slab_kernel, dim3((unsigned)sx, (unsigned)sy), dim3(256), 0, s, p);
         return hipGetLastError();
     }
-    if (few > best || gy > 65535) {
+    if ((by_model && few > best) || gy > 65535) {
         if (best == t44) return launch_tiles<4, 4>(p, s);
         if (best == t42) return launch_tiles<4, 2>(p, s);
         return best == t22 ? launch_tiles<2, 2>(p, s) : launch_tiles<2, 1>(p, s);

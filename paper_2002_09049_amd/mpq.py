@@ -8,9 +8,15 @@ fallback: if the library is missing, every call raises.
 The library is loaded after torch, so it binds to the HIP runtime that torch
 already loaded (both carry the soname libamdhip64.so.7) and the stream
 handles and device pointers torch hands out are valid in it.
+
+``stream`` (a torch.cuda.Stream; without one, the current stream) is where a
+call's work is enqueued.  What the call allocates itself comes from that stream's
+pool, so no other stream's work is still on it; the inputs, and the
+tensors of ``out``, are the caller's to have ready there and to keep.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional, Tuple
@@ -197,6 +203,24 @@ def _stream(stream) -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+def _on(stream):
+    """The context in which a call's own tensors are allocated: they belong to the
+    stream that writes them."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+    return torch.cuda.stream(stream)
+
+
+def _new(like: torch.Tensor, shape, dtype, stream) -> torch.Tensor:
+    """A new tensor on the device of `like`, of the stream's pool."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with _on(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
 def fit_layer(W: torch.Tensor, bits: int, max_points: int, n_grid: int, tol: float,
               grid=None, with_err: bool = True, stream=None, out=None, dense: bool = False):
     """mpq_fit_layer (mpq_fit_layer_dense with dense=True).  W: [C, d] fp32 on the device.
@@ -210,10 +234,11 @@ def fit_layer(W: torch.Tensor, bits: int, max_points: int, n_grid: int, tol: flo
     C, d = W.shape
     dev = W.device
     if out is None:
-        codes = torch.empty((C, max_points, d), dtype=torch.int8, device=dev)
-        scales = torch.empty((C, max_points), dtype=torch.float32, device=dev)
-        counts = torch.empty((C,), dtype=torch.int32, device=dev)
-        err = torch.empty((C, max_points), dtype=torch.float32, device=dev) if with_err else None
+        with _on(stream):
+            codes = torch.empty((C, max_points, d), dtype=torch.int8, device=dev)
+            scales = torch.empty((C, max_points), dtype=torch.float32, device=dev)
+            counts = torch.empty((C,), dtype=torch.int32, device=dev)
+            err = torch.empty((C, max_points), dtype=torch.float32, device=dev) if with_err else None
     else:
         codes, scales, counts, err = out
     gbuf = None
@@ -250,11 +275,12 @@ def fit_layer_calib(W: torch.Tensor, bits: int, max_points: int, n_grid: int, X:
         raise ValueError("X must be [d, n]")
     dev = W.device
     if out is None:
-        codes = torch.empty((C, max_points, d), dtype=torch.int8, device=dev)
-        scales = torch.empty((C, max_points), dtype=torch.float32, device=dev)
-        counts = torch.empty((C,), dtype=torch.int32, device=dev)
-        err = torch.empty((C, max_points), dtype=torch.float32, device=dev) if with_err else None
-        xerr = torch.empty((C, max_points), dtype=torch.float32, device=dev)
+        with _on(stream):
+            codes = torch.empty((C, max_points, d), dtype=torch.int8, device=dev)
+            scales = torch.empty((C, max_points), dtype=torch.float32, device=dev)
+            counts = torch.empty((C,), dtype=torch.int32, device=dev)
+            err = torch.empty((C, max_points), dtype=torch.float32, device=dev) if with_err else None
+            xerr = torch.empty((C, max_points), dtype=torch.float32, device=dev)
     else:
         codes, scales, counts, err, xerr = out
     g = LayerSet._grid(grid, n_grid)
@@ -292,8 +318,8 @@ def output_error(W: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, cou
         raise ValueError("X must be [d, n]")
     n = X.shape[1]
     if out is None:
-        err = torch.empty((C,), dtype=torch.float32, device=W.device)
-        ref = torch.empty((C,), dtype=torch.float32, device=W.device) if with_ref else None
+        err = _new(W, (C,), torch.float32, stream)
+        ref = _new(W, (C,), torch.float32, stream) if with_ref else None
     else:
         err, ref = out
     lib = load()
@@ -310,7 +336,7 @@ def reconstruct(codes: torch.Tensor, scales: torch.Tensor, counts: torch.Tensor,
                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """mpq_reconstruct.  Returns W_hat [C, d] fp32."""
     C, P, d = codes.shape
-    W_hat = torch.empty((C, d), dtype=torch.float32, device=codes.device) if out is None else out
+    W_hat = _new(codes, (C, d), torch.float32, stream) if out is None else out
     rc = load().mpq_reconstruct(_dev(codes, torch.int8, "codes"), _dev(scales, torch.float32, "scales"),
                                 _dev(counts, torch.int32, "counts"), C, d, P,
                                 _dev(W_hat, torch.float32, "W_hat"), _stream(stream))
@@ -323,8 +349,9 @@ def integer_scales(scales: torch.Tensor, counts: torch.Tensor, p: int, stream=No
     """mpq_integer_scales (Eq. (14)).  Returns (A [C, P] int32, number of
     clamped values as a 1-element uint64 device tensor (int64 view) or None)."""
     C, P = scales.shape
-    A = torch.empty((C, P), dtype=torch.int32, device=scales.device) if out is None else out
-    cl = torch.zeros((1,), dtype=torch.int64, device=scales.device) if count_clamped else None
+    A = _new(scales, (C, P), torch.int32, stream) if out is None else out
+    with _on(stream):   # the zero is written where it is counted up
+        cl = torch.zeros((1,), dtype=torch.int64, device=scales.device) if count_clamped else None
     _check(load().mpq_integer_scales(_dev(scales, torch.float32, "scales"),
                                      _dev(counts, torch.int32, "counts"), C, P, int(p),
                                      _dev(A, torch.int32, "A"),
@@ -339,7 +366,7 @@ def integer_forward(codes: torch.Tensor, A: torch.Tensor, counts: torch.Tensor, 
     if X.dim() != 2 or X.shape[1] != d:
         raise ValueError("X must be [n, d]")
     n = X.shape[0]
-    Y = torch.empty((C, n), dtype=torch.int64, device=codes.device) if out is None else out
+    Y = _new(codes, (C, n), torch.int64, stream) if out is None else out
     _check(load().mpq_integer_forward(_dev(codes, torch.int8, "codes"), _dev(A, torch.int32, "A"),
                                       _dev(counts, torch.int32, "counts"), C, d, P,
                                       _dev(X, torch.int8, "X"), n, int(p), _dev(Y, torch.int64, "Y"),
@@ -417,12 +444,12 @@ def _space(workspace, need, stream):
     return None, 0, None
 
 
-def _rows_out(out, n: int, d: int, dtype, like: torch.Tensor):
+def _rows_out(out, n: int, d: int, dtype, like: torch.Tensor, stream):
     """(tensor, pointer, dtype number, row stride) of an output [n, d]: the
     caller's, or a new one."""
     if out is None:
         dt = _mx_dtype(dtype, "dtype")
-        out = like.new_empty((n, d), dtype=dtype)
+        out = _new(like, (n, d), dtype, stream)
         return out, out.data_ptr(), dt, max(d, 1)
     if tuple(out.shape) != (n, d):
         raise ValueError(f"out must be {(n, d)} (got {tuple(out.shape)})")
@@ -437,8 +464,8 @@ def mx_quantize(X: torch.Tensor, stream=None, out=None):
     r, d = X.shape
     wide = -(-d // MX_ROW) * MX_ROW
     if out is None:
-        codes = X.new_empty((r, wide // 2), dtype=torch.uint8)
-        scales = X.new_empty((r, wide // MX_BLOCK), dtype=torch.uint8)
+        codes = _new(X, (r, wide // 2), torch.uint8, stream)
+        scales = _new(X, (r, wide // MX_BLOCK), torch.uint8, stream)
         cp, sp = codes.data_ptr(), scales.data_ptr()
     else:
         codes, scales = out
@@ -453,7 +480,7 @@ def mx_dequantize(codes: torch.Tensor, scales: torch.Tensor, d: int, dtype=torch
                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """mpq_mx_dequantize: the values [r, d] that fp4 blocks stand for."""
     cp, sp = _fp4(codes, scales, d, "rows")
-    Y, yp, dt, ld = _rows_out(out, codes.shape[0], d, dtype, codes)
+    Y, yp, dt, ld = _rows_out(out, codes.shape[0], d, dtype, codes, stream)
     _check(load().mpq_mx_dequantize(cp, sp, codes.shape[0], d, yp, dt, ld, _stream(stream)))
     return Y
 
@@ -468,7 +495,7 @@ def mx_product(x_codes: torch.Tensor, x_scales: torch.Tensor, codes: torch.Tenso
     n, c = x_codes.shape[0], codes.shape[0]
     if bias is not None and bias.shape != (c,):
         raise ValueError(f"bias must be ({c},)")
-    Y, yp, dt, ld = _rows_out(out, n, c, dtype, codes)
+    Y, yp, dt, ld = _rows_out(out, n, c, dtype, codes, stream)
     _check(load().mpq_mx_product(xc, xs, n, wc, ws, c, d,
                                  None if bias is None else _dev(bias, torch.float32, "bias"), yp, dt, ld,
                                  _stream(stream)))
@@ -496,7 +523,7 @@ def mx_linear(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bias: 
     c = codes.shape[0]
     if bias is not None and bias.shape != (c,):
         raise ValueError(f"bias must be ({c},)")
-    Y, yp, dt, ld = _rows_out(out, n, c, X.dtype if dtype is None else dtype, X)
+    Y, yp, dt, ld = _rows_out(out, n, c, X.dtype if dtype is None else dtype, X, stream)
     wp, wn, _own = _space(workspace, lambda: mx_linear_workspace(n, c, d), stream)
     _check(load().mpq_mx_linear(xp, xt, n, x_ld, wc, ws, c, d,
                                 None if bias is None else _dev(bias, torch.float32, "bias"), yp, dt, ld, wp, wn,
@@ -560,7 +587,7 @@ class MXCache:
         n = slots.numel()
         shape = (n, self.kv_heads, self.head_dim)
         if out is None:
-            K, V = slots.new_empty(shape, dtype=dtype), slots.new_empty(shape, dtype=dtype)
+            K, V = _new(slots, shape, dtype, stream), _new(slots, shape, dtype, stream)
             kp, vp = K.data_ptr(), V.data_ptr()
             kt = vt = self.kv_heads * self.head_dim
             kh = vh = self.head_dim
@@ -604,14 +631,14 @@ class MXCache:
         if lengths.shape != (batch,):
             raise ValueError("lengths must be [batch]")
         if out is None:
-            O = Q.new_empty(shape)
+            O = _new(Q, shape, Q.dtype, stream)
             op, ob, oh = O.data_ptr(), heads * self.head_dim, self.head_dim
         else:
             O = out
             if O.dtype != Q.dtype:
                 raise ValueError("out must have Q's dtype")
             op, ob, oh = _heads(O, shape, "out")
-        lse = Q.new_empty((batch, heads), dtype=torch.float32) if with_lse else None
+        lse = _new(Q, (batch, heads), torch.float32, stream) if with_lse else None
         pages = page_table.shape[1]
         ld = page_table.stride(0) if batch > 1 else pages
         wp, wn, _own = _space(workspace, lambda: self.attend_workspace(batch, heads, pages), stream)

@@ -41,3 +41,57 @@ def test_linear_is_the_two_calls_bit_for_bit(n, c, d):
     one = mpq.mx_linear(X, *W)
     assert bool(torch.isfinite(one).all())
     assert torch.equal(one, two), int((one != two).sum())
+
+
+def _pool_of(t):
+    """The stream whose pool of torch's allocator a tensor's memory belongs to."""
+    import torch
+    for seg in torch.cuda.memory_snapshot():
+        if seg["address"] <= t.data_ptr() < seg["address"] + seg["total_size"]:
+            return seg["stream"]
+    raise AssertionError("not of the allocator")
+
+
+def test_outputs_belong_to_the_stream_that_writes_them():
+    """With stream=, a call's new outputs come from that stream's pool: memory
+    that the current stream's work may still use is not among it."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    say("case outputs on a stream")
+    W, X = _uneven((48, 96), 1), _uneven((6, 96), 2)
+    batch = X.t().contiguous()
+    ints = torch.randint(-100, 101, (5, 96), device="cuda").to(torch.int8)
+    cache = mpq.MXCache.empty(9, 16, 2, 64, "fp8")
+    K, V = _uneven((20, 128), 3).reshape(20, 2, 64), _uneven((20, 128), 4).reshape(20, 2, 64)
+    slots = torch.arange(20, device="cuda")
+    table = torch.arange(2, dtype=torch.int32, device="cuda")[None]
+    length = torch.tensor([20], dtype=torch.int32, device="cuda")
+    codes, scales = mpq.mx_quantize(W)
+    xc, xs = mpq.mx_quantize(X)
+    fit = mpq.fit_layer(W, 4, 3, 64, 0.01)
+    A, _ = mpq.integer_scales(fit[1], fit[2], 8)
+    cache.write(K, V, slots)
+
+    def calls(stream):
+        yield "fit_layer", mpq.fit_layer(W, 4, 3, 64, 0.01, stream=stream)
+        yield "fit_layer_calib", mpq.fit_layer_calib(W, 4, 3, 64, batch, 0.01, stream=stream)
+        yield "output_error", mpq.output_error(W, *fit[:3], batch, with_ref=True, stream=stream)
+        yield "reconstruct", (mpq.reconstruct(*fit[:3], stream=stream),)
+        yield "integer_scales", mpq.integer_scales(fit[1], fit[2], 8, stream=stream)
+        yield "integer_forward", (mpq.integer_forward(fit[0], A, fit[2], ints, 8, stream=stream),)
+        yield "mx_quantize", mpq.mx_quantize(W, stream=stream)
+        yield "mx_dequantize", (mpq.mx_dequantize(codes, scales, 96, stream=stream),)
+        yield "mx_product", (mpq.mx_product(xc, xs, codes, scales, 96, stream=stream),)
+        yield "mx_linear", (mpq.mx_linear(X, codes, scales, stream=stream),)
+        yield "read", cache.read(slots, stream=stream)
+        yield "attend", cache.attend(K[:1], table, length, with_lse=True, stream=stream)
+
+    want = dict(calls(None))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, torch.cuda.ExternalStream(side.cuda_stream)):
+        for name, got in calls(stream):
+            side.synchronize()
+            for a, b in zip(got, want[name]):
+                assert _pool_of(a) == side.cuda_stream, name
+                assert torch.equal(a, b), name

@@ -115,10 +115,13 @@ __device__ __forceinline__ void to_bf16(const uint32_t *w, float sc, bf16x2 (&v)
     }
 }
 
-// x as the sum of kPieces bf16 values (each piece the rest's nearest).
-template <int kPieces, int kN, class V>
+// x as the sum of kPieces bf16 values (each piece the rest's nearest).  kWide: an
+// fp32 value of any size; one whose nearest would be infinity begins with
+// bf16's largest, and the next piece has the rest (an infinity's, a NaN's too).
+template <int kPieces, bool kWide, int kN, class V>
 __device__ __forceinline__ void split(const float (&x)[kN], V (&out)[kPieces])
 {
+    constexpr float kLargest = 0x1.fep127f;
     float rest[kN];
 #pragma unroll
     for (int i = 0; i < kN; ++i) rest[i] = x[i];
@@ -126,7 +129,7 @@ __device__ __forceinline__ void split(const float (&x)[kN], V (&out)[kPieces])
     for (int p = 0; p < kPieces; ++p)
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
-            const __bf16 h = (__bf16)rest[i];
+            const __bf16 h = (__bf16)(kWide && p == 0 ? fminf(fmaxf(rest[i], -kLargest), kLargest) : rest[i]);
             out[p][i] = h;
             rest[i] -= (float)h;
         }
@@ -309,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, kNb > 4 || kQ > 2 ? 2 : 3) mx_attend
             l += p[x];
         }
         bf16x4 pf[kP];
-        split(p, pf);
+        split<kP, false>(p, pf);
 #pragma unroll
         for (int q = 0; q < S::kVg; ++q) {
             // the four tokens' kE dimensions as bf16 pairs of dimensions, then
@@ -360,7 +363,7 @@ __global__ void __launch_bounds__(kThreads, kNb > 4 || kQ > 2 ? 2 : 3) mx_attend
             if (r >= cols || 8 * (g * kNb + i) >= a.c.dim)
 #pragma unroll
                 for (int y = 0; y < 8; ++y) x[i][y] = 0.0f;
-            split(x[i], qf[i]);
+            split<kQ, (kQ > 2)>(x[i], qf[i]);
         }
         int i = 0;
         for (; i + 2 < mine; i += 2) {

@@ -95,3 +95,39 @@ def test_outputs_belong_to_the_stream_that_writes_them():
             for a, b in zip(got, want[name]):
                 assert _pool_of(a) == side.cuda_stream, name
                 assert torch.equal(a, b), name
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+def test_attend_queries_up_to_the_largest_fp32(fmt):
+    """fp32 queries past bf16's largest value are finite, and split exactly; an
+    infinity or a NaN gives its own head a NaN and no other."""
+    import torch
+    import mx_ref as ref
+    from paper_2002_09049_amd import mpq
+    say(f"case mx attend huge queries {fmt}")
+    rng = np.random.default_rng(6)
+    n, dim = 50, 64
+    cache = mpq.MXCache.empty(4, 16, 1, dim, fmt)
+    K = (rng.standard_normal((n, 1, dim)) * 2.0 ** -110).astype(np.float32)
+    V = rng.standard_normal((n, 1, dim)).astype(np.float32)
+    slots = torch.arange(n, device="cuda")
+    cache.write(torch.from_numpy(K).cuda(), torch.from_numpy(V).cuda(), slots)
+    k, v = (t.double().cpu().numpy()[:, 0] for t in cache.read(slots))
+    q = (rng.uniform(-1, 1, (1, 5, dim)) * 2.0 ** 126).astype(np.float32)
+    top = np.finfo(np.float32).max
+    q[0, 0, ::5], q[0, 1, ::7], q[0, 2, 3] = top, -top, np.float32(3.3961e38)   # bf16: 3.38953e38, ties at 3.39618e38
+    q[0, 3, 9], q[0, 4, 60] = np.inf, np.nan
+    scale = 2.0 ** -19
+    table = torch.arange(4, dtype=torch.int32, device="cuda")[None]
+    O, lse = cache.attend(torch.from_numpy(q).cuda(), table, torch.tensor([n], dtype=torch.int32, device="cuda"),
+                          scale=scale, with_lse=True)
+    O, lse = O.double().cpu().numpy()[0], lse.double().cpu().numpy()[0]
+    assert np.isnan(O[3:]).all() and np.isnan(lse[3:]).all()
+    e = 2.0 ** -24
+    for h in range(3):
+        x = q[0, h].astype(np.float64)
+        want, l, mag = ref.attend(x, k, v, scale)
+        s = np.abs(k @ x) * scale
+        delta = e * ((3 * dim + 8) * scale * (np.abs(k) @ np.abs(x)) + 4 * (s + s.max())).max() + 2.0 ** -22
+        assert (np.abs(O[h] - want) <= (2 * delta + e + 2 * (n + 64) * e) * mag + e * np.abs(want)).all()
+        assert abs(lse[h] - l) <= delta + (n + 64) * e + 2.0 ** -22 * (1 + abs(l))

@@ -429,13 +429,18 @@ def _fp4(codes: torch.Tensor, scales: torch.Tensor, d: int, name: str):
     return _dev(codes, torch.uint8, f"{name} codes"), _dev(scales, torch.uint8, f"{name} scales")
 
 
+# the place of a workspace of no bytes (torch gives it none): without one the
+# library would take it that there is no workspace and allocate its own
+_NO_BYTES = 16
+
+
 def _space(workspace, need, stream):
     """(pointer, bytes, owner) of a call's workspace: the caller's; else, on the
     current stream, need() bytes of torch's allocator (the owner keeps them
     until the call is enqueued); else none, and the library takes its own
     scratch on the caller's stream."""
     if workspace is not None:
-        return _dev(workspace, torch.uint8, "workspace"), workspace.numel(), None
+        return _dev(workspace, torch.uint8, "workspace") or _NO_BYTES, workspace.numel(), None
     if stream is None:
         n = need()
         if n > 0:

@@ -131,3 +131,27 @@ def test_attend_queries_up_to_the_largest_fp32(fmt):
         delta = e * ((3 * dim + 8) * scale * (np.abs(k) @ np.abs(x)) + 4 * (s + s.max())).max() + 2.0 ** -22
         assert (np.abs(O[h] - want) <= (2 * delta + e + 2 * (n + 64) * e) * mag + e * np.abs(want)).all()
         assert abs(lse[h] - l) <= delta + (n + 64) * e + 2.0 ** -22 * (1 + abs(l))
+
+
+def test_a_workspace_that_is_too_small_is_refused():
+    """An empty one too, which has no address; where none is needed, it will do."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    say("case mx small workspaces")
+    empty = torch.empty((0,), dtype=torch.uint8, device="cuda")
+    W = mpq.mx_quantize(_uneven((48, 96), 1))
+    need = mpq.mx_linear_workspace(6, 48, 96)
+    assert need > 0 and mpq.mx_linear_workspace(3, 48, 96) == 0
+    X = _uneven((6, 96), 2)
+    for space in (empty, torch.empty((need - 1,), dtype=torch.uint8, device="cuda")):
+        with pytest.raises(mpq.MPQError, match="too small"):
+            mpq.mx_linear(X, *W, workspace=space)
+    assert torch.equal(mpq.mx_linear(X[:3], *W, workspace=empty), mpq.mx_linear(X[:3], *W))
+    cache = mpq.MXCache.empty(200, 16, 1, 32, "fp8")
+    Q = _uneven((1, 32), 3)[:, None]
+    table = torch.arange(200, dtype=torch.int32, device="cuda")[None]
+    length = torch.tensor([30], dtype=torch.int32, device="cuda")
+    assert cache.attend_workspace(1, 1, 200) > 0 and cache.attend_workspace(1, 1, 2) == 0
+    with pytest.raises(mpq.MPQError, match="too small"):
+        cache.attend(Q, table, length, workspace=empty)
+    assert torch.equal(cache.attend(Q, table[:, :2], length, workspace=empty), cache.attend(Q, table[:, :2], length))

@@ -434,17 +434,17 @@ def _fp4(codes: torch.Tensor, scales: torch.Tensor, d: int, name: str):
 _NO_BYTES = 16
 
 
-def _space(workspace, need, stream):
+def _space(workspace, need, stream, like: torch.Tensor):
     """(pointer, bytes, owner) of a call's workspace: the caller's; else, on the
-    current stream, need() bytes of torch's allocator (the owner keeps them
-    until the call is enqueued); else none, and the library takes its own
-    scratch on the caller's stream."""
+    current stream, need() bytes of torch's allocator on the device of `like` (the
+    owner keeps them until the call is enqueued); else none, and the library
+    takes its own scratch on the caller's stream."""
     if workspace is not None:
         return _dev(workspace, torch.uint8, "workspace") or _NO_BYTES, workspace.numel(), None
     if stream is None:
         n = need()
         if n > 0:
-            own = torch.empty((n,), dtype=torch.uint8, device="cuda")
+            own = like.new_empty((n,), dtype=torch.uint8)
             return own.data_ptr(), n, own
     return None, 0, None
 
@@ -529,7 +529,7 @@ def mx_linear(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bias: 
     if bias is not None and bias.shape != (c,):
         raise ValueError(f"bias must be ({c},)")
     Y, yp, dt, ld = _rows_out(out, n, c, X.dtype if dtype is None else dtype, X, stream)
-    wp, wn, _own = _space(workspace, lambda: mx_linear_workspace(n, c, d), stream)
+    wp, wn, _own = _space(workspace, lambda: mx_linear_workspace(n, c, d), stream, X)
     _check(load().mpq_mx_linear(xp, xt, n, x_ld, wc, ws, c, d,
                                 None if bias is None else _dev(bias, torch.float32, "bias"), yp, dt, ld, wp, wn,
                                 _stream(stream)))
@@ -646,7 +646,7 @@ class MXCache:
         lse = _new(Q, (batch, heads), torch.float32, stream) if with_lse else None
         pages = page_table.shape[1]
         ld = page_table.stride(0) if batch > 1 else pages
-        wp, wn, _own = _space(workspace, lambda: self.attend_workspace(batch, heads, pages), stream)
+        wp, wn, _own = _space(workspace, lambda: self.attend_workspace(batch, heads, pages), stream, Q)
         _check(load().mpq_mx_attend(self._at, qp, qb, qh, _mx_dtype(Q.dtype, "Q"), batch, heads,
                                     page_table.data_ptr(), ld, pages, _dev(lengths, torch.int32, "lengths"),
                                     int(window), self.head_dim ** -0.5 if scale is None else float(scale), op, ob, oh,

@@ -466,7 +466,7 @@ int mpq_integer_forward_layers(const mpq_int_layer *layers, int n_layers, int ma
  * mpq_mx_quantize - rows to fp4 blocks.
  *   X      [rows][ld] of dtype, the first d of each row (input); ld >= d.
  *   codes  [rows][D / 2], scales [rows][D / 32] (outputs).
- *   rows >= 0, 1 <= d <= MPQ_MX_MAX_D.
+ *   rows >= 0, 1 <= d <= MPQ_MX_MAX_D, rows * D at most 2^42.
  * mpq_mx_dequantize - the values that they stand for, rounded to dtype (exact
  * in fp32 and bf16).  Y [rows][ld] of dtype (output).
  * Errors: MPQ_ERR_INVALID_ARG, MPQ_ERR_HIP.

@@ -31,6 +31,14 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 constexpr int kFp4 = 0, kFp8 = 1;   // MPQ_MX_FP4, MPQ_MX_FP8
 constexpr int kMxBlock = 32;
 
+// The work-items of a launch are counted in 32 bits along each dimension: more
+// than kGridRow workgroups in x (of at most 1024) go in rows of that many, along
+// the dimension left free.  The last row goes past the end.
+constexpr int64_t kGridRow = 1 << 20;
+inline unsigned grid_x(int64_t blocks) { return (unsigned)(blocks < kGridRow ? blocks : kGridRow); }
+inline int64_t grid_rows(int64_t blocks) { return (blocks + kGridRow - 1) / kGridRow; }
+__device__ __forceinline__ int64_t block_of(unsigned row) { return row * kGridRow + blockIdx.x; }
+
 // Eight consecutive values of a row as they lie in memory: what a load in
 // flight fills (their values taken apart, the load would have to be done).
 template <class T>

@@ -36,7 +36,7 @@ __device__ __forceinline__ bool place(int heads, int nb, Place &p)
 {
     const int per = 4 * nb, rows = rows_of(nb);
     const uint32_t row = small_quotient(threadIdx.x, 1.0f / (float)per);
-    const int64_t row0 = (int64_t)blockIdx.x * rows, token0 = quotient(row0, heads);
+    const int64_t row0 = block_of(blockIdx.y) * rows, token0 = quotient(row0, heads);
     const uint32_t h = (uint32_t)(row0 - token0 * heads) + row;   // below 65535 + 64
     const uint32_t more = small_quotient(h, 1.0f / (float)heads);
     p.token = token0 + more;
@@ -142,21 +142,21 @@ int64_t row_blocks(const MxCacheView &c, int64_t tokens)
 }  // namespace
 
 template <class T>
-static hipError_t write_as(const MxCacheView &c, const MxRows &r, int64_t tokens, const int64_t *slots, unsigned blocks,
+static hipError_t write_as(const MxCacheView &c, const MxRows &r, int64_t tokens, const int64_t *slots, dim3 grid,
                            hipStream_t s)
 {
     auto kern = c.fmt == kFp4 ? mx_cache_write_kernel<kFp4, T> : mx_cache_write_kernel<kFp8, T>;
-    hipLaunchKernelGGL(kern, dim3(blocks), dim3(kThreads), 0, s, c, (const T *)r.K, (const T *)r.V, r.k_tok,
+    hipLaunchKernelGGL(kern, grid, dim3(kThreads), 0, s, c, (const T *)r.K, (const T *)r.V, r.k_tok,
                        r.k_head, r.v_tok, r.v_head, tokens, slots);
     return hipGetLastError();
 }
 
 template <class T>
-static hipError_t read_as(const MxCacheView &c, const MxRows &r, int64_t tokens, const int64_t *slots, unsigned blocks,
+static hipError_t read_as(const MxCacheView &c, const MxRows &r, int64_t tokens, const int64_t *slots, dim3 grid,
                           hipStream_t s)
 {
     auto kern = c.fmt == kFp4 ? mx_cache_read_kernel<kFp4, T> : mx_cache_read_kernel<kFp8, T>;
-    hipLaunchKernelGGL(kern, dim3(blocks), dim3(kThreads), 0, s, c, (T *)r.K, (T *)r.V, r.k_tok, r.k_head, r.v_tok,
+    hipLaunchKernelGGL(kern, grid, dim3(kThreads), 0, s, c, (T *)r.K, (T *)r.V, r.k_tok, r.k_head, r.v_tok,
                        r.v_head, tokens, slots);
     return hipGetLastError();
 }
@@ -166,11 +166,12 @@ hipError_t launch_mx_cache_write(const MxCacheView &c, const MxRows &r, int64_t 
 {
     const int64_t blocks = row_blocks(c, tokens);
     if (blocks <= 0) return hipSuccess;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (grid_rows(blocks) > 65535) return hipErrorInvalidValue;
+    const dim3 grid(grid_x(blocks), (unsigned)grid_rows(blocks));
     LaunchTimer timer(s, "mx_cache_write_kernel");
-    if (r.dtype == MPQ_F32) return write_as<float>(c, r, tokens, slots, (unsigned)blocks, s);
-    if (r.dtype == MPQ_F16) return write_as<_Float16>(c, r, tokens, slots, (unsigned)blocks, s);
-    return write_as<__bf16>(c, r, tokens, slots, (unsigned)blocks, s);
+    if (r.dtype == MPQ_F32) return write_as<float>(c, r, tokens, slots, grid, s);
+    if (r.dtype == MPQ_F16) return write_as<_Float16>(c, r, tokens, slots, grid, s);
+    return write_as<__bf16>(c, r, tokens, slots, grid, s);
 }
 
 hipError_t launch_mx_cache_read(const MxCacheView &c, const MxRows &r, int64_t tokens, const int64_t *slots,
@@ -178,11 +179,12 @@ hipError_t launch_mx_cache_read(const MxCacheView &c, const MxRows &r, int64_t t
 {
     const int64_t blocks = row_blocks(c, tokens);
     if (blocks <= 0) return hipSuccess;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (grid_rows(blocks) > 65535) return hipErrorInvalidValue;
+    const dim3 grid(grid_x(blocks), (unsigned)grid_rows(blocks));
     LaunchTimer timer(s, "mx_cache_read_kernel");
-    if (r.dtype == MPQ_F32) return read_as<float>(c, r, tokens, slots, (unsigned)blocks, s);
-    if (r.dtype == MPQ_F16) return read_as<_Float16>(c, r, tokens, slots, (unsigned)blocks, s);
-    return read_as<__bf16>(c, r, tokens, slots, (unsigned)blocks, s);
+    if (r.dtype == MPQ_F32) return read_as<float>(c, r, tokens, slots, grid, s);
+    if (r.dtype == MPQ_F16) return read_as<_Float16>(c, r, tokens, slots, grid, s);
+    return read_as<__bf16>(c, r, tokens, slots, grid, s);
 }
 
 }  // namespace mpq

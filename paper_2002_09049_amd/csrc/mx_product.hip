@@ -121,7 +121,8 @@ __global__ void __launch_bounds__(kFewWaves *kWave) mx_few_kernel(MxProduct p)
     __shared__ __align__(16) float part[kFewWaves][kNT][kWave * 4];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = lane % 16, g = lane / 16;
-    const int64_t c0 = (int64_t)blockIdx.x * 16, t0 = (int64_t)blockIdx.y * 16 * kNT;
+    const int64_t c0 = block_of(blockIdx.z) * 16, t0 = (int64_t)blockIdx.y * 16 * kNT;
+    if (c0 >= p.c) return;
     const int nb = p.nb;
     // rows past the end repeat the last one: their sums are not stored
     const int64_t wrow = min(c0 + r, p.c - 1);
@@ -165,7 +166,8 @@ __global__ void __launch_bounds__(kFewWaves *kWave) mx_token_kernel(MxProduct p,
     __shared__ __align__(4) uint8_t xscales[kFewWaves][kN][kChunkBlocks];          // block 4i + g at 4g + i
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = lane % 16, g = lane / 16;
-    const int64_t c0 = (int64_t)blockIdx.x * 16;
+    const int64_t c0 = block_of(blockIdx.z) * 16;
+    if (c0 >= p.c) return;
     const int nb = p.nb;
     const int64_t wrow = min(c0 + r, p.c - 1);
     f32x4 acc[1] = {f32x4{0, 0, 0, 0}};
@@ -722,11 +724,14 @@ __global__ void __launch_bounds__(256) mx_slab_kernel(MxProduct p)
     }
 }
 
+// Workgroups of 256 threads that one launch can have in x.
+constexpr int64_t kMostGroups = (1 << 24) - 1;
+
 template <int kTM, int kTN>
 hipError_t launch_tiles(const MxProduct &p, hipStream_t s)
 {
     const int64_t tiles = ((p.c + 64 * kTM - 1) / (64 * kTM)) * ((p.n + 64 * kTN - 1) / (64 * kTN));
-    if (tiles > 0x40000000LL) return hipErrorInvalidValue;
+    if (tiles > kMostGroups - kXcds) return hipErrorInvalidValue;   // more than 2^37 outputs
     LaunchTimer timer(s, kTM == 2 ? (kTN == 1 ? "mx_tile_kernel<2,1>" : "mx_tile_kernel<2,2>")
                                   : (kTN == 2 ? "mx_tile_kernel<4,2>" : "mx_tile_kernel<4,4>"));
     hipLaunchKernelGGL((mx_tile_kernel<kTM, kTN>), dim3((unsigned)((tiles + kXcds - 1) / kXcds * kXcds)), dim3(256), 0, s, p);
@@ -736,7 +741,8 @@ hipError_t launch_tiles(const MxProduct &p, hipStream_t s)
 template <int kN>
 hipError_t launch_token_as(const MxProduct &p, const void *X, int dtype, int64_t x_ld, int d, hipStream_t s)
 {
-    const dim3 grid((unsigned)((p.c + 15) / 16)), threads(kFewWaves * kWave);
+    const int64_t gx = (p.c + 15) / 16;
+    const dim3 grid(grid_x(gx), 1, (unsigned)grid_rows(gx)), threads(kFewWaves * kWave);
     if (dtype == MPQ_F32)
         hipLaunchKernelGGL((mx_token_kernel<kN, float>), grid, threads, 0, s, p, (const float *)X, x_ld, d);
     else if (dtype == MPQ_F16)
@@ -753,7 +759,7 @@ bool mx_quantizes_inside(int64_t n) { return n <= 4; }
 hipError_t launch_mx_token(const MxProduct &p, const void *X, int dtype, int64_t x_ld, int64_t d, hipStream_t s)
 {
     if (p.n <= 0 || p.c <= 0) return hipSuccess;
-    if (!mx_quantizes_inside(p.n) || (p.c + 15) / 16 > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (!mx_quantizes_inside(p.n) || grid_rows((p.c + 15) / 16) > 65535) return hipErrorInvalidValue;
     LaunchTimer timer(s, "mx_token_kernel");
     return p.n == 1 ? launch_token_as<1>(p, X, dtype, x_ld, (int)d, s) : launch_token_as<4>(p, X, dtype, x_ld, (int)d, s);
 }
@@ -806,7 +812,7 @@ hipError_t launch_mx_product(const MxProduct &p, hipStream_t s)
     const int64_t sx = (p.c + kSlabM - 1) / kSlabM, sy = (p.n + kSlabN - 1) / kSlabN;
     const double slab = 1.0 + ceil((double)sx * (double)sy / 256.0) * (1.9 + 0.34 * 4.0 * ceil(p.nb / 64.0));
     const bool by_model = !mx_quantizes_inside(p.n);
-    if (by_model && slab < best && slab < few && sx <= 0x7fffffffLL && sy <= 65535) {
+    if (by_model && slab < best && slab < few && sx <= kMostGroups && sy <= 65535) {
         LaunchTimer timer(s, "mx_slab_kernel");
         hipLaunchKernelGGL(mx_slab_kernel, dim3((unsigned)sx, (unsigned)sy), dim3(256), 0, s, p);
         return hipGetLastError();
@@ -816,10 +822,10 @@ hipError_t launch_mx_product(const MxProduct &p, hipStream_t s)
         if (best == t42) return launch_tiles<4, 2>(p, s);
         return best == t22 ? launch_tiles<2, 2>(p, s) : launch_tiles<2, 1>(p, s);
     }
-    if (gx > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (grid_rows(gx) > 65535) return hipErrorInvalidValue;
     LaunchTimer timer(s, "mx_few_kernel");
     auto kern = nt == 1 ? mx_few_kernel<1> : nt == 2 ? mx_few_kernel<2> : mx_few_kernel<4>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)gx, (unsigned)gy), dim3(kFewWaves * kWave), 0, s, p);
+    hipLaunchKernelGGL(kern, dim3(grid_x(gx), (unsigned)gy, (unsigned)grid_rows(gx)), dim3(kFewWaves * kWave), 0, s, p);
     return hipGetLastError();
 }
 

@@ -25,7 +25,7 @@ constexpr int kThreads = 256, kElems = kThreads * 8;
 // The row and the place in it of this thread's eight elements.
 __device__ __forceinline__ void place(int w, int64_t &row, int &j)
 {
-    const int64_t first = (int64_t)blockIdx.x * kElems;
+    const int64_t first = block_of(blockIdx.y) * kElems;
     const int64_t row0 = quotient(first, w);
     const uint32_t off = (uint32_t)(first - row0 * w) + 8 * threadIdx.x;
     // rows of 2048 or more: the first one or the next
@@ -67,17 +67,17 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t *
 
 template <class T>
 hipError_t quantize_as(const T *X, int64_t rows, int d, int64_t ld, int w, uint8_t *codes, uint8_t *scales,
-                       unsigned blocks, hipStream_t s)
+                       dim3 grid, hipStream_t s)
 {
-    hipLaunchKernelGGL(mx_quantize_kernel<T>, dim3(blocks), dim3(kThreads), 0, s, X, rows, d, ld, w, codes, scales);
+    hipLaunchKernelGGL(mx_quantize_kernel<T>, grid, dim3(kThreads), 0, s, X, rows, d, ld, w, codes, scales);
     return hipGetLastError();
 }
 
 template <class T>
 hipError_t dequantize_as(const uint8_t *codes, const uint8_t *scales, int64_t rows, int d, int w, T *Y, int64_t ld,
-                         unsigned blocks, hipStream_t s)
+                         dim3 grid, hipStream_t s)
 {
-    hipLaunchKernelGGL(mx_dequantize_kernel<T>, dim3(blocks), dim3(kThreads), 0, s, codes, scales, rows, d, w, Y, ld);
+    hipLaunchKernelGGL(mx_dequantize_kernel<T>, grid, dim3(kThreads), 0, s, codes, scales, rows, d, w, Y, ld);
     return hipGetLastError();
 }
 
@@ -89,12 +89,12 @@ hipError_t launch_mx_quantize(const void *X, int dtype, int64_t rows, int64_t d,
     const int w = (int)mx_row(d);
     const int64_t blocks = (rows * w + kElems - 1) / kElems;
     if (blocks <= 0) return hipSuccess;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (grid_rows(blocks) > 65535) return hipErrorInvalidValue;
+    const dim3 grid(grid_x(blocks), (unsigned)grid_rows(blocks));
     LaunchTimer timer(s, "mx_quantize_kernel");
-    const unsigned n = (unsigned)blocks;
-    if (dtype == MPQ_F32) return quantize_as((const float *)X, rows, (int)d, ld, w, codes, scales, n, s);
-    if (dtype == MPQ_F16) return quantize_as((const _Float16 *)X, rows, (int)d, ld, w, codes, scales, n, s);
-    return quantize_as((const __bf16 *)X, rows, (int)d, ld, w, codes, scales, n, s);
+    if (dtype == MPQ_F32) return quantize_as((const float *)X, rows, (int)d, ld, w, codes, scales, grid, s);
+    if (dtype == MPQ_F16) return quantize_as((const _Float16 *)X, rows, (int)d, ld, w, codes, scales, grid, s);
+    return quantize_as((const __bf16 *)X, rows, (int)d, ld, w, codes, scales, grid, s);
 }
 
 hipError_t launch_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t d, void *Y,
@@ -103,12 +103,12 @@ hipError_t launch_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int
     const int w = (int)mx_row(d);
     const int64_t blocks = (rows * w + kElems - 1) / kElems;
     if (blocks <= 0) return hipSuccess;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (grid_rows(blocks) > 65535) return hipErrorInvalidValue;
+    const dim3 grid(grid_x(blocks), (unsigned)grid_rows(blocks));
     LaunchTimer timer(s, "mx_dequantize_kernel");
-    const unsigned n = (unsigned)blocks;
-    if (dtype == MPQ_F32) return dequantize_as(codes, scales, rows, (int)d, w, (float *)Y, ld, n, s);
-    if (dtype == MPQ_F16) return dequantize_as(codes, scales, rows, (int)d, w, (_Float16 *)Y, ld, n, s);
-    return dequantize_as(codes, scales, rows, (int)d, w, (__bf16 *)Y, ld, n, s);
+    if (dtype == MPQ_F32) return dequantize_as(codes, scales, rows, (int)d, w, (float *)Y, ld, grid, s);
+    if (dtype == MPQ_F16) return dequantize_as(codes, scales, rows, (int)d, w, (_Float16 *)Y, ld, grid, s);
+    return dequantize_as(codes, scales, rows, (int)d, w, (__bf16 *)Y, ld, grid, s);
 }
 
 }  // namespace mpq

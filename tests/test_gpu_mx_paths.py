@@ -155,3 +155,68 @@ def test_a_workspace_that_is_too_small_is_refused():
     with pytest.raises(mpq.MPQError, match="too small"):
         cache.attend(Q, table, length, workspace=empty)
     assert torch.equal(cache.attend(Q, table[:, :2], length, workspace=empty), cache.attend(Q, table[:, :2], length))
+
+
+def _room(gib):
+    import torch
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gib << 30:
+        pytest.skip(f"needs {gib} GiB of device memory")
+
+
+def test_rows_past_one_launch_dimension():
+    """2^35 held elements and more: 2^24 workgroups of 256 threads, whose
+    threads no longer count in 32 bits."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    _room(24)
+    rows = (1 << 28) + 37
+    say(f"case mx rows {rows} x 1")
+    some = torch.tensor([1.0, -1.5, 0.0, 2.0, -3.0, 0.75, 4.0, -6.0, 0.5, 12.0, -0.0625], device="cuda").half()
+    X = some[torch.arange(rows, dtype=torch.int32, device="cuda") % 11][:, None]      # each held exactly
+    codes, scales = mpq.mx_quantize(X)
+    Y = mpq.mx_dequantize(codes, scales, 1, dtype=torch.float16)
+    assert torch.equal(X, Y)
+    tail = mpq.mx_quantize(X[-50:])
+    assert torch.equal(codes[-50:], tail[0]) and torch.equal(scales[-50:], tail[1])
+
+
+@pytest.mark.parametrize("n", [1, 6])
+def test_products_past_one_launch_dimension(n):
+    """2^27 rows of W and more: 2^23 workgroups of 512 threads."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    _room(30)
+    c, d, part = (1 << 27) + 4099, 40, 4096
+    say(f"case mx product of {c} rows, {n} tokens")
+    w = mpq.mx_quantize(_uneven((part, d), 5))
+    codes, scales = (torch.empty((c, t.shape[1]), dtype=torch.uint8, device="cuda") for t in w)
+    for whole, t in ((codes, w[0]), (scales, w[1])):
+        whole[:c // part * part].view(-1, part, t.shape[1])[:] = t
+        whole[c // part * part:] = t[:c % part]
+    X = _uneven((n, d), 6)
+    few = mpq.mx_linear(X, *w)
+    for Y in (mpq.mx_linear(X, codes, scales), mpq.mx_product(*mpq.mx_quantize(X), codes, scales, d)):
+        assert torch.equal(Y[:, :c // part * part].view(n, -1, part), few[:, None].expand(n, c // part, part))
+        assert torch.equal(Y[:, c // part * part:], few[:, :c % part])
+
+
+def test_cache_past_one_launch_dimension():
+    """2^30 rows of one block and more, of which a few have a slot."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    _room(40)
+    n, page = (1 << 30) + 70, 16
+    say(f"case mx cache of {n} tokens")
+    cache = mpq.MXCache.empty(8, page, 1, 1, "fp8")
+    K = torch.zeros((n, 1, 1), dtype=torch.bfloat16, device="cuda")
+    slots = torch.full((n,), -1, dtype=torch.int64, device="cuda")
+    where = torch.tensor([0, 5, (1 << 20) * 64 - 1, (1 << 20) * 64, (1 << 30) - 1, 1 << 30, n - 1], device="cuda")
+    value = torch.tensor([1.0, -2.0, 0.5, 3.0, -4.0, 1.5, 7.0], device="cuda").bfloat16()     # held exactly
+    K[where, 0, 0] = value
+    slots[where] = torch.arange(7, device="cuda") * 17
+    cache.write(K, K, slots)
+    k, v = cache.read(slots[where], dtype=torch.bfloat16)
+    assert torch.equal(k[:, 0, 0], value) and torch.equal(v[:, 0, 0], value)
+    k, v = cache.read(slots, dtype=torch.bfloat16)
+    assert torch.equal(k, K) and torch.equal(v, K)

@@ -365,7 +365,7 @@ std::vector<FitJob> build_fit_jobs(Search mode, bool hist_fits, const mpq_layer 
         FitJob j = fresh(v);
         for (int l = 0; l <= n_layers; ++l) {
             const bool flush = l == n_layers || j.b.n_layers == mpq::kMaxBatchLayers ||
-                               j.channels + (l < n_layers ? layers[l].c_out : 0) > 0x7fffffffLL;
+                               j.channels + (l < n_layers ? layers[l].c_out : 0) > mpq::kMaxLaunchChannels;
             if (flush && j.b.n_layers > 0) {
                 jobs.push_back(j);
                 j = fresh(v);
@@ -939,7 +939,7 @@ int clip_first_points(const mpq_layer *layers, int n_layers, int M, int P, int G
         int64_t ch = 0;
         for (int l = 0; l <= n_layers; ++l) {
             if ((l == n_layers || b.n_layers == mpq::kMaxClipLayers ||
-                 (l < n_layers && ch + layers[l].c_out > 0x7fffffffLL)) && b.n_layers > 0) {
+                 (l < n_layers && ch + layers[l].c_out > mpq::kMaxLaunchChannels)) && b.n_layers > 0) {
                 batches.push_back({b, ch});
                 b.n_layers = 0;
                 ch = 0;
@@ -1291,7 +1291,7 @@ int paper_impl(const mpq_layer *layers, int n_layers, int bits, int max_points, 
         fresh();
         for (int l = 0; l <= n_layers; ++l) {
             const bool flush = l == n_layers || j.b.n_layers == mpq::kMaxBatchLayers ||
-                               j.channels + (l < n_layers ? layers[l].c_out : 0) > 0x7fffffffLL;
+                               j.channels + (l < n_layers ? layers[l].c_out : 0) > mpq::kMaxLaunchChannels;
             if (flush && j.b.n_layers > 0) {
                 jobs.push_back(j);
                 fresh();

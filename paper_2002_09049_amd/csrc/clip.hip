@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kClipThreads) clip_choose_kernel(const ClipBat
 hipError_t launch_clip(const ClipBatch &b, int64_t channels, bool choose, hipStream_t s)
 {
     if (channels <= 0) return hipSuccess;
-    if (channels > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (!launchable(channels, kClipThreads)) return hipErrorInvalidValue;
     LaunchTimer timer(s, choose ? "clip_choose_kernel" : "clip_cand_kernel");
     hipLaunchKernelGGL(choose ? clip_choose_kernel : clip_cand_kernel, dim3((unsigned)channels),
                        dim3(kClipThreads), 0, s, b);

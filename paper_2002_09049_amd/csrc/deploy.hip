@@ -303,7 +303,7 @@ hipError_t launch_integer_scales(const float *scales, const int32_t *counts, int
 {
     const int64_t n = C * P;
     if (n <= 0) return hipSuccess;
-    if ((n + 255) / 256 > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (!launchable((n + 255) / 256, 256)) return hipErrorInvalidValue;
     LaunchTimer timer(s, "integer_scales_kernel");
     hipLaunchKernelGGL(integer_scales_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, scales,
                        counts, C, P, p, A, clamped);
@@ -334,7 +334,7 @@ hipError_t launch_int_forward(IntGroup &h, int mode, hipStream_t s)
         blocks += (tiles + kIXcds - 1) / kIXcds * kIXcds;
     }
     if (blocks == 0) return hipSuccess;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (!launchable(blocks, kIThreads)) return hipErrorInvalidValue;
     // chunks of four points (eight per chunk held a workgroup to one per CU,
     // 113 KB of LDS: ResNet-50's step took 0.81 ms against 0.60 ms)
     auto kern = mode == kLoad16 ? int_forward_kernel<kLoad16, 4>

@@ -219,6 +219,7 @@ FitLayout fit_layout(int64_t d, int G)
 hipError_t launch_fit(const FitParams &p, const FitLayout &L, hipStream_t s)
 {
     static_assert(kCandPerThread == 2, "layout assumes two candidates per thread");
+    if (!launchable(p.C, kFitThreads)) return hipErrorInvalidValue;
     auto kern = fit_dense_kernel<kCandPerThread>;
     if (L.lds > 65536) {
         hipError_t e = hipFuncSetAttribute((const void *)kern,

@@ -126,7 +126,7 @@ __global__ void zero_i32_kernel(int32_t *p, int64_t n)
 hipError_t launch_zero_i32(int32_t *p, int64_t n, hipStream_t s)
 {
     if (n <= 0) return hipSuccess;
-    if (n > (int64_t)256 * 0x7fffffff) return hipErrorInvalidValue;
+    if (!launchable((n + 255) / 256, 256)) return hipErrorInvalidValue;
     LaunchTimer timer(s, "zero_i32_kernel");
     hipLaunchKernelGGL(zero_i32_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, p, n);
     return hipGetLastError();

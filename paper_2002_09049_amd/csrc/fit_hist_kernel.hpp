@@ -988,7 +988,7 @@ fit_hist_kernel(const HistBatch B)
 template <int T, int EPT, int kMode, int kM>
 hipError_t launch_hist_t(const HistBatch &b, int64_t channels, hipStream_t s)
 {
-    if (kM > 0 && b.M != kM) return hipErrorInvalidValue;
+    if ((kM > 0 && b.M != kM) || !launchable(channels, T)) return hipErrorInvalidValue;
     auto kern = fit_hist_kernel<T, EPT, kMode, kM>;
     const size_t lds = hist_lds(kMode, T, b.M, b.G, b.points);
     if (lds > 60000) {

@@ -450,7 +450,7 @@ size_t paper_lds(int64_t dmax)
 hipError_t launch_fit_paper(const PaperBatch &b, int variant, int64_t channels, int64_t dmax, hipStream_t s)
 {
     if (channels <= 0) return hipSuccess;
-    if (channels > 0x7fffffffLL || dmax > kPaperMaxDim) return hipErrorInvalidValue;
+    if (!launchable(channels, kPT) || dmax > kPaperMaxDim) return hipErrorInvalidValue;
     const size_t lds = paper_lds(dmax);
     switch (variant) {
     case 0: return launch_paper_t<2>(b, channels, lds, s);

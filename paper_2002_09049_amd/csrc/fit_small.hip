@@ -340,7 +340,7 @@ hipError_t launch_small_t(const HistBatch &b, int64_t channels, hipStream_t s)
 hipError_t launch_fit_small(const HistBatch &b, int d, int64_t channels, hipStream_t s)
 {
     if (channels <= 0) return hipSuccess;
-    if (channels > 0x7fffffffLL - kSmallWaves) return hipErrorInvalidValue;
+    if (!launchable((channels + kSmallWaves - 1) / kSmallWaves, kSmallWaves * kWave)) return hipErrorInvalidValue;
     static_assert(kSmallMaxDim == 16, "one instantiation per length below");
     switch (d) {
     case 1: return launch_small_t<1>(b, channels, s);

@@ -13,6 +13,14 @@ namespace mpq {
 int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 int hip_fail(hipError_t e, const char *what);
 
+// Whether a launch of so many workgroups in x can be made: its threads along a
+// dimension count in 32 bits, and of more the runtime runs only some, without an
+// error.
+inline bool launchable(int64_t blocks, int threads) { return blocks <= 0xffffffffLL / threads; }
+// Channels of several layers in one launch, one workgroup (of up to 1024
+// threads) each.
+constexpr int64_t kMaxLaunchChannels = (1 << 22) - 1;
+
 // Brackets one kernel launch with events on its stream while timing is on
 // (mpq_timing_enable); otherwise does nothing.
 class LaunchTimer {

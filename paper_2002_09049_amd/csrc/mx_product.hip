@@ -724,14 +724,11 @@ __global__ void __launch_bounds__(256) mx_slab_kernel(MxProduct p)
     }
 }
 
-// Workgroups of 256 threads that one launch can have in x.
-constexpr int64_t kMostGroups = (1 << 24) - 1;
-
 template <int kTM, int kTN>
 hipError_t launch_tiles(const MxProduct &p, hipStream_t s)
 {
     const int64_t tiles = ((p.c + 64 * kTM - 1) / (64 * kTM)) * ((p.n + 64 * kTN - 1) / (64 * kTN));
-    if (tiles > kMostGroups - kXcds) return hipErrorInvalidValue;   // more than 2^37 outputs
+    if (!launchable(tiles + kXcds - 1, 256)) return hipErrorInvalidValue;   // more than 2^37 outputs
     LaunchTimer timer(s, kTM == 2 ? (kTN == 1 ? "mx_tile_kernel<2,1>" : "mx_tile_kernel<2,2>")
                                   : (kTN == 2 ? "mx_tile_kernel<4,2>" : "mx_tile_kernel<4,4>"));
     hipLaunchKernelGGL((mx_tile_kernel<kTM, kTN>), dim3((unsigned)((tiles + kXcds - 1) / kXcds * kXcds)), dim3(256), 0, s, p);
@@ -812,7 +809,7 @@ hipError_t launch_mx_product(const MxProduct &p, hipStream_t s)
     const int64_t sx = (p.c + kSlabM - 1) / kSlabM, sy = (p.n + kSlabN - 1) / kSlabN;
     const double slab = 1.0 + ceil((double)sx * (double)sy / 256.0) * (1.9 + 0.34 * 4.0 * ceil(p.nb / 64.0));
     const bool by_model = !mx_quantizes_inside(p.n);
-    if (by_model && slab < best && slab < few && sx <= kMostGroups && sy <= 65535) {
+    if (by_model && slab < best && slab < few && launchable(sx, 256) && sy <= 65535) {
         LaunchTimer timer(s, "mx_slab_kernel");
         hipLaunchKernelGGL(mx_slab_kernel, dim3((unsigned)sx, (unsigned)sy), dim3(256), 0, s, p);
         return hipGetLastError();

@@ -1254,7 +1254,7 @@ hipError_t launch_output_error_group(const ErrLayerIn *in, int n_in, int group, 
             blocks += ((int64_t)L.tiles + kXcds - 1) / kXcds * kXcds -
                       (planned + kXcds - 1) / kXcds * kXcds;
         }
-        if (blocks > 0x7fffffffLL || fblocks > 0x7fffffffLL || nblocks > 0x7fffffffLL || sblocks > 0x7fffffffLL)
+        if (!launchable(blocks, kThreads) || fblocks > 0x7fffffffLL || !launchable(nblocks, 256) || sblocks > 0x7fffffffLL)
             return hipErrorInvalidValue;
         hipError_t e = hipSuccess;
         // the descriptor table at the head of the group's scratch
@@ -1271,7 +1271,7 @@ hipError_t launch_output_error_group(const ErrLayerIn *in, int n_in, int group, 
         // the scan and the forming in one launch where a call has both now
         const int scans = (parts & kErrScan) ? (int)sblocks : 0;
         const int64_t forms = (parts & kErrKernels) ? fblocks : 0;
-        if (scans + forms > 0x7fffffffLL) return hipErrorInvalidValue;
+        if (!launchable(scans + forms, std::max(kScanThreads, kFormThreads))) return hipErrorInvalidValue;
         if (e == hipSuccess && scans + forms > 0) {
             const dim3 grid((unsigned)(scans + forms));
             LaunchTimer timer(s, forms ? "form_d_kernel" : "scan_x_kernel");

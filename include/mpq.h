@@ -564,7 +564,10 @@ int mpq_mx_cache_read(const mpq_mx_cache *cache, void *K, int64_t k_stride, int6
  * A sequence without tokens has O = 0 and lse = -infinity.  What the cache
  * holds outside the tokens named, NaN included, has no influence.  Sums and
  * softmax statistics are fp32; p_j enters the matrix cores as two or three
- * bf16 pieces (relative error 2^-16 for 16-bit dtypes, 2^-24 for fp32).
+ * bf16 pieces (relative error 2^-16 for 16-bit dtypes, 2^-24 for fp32).  Held
+ * values enter them as bf16: exactly, but for fp8 blocks with a scale byte
+ * below 3 (nothing in them reaches 2^-116), whose values are rounded to
+ * multiples of 2^-133.
  *   workspace_opt, workspace_bytes  as for mpq_mx_linear, of at least
  *               mpq_mx_attend_workspace(cache, batch, q_heads, max_pages)
  *               bytes (enough for any window).

@@ -18,8 +18,9 @@
 //    (heads of up to 64: four) consecutive dimensions 8 (l % 16) ..; each is
 //    converted with its own token's scale, and v_perm pairs tokens.  Output
 //    register j then belongs to dimension 8 (row) + j.
-// Elements convert to bf16 exactly (at most four significant bits, any
-// power of two of a scale).  Q and P are split into bf16 pieces whose sum is
+// Elements convert to bf16 exactly (at most four significant bits), but for fp8
+// blocks with a scale byte below 3 (nothing in them reaches 2^-116): theirs
+// are rounded to multiples of 2^-133, bf16's least.  Q and P are split into bf16 pieces whose sum is
 // the value: Q exactly (1 piece for bf16, 2 for f16, 3 for f32), P to 2^-16
 // (2 pieces; outputs of 16 bits) or 2^-24 (3).
 //

@@ -220,3 +220,45 @@ def test_cache_past_one_launch_dimension():
     assert torch.equal(k[:, 0, 0], value) and torch.equal(v[:, 0, 0], value)
     k, v = cache.read(slots, dtype=torch.bfloat16)
     assert torch.equal(k, K) and torch.equal(v, K)
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("small", ["keys", "values"])
+def test_attend_smallest_blocks(fmt, small):
+    """Blocks of the least scale bytes: fp4 exactly, fp8 with each element
+    rounded to a multiple of 2^-133 (at most 2^-134 off)."""
+    import torch
+    import mx_ref as ref
+    from paper_2002_09049_amd import mpq
+    say(f"case mx attend smallest blocks {fmt} {small}")
+    n, dim, e, least = 90, 64, 2.0 ** -24, 2.0 ** -134 if fmt == "fp8" else 0.0
+    for power in (-114, -117, -119, -122, -125, -127):
+        rng = np.random.default_rng(-power)
+        cache = mpq.MXCache.empty(6, 16, 1, dim, fmt)
+        K, V = (rng.standard_normal((n, 1, dim)).astype(np.float32) for _ in "KV")
+        q = rng.uniform(-1, 1, (1, 1, dim))
+        scale = dim ** -0.5
+        if small == "keys":
+            K = np.ldexp(K, power)
+            q, scale = np.ldexp(q, 120), scale * 2.0 ** (-power - 120)
+        else:
+            V = np.ldexp(V, power)
+        q = q.astype(np.float32)
+        slots = torch.arange(n, device="cuda")
+        cache.write(torch.from_numpy(K).cuda(), torch.from_numpy(V).cuda(), slots)
+        k, v = (t.double().cpu().numpy()[:, 0] for t in cache.read(slots))
+        table = torch.arange(6, dtype=torch.int32, device="cuda")[None]
+        O, lse = cache.attend(torch.from_numpy(q).cuda(), table, torch.tensor([n], dtype=torch.int32, device="cuda"),
+                              scale=scale, with_lse=True)
+        x = q[0, 0].astype(np.float64)
+        want, l, mag = ref.attend(x, k, v, scale)
+        s = np.abs(k @ x) * scale
+        delta = e * ((3 * dim + 8) * scale * (np.abs(k) @ np.abs(x)) + 4 * (s + s.max())).max() + 2.0 ** -22
+        if small == "keys":
+            delta += scale * least * np.abs(x).sum()
+        room = (2 * delta + e + 2 * (n + 64) * e) * mag + e * np.abs(want) + 2.0 ** -149 * (n + 64)
+        if small == "values":
+            room += least
+        o = O.double().cpu().numpy()[0, 0]
+        assert (np.abs(o - want) <= room).all(), (power, np.max(np.abs(o - want) / room))
+        assert abs(float(lse) - l) <= delta + (n + 64) * e + 2.0 ** -22 * (1 + abs(l)), power

@@ -636,7 +636,7 @@ class MXCache:
         if lengths.shape != (batch,):
             raise ValueError("lengths must be [batch]")
         if out is None:
-            O = _new(Q, shape, Q.dtype, stream)
+            O = Q.new_empty(shape) if stream is None else _new(Q, shape, Q.dtype, stream)
             op, ob, oh = O.data_ptr(), heads * self.head_dim, self.head_dim
         else:
             O = out

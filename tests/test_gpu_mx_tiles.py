@@ -158,3 +158,31 @@ def test_captured_calls_of_two_launches():
         torch.cuda.synchronize()
         for a, b in zip(got, want):
             assert torch.equal(a, b) and bool(torch.isfinite(b.float()).all()), i
+
+
+# a size for each of the product's kernels
+KINDS = [(1, 300, 2000), (4, 40, 700), (12, 300, 2000), (40, 500, 2100), (500, 4001, 1300), (1000, 4001, 1300),
+         (2000, 4001, 1300), (3900, 4001, 700)]
+
+
+@pytest.mark.parametrize("n,c,d", KINDS)
+def test_blocks_of_different_sizes(n, c, d):
+    """Blocks 2^24 apart within a row: small ones beside large ones err by
+    roundings of the whole sum alone."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    say(f"case mx uneven blocks n={n} c={c} d={d}")
+    g = torch.Generator(device="cuda").manual_seed(n + c)
+
+    def uneven(r):
+        x = torch.randn((r, d), generator=g, device="cuda")
+        size = torch.randint(-12, 13, (r, -(-d // 32)), generator=g, device="cuda")
+        return torch.ldexp(x, size.repeat_interleave(32, 1)[:, :d])
+
+    w, x = mpq.mx_quantize(uneven(c)), uneven(n)
+    Y = mpq.mx_linear(x, *w)
+    xv, wv = mpq.mx_dequantize(*mpq.mx_quantize(x), d).double(), mpq.mx_dequantize(*w, d).double().t().contiguous()
+    want, mag = xv @ wv, xv.abs() @ wv.abs()
+    most = (128 + -(-d // 128) + 16) * E * mag + E * want.abs()
+    err = (Y.double() - want).abs()
+    assert bool((err <= most).all()), float((err / most).max())

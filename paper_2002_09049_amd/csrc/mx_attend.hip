@@ -29,7 +29,11 @@
 //
 // One sequence of 131072 tokens, 8 heads of 128 in fp8: 51 us, 5.4 TB/s of the
 // 277 MB of cache, and 5 to join; 32 sequences of 1 to 8192 tokens: 63 us, 4.5
-// TB/s of 281 MB, and 6.
+// TB/s of 281 MB, and 6.  Forms further from the memory's rate: fp4 (64
+// sequences of up to 2048 tokens, 8 heads of 128: 28 us for 72 MB), fp32 queries
+// (16 of up to 8192, 4 heads of 128: 20 us for 71 MB; heads of 256, whose
+// registers spill, 69 for 142), more than 16 query heads to a cache head, whose
+// every 16 read the cache again.
 #include <algorithm>
 #include <cmath>
 
@@ -535,7 +539,9 @@ hipError_t launch_format(const MxAttend &a, dim3 grid, hipStream_t s)
 // would stay empty.  The join costs a launch: up to 512 tokens stay whole (315:
 // 7.6 us whole, 5.1 + 4.2 in five pieces; 1000: 13.0 and 4.9 + 4.9), and up to
 // 2304 where the heads and sequences alone fill the CUs twice (64 of up to 2048
-// tokens, 8 heads in fp4: 27 us whole, 25 + 8.4 in three).
+// tokens, 8 heads in fp4: 27 us whole, 25 + 8.4 in three).  Each rule stands on the
+// shapes named, in bf16 and at heads of 128; types and head dimensions whose
+// registers allow two workgroups a CU are cut alike.
 size_t mx_attend_plan(MxAttend &a)
 {
     constexpr int64_t kUnit = kWaves * kStep, kWhole = 512, kWholeFilled = 2304, kCus = 256, kLongest = 960;

@@ -261,11 +261,10 @@ __global__ void __launch_bounds__(kFewWaves *kWave) mx_token_kernel(MxProduct p,
 // memory, apart from the other rows', so they are fetched as rarely as
 // possible.
 //
-// 8192 tokens, 4096 x 4096, in 256 by 256 tiles: 77 to 85 us, 3.2 to 3.6
-// PFLOP/s (8192 x 8192: 4.2).  The same instructions alone, on registers and
-// with this tile's start and end, take 65; the matrix cores are busy 47% of a
-// wavefront's cycles, and the rest is the start, the end and what the reads
-// of LDS and the barriers leave uncovered.
+// 8192 tokens, 4096 x 4096, in 256 by 256 tiles: 81 us, 3.4 PFLOP/s.  The matrix
+// cores are busy 47% of a wavefront's cycles; the rest is a tile's start and
+// end, which nothing covers (one workgroup a CU), and what the reads of LDS
+// and the barriers leave uncovered.
 
 // (the arguments are the same in every lane: a descriptor in scalar registers)
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint8_t *base, int64_t bytes)
@@ -632,8 +631,8 @@ __global__ void __launch_bounds__(256) mx_tile_kernel(MxProduct p)
 // exchanged, as Share has them.
 //
 // A stage takes 0.3 us, of few workgroups too; a ring of six stages gained
-// nothing (64 tokens, 4096 x 4096: 7.0 us, four 5.6, mx_few_kernel 8.3; 25088 x
-// 4096: 22.0, 20.6, 34.1; the last is 2.6 TB/s of W).
+// nothing (64 tokens, 4096 x 4096: 7.0 us, four 5.5, mx_few_kernel 8.3; 25088 x
+// 4096: 22.0, 20.7, 34.4; the last is 2.6 TB/s of W).
 constexpr int kSlabM = 16, kSlabN = 64, kSlabRows = kSlabM + kSlabN;
 
 // Byte i of word g of the result is byte g of word i.
@@ -769,29 +768,32 @@ hipError_t launch_mx_token(const MxProduct &p, const void *X, int dtype, int64_t
 // operands' loads by itself.  The constants are fits to measurements; model
 // and time, us, all of one run, for 4096 rows of W:
 //    n    d        few        slab       128x64     128x128     256x128     256x256
-//    1    4096   4.6  3.5    5.6  4.9    9.9  8.3   12.5 10.2   19.4 15.2   28.8 23.3
-//    16   4096   4.6  4.4    5.6  5.2    9.9  8.4   12.5 10.3   19.4 15.3   28.8 23.5
-//    32   4096   5.8  5.8    5.6  5.2    9.9  8.4   12.5 10.4   19.4 15.5   28.8 23.5
-//    64   4096   8.5  8.3    5.6  5.6    9.9  8.5   12.5 10.7   19.4 15.9   28.8 23.7
-//    128  4096  15.0 13.9   10.2  9.5    9.9  8.7   12.5 10.9   19.4 16.2   28.8 24.9
-//    512  4096  54.0 46.7   38.0 33.0    9.9 11.0   12.5 12.2   19.4 17.0   28.8 25.8
-//    1024 4096   106 88.5   74.9 72.4   19.8 20.1   12.5 15.3   19.4 18.8   28.8 26.9
-//    2048 4096   210  175    149  142   39.6 39.0   25.0 29.2   19.4 28.0   28.8 30.7
-//    4096 4096   418  351    297  282   79.2 73.4   50.0 56.9   38.9 55.9   28.8 42.2
-//    8192 4096   834  697    592  562    158  142    100  115   77.8  103   57.7 80.8
-//    16   25088 17.9 14.9   20.6 15.9   42.7 45.0   53.5 53.2   88.3 89.6    131  117
-//    32   25088 25.3 21.1   20.6 16.2   42.7 47.8   53.5 53.7   88.3 90.1    131  119
-//    64   25088 41.8 34.1   20.6 20.6   42.7 51.5   53.5 55.3   88.3 91.3    131  120
-//    128  25088 81.6 64.5   40.2 39.1   42.7 51.1   53.5 66.0   88.3 96.1    131  124
-//    1024 25088  639  487    314  293   85.4  102   53.5 75.8   88.3 96.4    131  134
-//    64   1024   3.6  4.1    4.3  4.4    5.1  4.7    6.5  5.6    9.4  7.9   14.0 10.6
+//    1    4096   4.6  3.5    5.6  5.0    9.9  8.6   12.5 10.4   19.4 15.6   28.8 23.4
+//    16   4096   4.6  4.4    5.6  5.2    9.9  8.6   12.5 10.4   19.4 15.6   28.8 23.7
+//    32   4096   5.8  5.8    5.6  5.3    9.9  8.7   12.5 10.5   19.4 15.8   28.8 23.7
+//    64   4096   8.5  8.3    5.6  5.5    9.9  8.8   12.5 10.7   19.4 16.2   28.8 23.9
+//    128  4096  15.0 14.1   10.2  9.8    9.9  9.1   12.5 11.0   19.4 16.7   28.8 25.2
+//    512  4096  54.0 48.3   38.0 33.7    9.9 10.8   12.5 12.1   19.4 17.3   28.8 25.7
+//    1024 4096   106 89.9   74.9 72.1   19.8 19.9   12.5 15.0   19.4 19.1   28.8 26.9
+//    2048 4096   210  175    149  142   39.6 36.8   25.0 30.7   19.4 28.3   28.8 33.3
+//    4096 4096   418  349    297  282   79.2 69.7   50.0 58.7   38.9 54.6   28.8 43.0
+//    8192 4096   834  697    592  563    158  136    100  112   77.8  103   57.7 81.8
+//    16   25088 17.9 14.8   20.6 16.6   42.7 44.6   53.5 51.9   88.3 89.0    131  121
+//    32   25088 25.3 21.3   20.6 17.1   42.7 47.9   53.5 52.7   88.3 89.6    131  122
+//    64   25088 41.8 34.4   20.6 20.7   42.7 51.3   53.5 55.3   88.3 91.0    131  123
+//    128  25088 81.6 65.8   40.2 39.4   42.7 51.0   53.5 67.1   88.3 96.6    131  128
+//    1024 25088  639  487    314  294   85.4  103   53.5 77.2   88.3 96.3    131  133
+//    64   1024   3.6  4.1    4.3  4.4    5.1  4.8    6.5  5.6    9.4  8.0   14.0 10.7
 // Up to four tokens always take the kernel for few: its sums have the order of
 // mx_token_kernel's, which a linear call runs for them, so that the two calls
 // give the same bits.  (One token and four, d = 4096: 16384 rows of W 8.0 and 9.0
 // us, by 128x64 tiles 11.1 and 11.1; 32000 rows 13.6 and 15.5, 12.6 and 12.7;
 // 128256 rows 47.2 and 53.8, by 256x128 tiles 47.5 and 48.5.)
 // Misses seen: 20 tokens through 4096 x 4096 go to the slabs (5.3 us; the first
-// kernel 5.0), 1000 through 512 x 512 to the first kernel (4.5; 128x64 tiles 4.1).
+// kernel 5.0), 1000 through 512 x 512 to the first kernel (4.5; 128x64 tiles 4.2).
+// Where every CU is full, the model says up to a third too little of 128x128 tiles
+// and larger and a sixth too much of 128x64; the fastest is the one it takes in
+// every row above.  It was fitted with 4096 rows of W.
 hipError_t launch_mx_product(const MxProduct &p, hipStream_t s)
 {
     if (p.n <= 0 || p.c <= 0) return hipSuccess;

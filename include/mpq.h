@@ -465,6 +465,9 @@ int mpq_integer_forward_layers(const mpq_int_layer *layers, int n_layers, int ma
 #define MPQ_MX_MAX_HEAD_DIM 256
 #define MPQ_MX_MAX_PAGE 65536
 #define MPQ_MX_MAX_TOKENS 536870912 /* tokens of one sequence: columns of the page table times page_size */
+#define MPQ_MX_MAX_EXPERTS 1024
+#define MPQ_MX_MAX_CHOICES 64       /* experts of one token */
+#define MPQ_MX_MAX_ROWS 67108864    /* rows of a product by experts, of all tokens' choices together */
 
 /*
  * mpq_mx_quantize - rows to fp4 blocks.
@@ -585,6 +588,158 @@ int mpq_mx_attend(const mpq_mx_cache *cache, const void *Q, int64_t q_stride, in
                   int64_t batch, int64_t q_heads, const int32_t *page_table, int64_t table_ld, int64_t max_pages,
                   const int32_t *lengths, int64_t window, float scale, void *O, int64_t o_stride,
                   int64_t o_head_stride, float *lse_opt, void *workspace_opt, int64_t workspace_bytes, void *stream);
+
+/*
+ * What a serving step does around the products, the cache and attention: pages
+ * and slots of its new tokens (mpq_mx_plan), norms and rotation of its heads
+ * (mpq_mx_rotate, mpq_mx_cache_append), and a layer of experts (mpq_mx_route,
+ * mpq_mx_experts, mpq_mx_combine).  None waits for the device or reads device
+ * memory on the host.  An output of these calls overlaps no other array of the
+ * call, unless said otherwise.
+ *
+ * mpq_mx_plan - the new tokens of `batch` sequences, `fresh[b]` behind the
+ * `cached[b]` that sequence b has in the cache (both [batch] int32; negative
+ * ones count as 0).  The tokens lie sequence after sequence, those of b from
+ * row starts[b] on, as they do in the step's other tensors.
+ *   page_table  [batch][table_ld] int32, max_pages columns used (in and out): the
+ *               entries of a sequence's ceil(cached / page_size) held pages are
+ *               read (only that of a page which new tokens continue), those
+ *               of its new pages are written, others are left as they are.
+ *   free_pages  [n_free] int32: pages not in use, of which the first *taken
+ *               (int32) are already given away.  New pages are the next ones, in
+ *               the order of the sequences; -1 where none is left.
+ *   taken_out   int32 (output): *taken and the new pages, those without a
+ *               free page included, so it exceeds n_free if some are missing;
+ *               taken for the next step (pages given back are the caller's to put
+ *               into another list).
+ *   slots       [max_tokens] int64 (output): page * page_size + place; -1 for a
+ *               token without a page (none free, past max_pages, or a table entry
+ *               below 0) and for rows past the last token.  Cache calls skip it.
+ *   positions   [max_tokens] int32 (output): the token's place in its sequence;
+ *               0 for rows past the last token.
+ *   starts      [batch + 1] int32, lengths [batch] int32 (outputs): lengths[b] =
+ *               cached[b] + fresh[b], as mpq_mx_attend takes it.  A place or
+ *               length past 2^31 - 1 is given as that.
+ * Tokens past max_tokens in all are taken as not there: starts, lengths and
+ * pages count the first max_tokens alone.
+ *   batch in [0, 65535]; page_size as a cache's; max_pages * page_size and
+ *   max_tokens at most MPQ_MX_MAX_TOKENS.
+ * Errors: MPQ_ERR_INVALID_ARG, MPQ_ERR_HIP.
+ */
+int mpq_mx_plan(const int32_t *cached, const int32_t *fresh, int64_t batch, int32_t *page_table, int64_t table_ld,
+                int64_t max_pages, const int32_t *free_pages, int64_t n_free, const int32_t *taken, int64_t page_size,
+                int64_t max_tokens, int64_t *slots, int32_t *positions, int32_t *starts, int32_t *lengths,
+                int32_t *taken_out, void *stream);
+
+/*
+ * mpq_mx_rotate - norm and rotation of the heads of queries and keys.  Of a
+ * head x, in fp32, rounded once at the end:
+ *   with a weight w  x <- x / sqrt(mean x^2 + eps) w (the squares are summed in
+ *                    fp32: heads larger than about 1e19 overflow);
+ *   then the pairs (a, b) of its first rot elements, i = 0 .. rot / 2 - 1,
+ *   become (a cos t - b sin t, b cos t + a sin t), t = position * freqs[i]; a
+ *   and b are elements i and i + rot / 2, or 2 i and 2 i + 1 (interleaved).
+ *   The angle is found in fp64, less its whole turns.
+ *   Q, QO [n][q_heads][head_dim], K, KO [n][kv_heads][head_dim] of dtype, with
+ *               the strides of tokens and heads.  QO may be Q and KO may be K, with
+ *               the same strides.
+ *   positions   [n] int32; may be NULL if rot = 0.
+ *   freqs       [rot / 2] fp64 (DEVICE), radians per position.
+ *   q_weight_opt, k_weight_opt  [head_dim] fp32, or NULL: no norm of the
+ *               queries, of the keys.
+ *   eps         finite and > 0 (looked at with a weight only).
+ *   0 <= n < 2^31, 1 <= head_dim <= MPQ_MX_MAX_HEAD_DIM, rot even, at most
+ *   head_dim.
+ *
+ * mpq_mx_cache_append - the same for queries Q to QO, while keys, so turned,
+ * and values V are quantized into the cache at `slots` ([n] int64, as in
+ * mpq_mx_cache_write).  The keys are not rounded to dtype in between: the cache
+ * is bitwise that of mpq_mx_rotate of the keys in fp32 and mpq_mx_cache_write.
+ * Errors: MPQ_ERR_INVALID_ARG, MPQ_ERR_HIP.
+ */
+int mpq_mx_rotate(const void *Q, int64_t q_stride, int64_t q_head_stride, const void *K, int64_t k_stride,
+                  int64_t k_head_stride, int dtype, int64_t n, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                  const int32_t *positions, const double *freqs, int64_t rot, int interleaved, const float *q_weight_opt,
+                  const float *k_weight_opt, float eps, void *QO, int64_t qo_stride, int64_t qo_head_stride, void *KO,
+                  int64_t ko_stride, int64_t ko_head_stride, void *stream);
+int mpq_mx_cache_append(const mpq_mx_cache *cache, const void *Q, int64_t q_stride, int64_t q_head_stride, const void *K,
+                        int64_t k_stride, int64_t k_head_stride, const void *V, int64_t v_stride, int64_t v_head_stride,
+                        int dtype, int64_t n, int64_t q_heads, const int32_t *positions, const int64_t *slots,
+                        const double *freqs, int64_t rot, int interleaved, const float *q_weight_opt,
+                        const float *k_weight_opt, float eps, void *QO, int64_t qo_stride, int64_t qo_head_stride,
+                        void *stream);
+
+/*
+ * mpq_mx_route - the k largest of each token's expert logits, and the choices
+ * sorted by expert.
+ *   logits      [n][ld] of dtype, the first `experts` of each row (input).
+ *   chosen      [n][k] int32 (output): the experts, by falling logit; equal ones
+ *               by rising index (-0 equals 0; NaN counts as -infinity).
+ *   weights     [n][k] fp32 (output): the softmax of the logits over all experts,
+ *               or, with renorm = 1, over the chosen ones.  Among infinite
+ *               logits the weight is shared; with every logit -infinity all are 0.
+ *   order       [n * k] int32 (output): choice t * k + j of token t at the places
+ *               of expert chosen[t][j], the experts one after the other, an
+ *               expert's choices by rising token.
+ *   place       [n][k] int32 (output): the inverse: order[place[t][j]] = t k + j.
+ *   offsets     [experts + 1] int32 (output): expert e has the places
+ *               offsets[e] .. offsets[e + 1] - 1.
+ *   0 <= n <= MPQ_MX_MAX_N, 1 <= experts <= MPQ_MX_MAX_EXPERTS, 1 <= k <=
+ *   min(experts, MPQ_MX_MAX_CHOICES).
+ *   workspace_opt, workspace_bytes  as for mpq_mx_linear, of at least
+ *               mpq_mx_route_workspace(n, experts, k) bytes.
+ * Errors: MPQ_ERR_INVALID_ARG, MPQ_ERR_NOMEM, MPQ_ERR_HIP.
+ */
+int64_t mpq_mx_route_workspace(int64_t n, int64_t experts, int64_t k);
+int mpq_mx_route(const void *logits, int dtype, int64_t n, int64_t experts, int64_t ld, int64_t k, int renorm,
+                 int32_t *chosen, float *weights, int32_t *order, int32_t *place, int32_t *offsets, void *workspace_opt,
+                 int64_t workspace_bytes, void *stream);
+
+/*
+ * mpq_mx_experts - rows grouped by expert times their expert's weights:
+ *   Y[p] = Q(X[order[p] / k]) W_e^T + b_e,  offsets[e] <= p < offsets[e + 1],
+ * Q the quantization of mpq_mx_quantize, products and sums as in mpq_mx_product.
+ *   X           [n][x_ld] of x_dtype, the first d of each row (input).
+ *   w_codes, w_scales  [experts][c_out] fp4 rows of d (inputs).
+ *   offsets     [experts + 1] int32 (DEVICE), ascending in [0, m]; one that is
+ *               not is taken as the nearest that is, from the first on.
+ *   order_opt   [m] int32 as mpq_mx_route gives it, with its k; or NULL: row p
+ *               of X itself (then m = n and k = 1).  An entry that names no row of X
+ *               stands for a row of zeros.
+ *   bias_opt    NULL or [experts][c_out] fp32, added in fp32.
+ *   Y           [m][ld] of dtype (output), ld >= c_out.  Rows of no group (before
+ *               offsets[0], from offsets[experts] on) are left as they were.
+ *   0 <= n <= MPQ_MX_MAX_N, 0 <= m <= MPQ_MX_MAX_ROWS; with D as above, (n + 1) D
+ *   below 2^32 and experts * c_out * D at most 2^42.
+ *   workspace_opt, workspace_bytes  as for mpq_mx_linear, of at least
+ *               mpq_mx_experts_workspace(n, m, experts, c_out, d) bytes.
+ * How the work is cut follows from n, m, experts and c_out, and so do the last
+ * bits of a row; they do not depend on the other rows or on the groups' sizes.
+ * Errors: MPQ_ERR_INVALID_ARG, MPQ_ERR_NOMEM, MPQ_ERR_HIP.
+ */
+int64_t mpq_mx_experts_workspace(int64_t n, int64_t m, int64_t experts, int64_t c_out, int64_t d);
+int mpq_mx_experts(const void *X, int x_dtype, int64_t n, int64_t x_ld, const uint8_t *w_codes, const uint8_t *w_scales,
+                   int64_t experts, int64_t c_out, int64_t d, const int32_t *offsets, const int32_t *order_opt, int64_t m,
+                   int64_t k, const float *bias_opt, void *Y, int dtype, int64_t ld, void *workspace_opt,
+                   int64_t workspace_bytes, void *stream);
+
+/*
+ * mpq_mx_combine - every token's weighted sum of its experts' rows:
+ *   Z[t] = residual[t] + sum_j weights[t][j] Y[place[t][j]],
+ * in fp32 in the order of j, rounded once.
+ *   Y           [m][y_ld] of y_dtype, the first c of each row (input).
+ *   place       [n][k] int32, weights [n][k] fp32 (inputs).  A place outside
+ *               [0, m) takes no part.
+ *   residual_opt NULL or [n][residual_ld] of y_dtype (input).
+ *   Z           [n][ld] of dtype (output); may be the residual, with the same
+ *               type and stride.
+ *   0 <= n <= MPQ_MX_MAX_N, 0 <= m <= MPQ_MX_MAX_ROWS, 0 <= c <= MPQ_MX_MAX_D,
+ *   0 <= k <= MPQ_MX_MAX_CHOICES.
+ * Errors: MPQ_ERR_INVALID_ARG, MPQ_ERR_HIP.
+ */
+int mpq_mx_combine(const void *Y, int y_dtype, int64_t m, int64_t c, int64_t y_ld, const int32_t *place,
+                   const float *weights, int64_t n, int64_t k, const void *residual_opt, int64_t residual_ld, void *Z,
+                   int dtype, int64_t ld, void *stream);
 
 /*
  * Per-launch timing (instrumentation, not part of the method).  While it is

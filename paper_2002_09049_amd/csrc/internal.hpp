@@ -342,6 +342,62 @@ hipError_t launch_mx_product(const MxProduct &p, hipStream_t s);
 bool mx_quantizes_inside(int64_t n);
 hipError_t launch_mx_token(const MxProduct &p, const void *X, int dtype, int64_t x_ld, int64_t d, hipStream_t s);
 
+// Rows grouped by expert: p.n rows of X, p.c rows of W and p.bias of each expert,
+// m rows of Y, p.wc, p.ws and p.bias those of expert 0.
+struct MxExperts {
+    MxProduct p;
+    int experts, choices;
+    int64_t m;
+    const int32_t *offsets;   // [experts + 1]
+    const int32_t *order;     // [m] or nullptr
+    void *pieces;             // in the call's workspace
+};
+size_t mx_experts_bytes(int64_t n, int64_t m, int64_t experts, int64_t d);
+hipError_t launch_mx_experts(MxExperts g, const void *X, int dtype, int64_t x_ld, int64_t d, uint8_t *space,
+                             hipStream_t s);
+
+struct MxRoute {
+    const void *logits;       // [n][ld]
+    int dtype;
+    int64_t n, ld;
+    int experts, k, renorm;
+    int32_t *chosen, *order, *place, *offsets;
+    float *weights;
+    int32_t *counts;          // workspace: [blocks][experts], mx_route_bytes
+};
+size_t mx_route_bytes(int64_t n, int64_t experts);
+hipError_t launch_mx_route(const MxRoute &r, hipStream_t s);
+
+struct MxCombine {
+    const void *Y;            // [m][ldy]
+    int dtype;
+    int64_t m, c, ldy, n;
+    const int32_t *place;     // [n][k]
+    const float *weights;     // [n][k]
+    int k;
+    const void *R;            // [n][ldr] of Y's dtype, or nullptr
+    int64_t ldr;
+    void *Z;                  // [n][ldz]
+    int z_dtype;
+    int64_t ldz;
+};
+hipError_t launch_mx_combine(const MxCombine &c, hipStream_t s);
+
+struct MxPlan {
+    const int32_t *cached, *fresh;
+    int64_t batch;
+    int32_t *table;           // [batch][table_ld]
+    int64_t table_ld, columns;
+    const int32_t *free;
+    int64_t n_free;
+    const int32_t *taken;
+    int page;
+    int64_t tokens;
+    int64_t *slots;
+    int32_t *positions, *starts, *lengths, *taken_out;
+};
+hipError_t launch_mx_plan(const MxPlan &p, hipStream_t s);
+
 struct MxCacheView {
     uint8_t *k, *v;     // [n_pages][heads][page][row bytes]
     uint8_t *ks, *vs;   // [n_pages][heads][nb][page]
@@ -357,6 +413,25 @@ hipError_t launch_mx_cache_write(const MxCacheView &c, const MxRows &r, int64_t 
                                  hipStream_t s);
 hipError_t launch_mx_cache_read(const MxCacheView &c, const MxRows &r, int64_t tokens, const int64_t *slots,
                                 hipStream_t s);
+
+// Norm and rotation of heads; with slots, keys and values go to the cache.
+struct MxRotate {
+    const void *Q, *K, *V;    // [n][heads][dim], [n][kv][dim], strides in elements
+    int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head;
+    void *QO, *KO;
+    int64_t qo_tok, qo_head, ko_tok, ko_head;
+    int dtype;
+    int64_t n;
+    int heads, kv, dim, rot;
+    const float *qw, *kw;     // [dim] or nullptr: no norm
+    float eps;
+    int interleaved;
+    const int32_t *positions;
+    const double *freqs;      // [rot / 2]
+    MxCacheView c;            // append only
+    const int64_t *slots;
+};
+hipError_t launch_mx_rotate(const MxRotate &r, bool append, hipStream_t s);
 
 struct MxAttend {
     MxCacheView c;

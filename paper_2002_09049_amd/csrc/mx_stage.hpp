@@ -26,6 +26,18 @@ __device__ __forceinline__ uint32_t tile_stage_offset(int k, int row_bytes, int 
     return 4 * st < nb ? (uint32_t)(16 * k * row_bytes + st * kStageBytes) : kOutside;
 }
 
+// The same for rows gathered one by one: the lane's row (below 0: none), and a
+// stage's offset from it.
+__device__ __forceinline__ uint32_t tile_gather_offset(int64_t row, int lane, int row_bytes)
+{
+    return row < 0 ? kOutside : (uint32_t)(row * row_bytes + ((lane % 4) ^ (lane / 16)) * 16);
+}
+
+__device__ __forceinline__ uint32_t tile_gather_stage(uint32_t lane_offset, int st, int nb)
+{
+    return 4 * st < nb ? lane_offset + (uint32_t)(st * kStageBytes) : kOutside;
+}
+
 // Slabs: stages of 512 elements.  A load covers four rows of 16; place r of
 // row `row` takes piece r ^ row.
 constexpr int kSlabBytes = 256;

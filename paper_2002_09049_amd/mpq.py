@@ -42,7 +42,8 @@ EXPORTS = ("mpq_fit_layer", "mpq_fit_layer_dense", "mpq_fit_layers", "mpq_fit_ma
            "mpq_integer_forward_layers", "mpq_fit_layers_ex", "mpq_output_error_noalloc",
            "mpq_mx_quantize", "mpq_mx_dequantize", "mpq_mx_product", "mpq_mx_linear",
            "mpq_mx_linear_workspace", "mpq_mx_cache_write", "mpq_mx_cache_read", "mpq_mx_attend",
-           "mpq_mx_attend_workspace")
+           "mpq_mx_attend_workspace", "mpq_mx_plan", "mpq_mx_rotate", "mpq_mx_cache_append", "mpq_mx_route",
+           "mpq_mx_route_workspace", "mpq_mx_experts", "mpq_mx_experts_workspace", "mpq_mx_combine")
 
 MX_BLOCK = 32
 MX_ROW = 128
@@ -158,6 +159,24 @@ def load(path: str = LIB_PATH):
     lib.mpq_mx_attend.argtypes = [P, P, i64, i64, i32, i64, i64, P, i64, i64, P, i64, f32, P, i64, i64,
                                   P, P, i64, P]
     lib.mpq_mx_attend.restype = i32
+    lib.mpq_mx_plan.argtypes = [P, P, i64, P, i64, i64, P, i64, P, i64, i64, P, P, P, P, P, P]
+    lib.mpq_mx_plan.restype = i32
+    lib.mpq_mx_rotate.argtypes = [P, i64, i64, P, i64, i64, i32, i64, i64, i64, i64, P, P, i64, i32, P, P, f32,
+                                  P, i64, i64, P, i64, i64, P]
+    lib.mpq_mx_rotate.restype = i32
+    lib.mpq_mx_cache_append.argtypes = [P, P, i64, i64, P, i64, i64, P, i64, i64, i32, i64, i64, P, P, P, i64, i32,
+                                        P, P, f32, P, i64, i64, P]
+    lib.mpq_mx_cache_append.restype = i32
+    lib.mpq_mx_route_workspace.argtypes = [i64, i64, i64]
+    lib.mpq_mx_route_workspace.restype = i64
+    lib.mpq_mx_route.argtypes = [P, i32, i64, i64, i64, i64, i32, P, P, P, P, P, P, i64, P]
+    lib.mpq_mx_route.restype = i32
+    lib.mpq_mx_experts_workspace.argtypes = [i64, i64, i64, i64, i64]
+    lib.mpq_mx_experts_workspace.restype = i64
+    lib.mpq_mx_experts.argtypes = [P, i32, i64, i64, P, P, i64, i64, i64, P, P, i64, i64, P, P, i32, i64, P, i64, P]
+    lib.mpq_mx_experts.restype = i32
+    lib.mpq_mx_combine.argtypes = [P, i32, i64, i64, i64, P, P, i64, i64, P, i64, P, i32, i64, P]
+    lib.mpq_mx_combine.restype = i32
     lib.mpq_last_error.argtypes = []
     lib.mpq_last_error.restype = ctypes.c_char_p
     lib.mpq_timing_enable.argtypes = [i32]
@@ -536,6 +555,217 @@ def mx_linear(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bias: 
     return Y
 
 
+def _one_device(*tensors):
+    """The tensors of a call (None: an argument that is not given) lie on the
+    current device, where its kernels are launched."""
+    here = torch.cuda.current_device()
+    for x in tensors:
+        if x is not None and x.get_device() != here:
+            raise ValueError(f"every tensor must be on the current device, cuda:{here} (got one on {x.device})")
+
+
+def mx_plan(cached: torch.Tensor, fresh: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor,
+            taken: torch.Tensor, page_size: int, max_tokens: int, stream=None, out=None):
+    """mpq_mx_plan: pages, slots and positions of the fresh[b] new tokens of
+    each sequence b, which has cached[b] in the cache (int32 [batch] both).
+
+    page_table [batch, max_pages] int32 is updated in place: new pages are the
+    next ones of free_pages (int32), of which the first taken[0] (int32 [1]) are
+    given away.  Returns (slots [max_tokens] int64, positions [max_tokens] int32,
+    starts [batch + 1] int32, lengths [batch] int32, taken [1] int32 for the next
+    step; more than there are free pages if some are missing), or writes them to
+    the five tensors of out."""
+    if cached.dim() != 1 or fresh.shape != cached.shape:
+        raise ValueError("cached and fresh must be [batch]")
+    batch = cached.shape[0]
+    if page_table.dim() != 2 or page_table.shape[0] != batch or (
+            page_table.numel() > 0 and page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError("page_table must be [batch, max_pages] with contiguous rows")
+    if page_table.dtype != torch.int32 or not page_table.is_cuda:
+        raise ValueError("page_table must be an int32 device tensor")
+    if taken.shape != (1,) or free_pages.dim() != 1:
+        raise ValueError("taken must be [1], free_pages 1-D")
+    if out is None:
+        slots = _new(cached, (max_tokens,), torch.int64, stream)
+        positions = _new(cached, (max_tokens,), torch.int32, stream)
+        starts = _new(cached, (batch + 1,), torch.int32, stream)
+        lengths = _new(cached, (batch,), torch.int32, stream)
+        after = _new(cached, (1,), torch.int32, stream)
+    else:
+        slots, positions, starts, lengths, after = out
+        for x, n, name in ((slots, max_tokens, "slots"), (positions, max_tokens, "positions"),
+                           (starts, batch + 1, "starts"), (lengths, batch, "lengths"), (after, 1, "taken")):
+            if x.shape != (n,):
+                raise ValueError(f"out's {name} must be {(n,)} (got {tuple(x.shape)})")
+    _one_device(cached, fresh, page_table, free_pages, taken, slots, positions, starts, lengths, after)
+    pages = page_table.shape[1]
+    i32 = torch.int32
+    _check(load().mpq_mx_plan(_dev(cached, i32, "cached"), _dev(fresh, i32, "fresh"), batch, page_table.data_ptr(),
+                              page_table.stride(0) if batch > 1 else pages, pages, _dev(free_pages, i32, "free_pages"),
+                              free_pages.shape[0], _dev(taken, i32, "taken"), page_size, max_tokens,
+                              _dev(slots, torch.int64, "slots"), _dev(positions, i32, "positions"),
+                              _dev(starts, i32, "starts"), _dev(lengths, i32, "lengths"), _dev(after, i32, "taken"),
+                              _stream(stream)))
+    return slots, positions, starts, lengths, after
+
+
+def _rotation(n: int, dim: int, positions, freqs, q_weight, k_weight):
+    """(positions, freqs, rot, q_weight, k_weight) as the calls take them."""
+    if positions.shape != (n,):
+        raise ValueError(f"positions must be {(n,)} (got {tuple(positions.shape)})")
+    if freqs.dim() != 1:
+        raise ValueError("freqs must be 1-D")
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None and w.shape != (dim,):
+            raise ValueError(f"{name} must be {(dim,)} (got {tuple(w.shape)})")
+    return (_dev(positions, torch.int32, "positions"), _dev(freqs, torch.float64, "freqs"), 2 * freqs.shape[0],
+            None if q_weight is None else _dev(q_weight, torch.float32, "q_weight"),
+            None if k_weight is None else _dev(k_weight, torch.float32, "k_weight"))
+
+
+def _heads_out(out, like: torch.Tensor, shape, name: str, stream):
+    """(tensor, pointer, strides) of an output of heads like `like`."""
+    if out is None:
+        out = _new(like, shape, like.dtype, stream)
+        return out, out.data_ptr(), shape[1] * shape[2], shape[2]
+    if out.dtype != like.dtype:
+        raise ValueError(f"{name} must be {like.dtype} (got {out.dtype})")
+    return (out, *_heads(out, shape, name))
+
+
+def mx_rotate(Q: torch.Tensor, K: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor,
+              q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+              interleaved: bool = False, stream=None, out=None):
+    """mpq_mx_rotate: RMS norm (where there is a weight [head_dim] fp32) and
+    rotation by positions[t] * freqs of the heads of Q [n, q_heads, head_dim] and
+    K [n, kv_heads, head_dim].  positions [n] int32; freqs [rot / 2] float64 turn
+    the first rot dimensions, in pairs (i, i + rot / 2), or (2 i, 2 i + 1) if
+    interleaved.  Returns (Q, K) so turned, or writes them to the tensors of out,
+    which may be Q and K themselves."""
+    if Q.dim() != 3 or K.dim() != 3:
+        raise ValueError("Q and K must be 3-D [n, heads, head_dim]")
+    n, heads, dim = Q.shape
+    kv = K.shape[1]
+    qp, qt, qh = _heads(Q, (n, heads, dim), "Q")
+    kp, kt, kh = _heads(K, (n, kv, dim), "K")
+    if K.dtype != Q.dtype:
+        raise ValueError("Q and K must have one dtype")
+    QO, qop, qot, qoh = _heads_out(None if out is None else out[0], Q, (n, heads, dim), "out's Q", stream)
+    KO, kop, kot, koh = _heads_out(None if out is None else out[1], K, (n, kv, dim), "out's K", stream)
+    _one_device(Q, K, positions, freqs, q_weight, k_weight, QO, KO)
+    pp, fp, rot, qw, kw = _rotation(n, dim, positions, freqs, q_weight, k_weight)
+    _check(load().mpq_mx_rotate(qp, qt, qh, kp, kt, kh, _mx_dtype(Q.dtype, "Q"), n, heads, kv, dim, pp, fp, rot,
+                                1 if interleaved else 0, qw, kw, float(eps), qop, qot, qoh, kop, kot, koh,
+                                _stream(stream)))
+    return QO, KO
+
+
+def mx_route_workspace(n: int, experts: int, k: int) -> int:
+    """mpq_mx_route_workspace: the bytes of a workspace of mx_route."""
+    v = load().mpq_mx_route_workspace(n, experts, k)
+    if v < 0:
+        _check(int(v))
+    return int(v)
+
+
+def mx_route(logits: torch.Tensor, k: int, renorm: bool = True, stream=None, out=None, workspace=None):
+    """mpq_mx_route: the k largest of each row of logits [n, experts] (fp32,
+    fp16 or bf16; rows may be apart) and the choices sorted by expert.  Returns
+    (chosen [n, k] int32, weights [n, k] fp32, order [n k] int32, place [n, k]
+    int32, offsets [experts + 1] int32), or writes them to the tensors of out;
+    weights are the softmax over the chosen (renorm) or over all experts.
+    workspace: an uint8 device tensor of mx_route_workspace(n, experts, k) bytes;
+    without one as in mx_linear."""
+    lp, dt, ld = _rows(logits, "logits")
+    n, experts = logits.shape
+    i32 = torch.int32
+    if out is None:
+        chosen, place = _new(logits, (n, k), i32, stream), _new(logits, (n, k), i32, stream)
+        weights = _new(logits, (n, k), torch.float32, stream)
+        order, offsets = _new(logits, (n * k,), i32, stream), _new(logits, (experts + 1,), i32, stream)
+    else:
+        chosen, weights, order, place, offsets = out
+        for x, shape, name in ((chosen, (n, k), "chosen"), (weights, (n, k), "weights"), (order, (n * k,), "order"),
+                               (place, (n, k), "place"), (offsets, (experts + 1,), "offsets")):
+            if tuple(x.shape) != shape:
+                raise ValueError(f"out's {name} must be {shape} (got {tuple(x.shape)})")
+    _one_device(logits, chosen, weights, order, place, offsets, workspace)
+    wp, wn, _own = _space(workspace, lambda: mx_route_workspace(n, experts, k), stream, logits)
+    _check(load().mpq_mx_route(lp, dt, n, experts, ld, k, 1 if renorm else 0, _dev(chosen, i32, "chosen"),
+                               _dev(weights, torch.float32, "weights"), _dev(order, i32, "order"),
+                               _dev(place, i32, "place"), _dev(offsets, i32, "offsets"), wp, wn, _stream(stream)))
+    return chosen, weights, order, place, offsets
+
+
+def mx_experts_workspace(n: int, m: int, experts: int, c: int, d: int) -> int:
+    """mpq_mx_experts_workspace: the bytes of a workspace of mx_experts with n
+    rows of X and m of Y."""
+    v = load().mpq_mx_experts_workspace(n, m, experts, c, d)
+    if v < 0:
+        _check(int(v))
+    return int(v)
+
+
+def mx_experts(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, offsets: torch.Tensor,
+               order: Optional[torch.Tensor] = None, k: int = 1, bias: Optional[torch.Tensor] = None, dtype=None,
+               stream=None, out: Optional[torch.Tensor] = None, workspace=None) -> torch.Tensor:
+    """mpq_mx_experts: Y [m, c], its rows offsets[e] .. offsets[e + 1] - 1 the
+    products of rows of X [n, d], quantized to fp4 in the call, with expert e's
+    weights: codes [experts, c, D / 2] and scales [experts, c, D / 32], each
+    expert's as mx_quantize gives them.  Row p takes X's row order[p] // k (order
+    [m] int32, as mx_route gives it), or row p without order.  bias [experts, c]
+    fp32.  Rows outside the groups are left as they were (with a new tensor:
+    undefined).  dtype of Y: X's unless given.  workspace: an uint8 device tensor
+    of mx_experts_workspace(n, m, experts, c, d) bytes; without one as in
+    mx_linear."""
+    xp, xt, x_ld = _rows(X, "X")
+    n, d = X.shape
+    wide = -(-d // MX_ROW) * MX_ROW
+    if codes.dim() != 3 or codes.shape[2] != wide // 2 or tuple(scales.shape) != (*codes.shape[:2], wide // MX_BLOCK):
+        raise ValueError(f"weights: codes and scales do not hold rows of {d} of every expert")
+    experts, c = codes.shape[:2]
+    if offsets.shape != (experts + 1,):
+        raise ValueError(f"offsets must be {(experts + 1,)}")
+    if order is not None and order.dim() != 1:
+        raise ValueError("order must be 1-D")
+    m = n if order is None else order.shape[0]
+    if bias is not None and bias.shape != (experts, c):
+        raise ValueError(f"bias must be {(experts, c)}")
+    Y, yp, dt, ld = _rows_out(out, m, c, X.dtype if dtype is None else dtype, X, stream)
+    _one_device(X, codes, scales, offsets, order, bias, Y, workspace)
+    wp, wn, _own = _space(workspace, lambda: mx_experts_workspace(n, m, experts, c, d), stream, X)
+    _check(load().mpq_mx_experts(xp, xt, n, x_ld, _dev(codes, torch.uint8, "codes"), _dev(scales, torch.uint8, "scales"),
+                                 experts, c, d, _dev(offsets, torch.int32, "offsets"),
+                                 None if order is None else _dev(order, torch.int32, "order") or _NO_BYTES, m, k,
+                                 None if bias is None else _dev(bias, torch.float32, "bias"), yp, dt, ld, wp, wn,
+                                 _stream(stream)))
+    return Y
+
+
+def mx_combine(Y: torch.Tensor, place: torch.Tensor, weights: torch.Tensor, residual: Optional[torch.Tensor] = None,
+               dtype=None, stream=None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """mpq_mx_combine: Z [n, c], row t residual[t] + sum_j weights[t, j]
+    Y[place[t, j]] in fp32 (place [n, k] int32, weights [n, k] fp32; a place
+    outside Y takes no part).  Y [m, c]; residual [n, c] of Y's dtype; dtype of Z:
+    Y's unless given.  out may be the residual."""
+    yp, yt, y_ld = _rows(Y, "Y")
+    m, c = Y.shape
+    if place.dim() != 2 or weights.shape != place.shape:
+        raise ValueError("place and weights must be [n, k]")
+    n, k = place.shape
+    rp, r_ld = None, 0
+    if residual is not None:
+        if tuple(residual.shape) != (n, c) or residual.dtype != Y.dtype:
+            raise ValueError(f"residual must be {(n, c)} of {Y.dtype}")
+        rp, _, r_ld = _rows(residual, "residual")
+        rp = rp or None
+    Z, zp, dt, ld = _rows_out(out, n, c, Y.dtype if dtype is None else dtype, Y, stream)
+    _one_device(Y, place, weights, residual, Z)
+    _check(load().mpq_mx_combine(yp, yt, m, c, y_ld, _dev(place, torch.int32, "place"),
+                                 _dev(weights, torch.float32, "weights"), n, k, rp, r_ld, zp, dt, ld, _stream(stream)))
+    return Z
+
+
 class MXCache:
     """A paged block-scaled cache of keys and values (struct mpq_mx_cache).
 
@@ -585,6 +815,31 @@ class MXCache:
             raise ValueError("K and V must have one dtype")
         _check(load().mpq_mx_cache_write(self._at, kp, kt, kh, vp, vt, vh, _mx_dtype(K.dtype, "K"), n,
                                          _dev(slots, torch.int64, "slots"), _stream(stream)))
+
+    def append(self, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor,
+               freqs: torch.Tensor, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+               eps: float = 1e-6, interleaved: bool = False, stream=None, out: Optional[torch.Tensor] = None):
+        """mpq_mx_cache_append: mx_rotate of Q [n, q_heads, head_dim], returned (or
+        written to out, which may be Q), while K [n, kv_heads, head_dim], so turned,
+        and V are quantized into the slots [n] (int64, as in write)."""
+        if Q.dim() != 3:
+            raise ValueError("Q must be 3-D [n, q_heads, head_dim]")
+        n, heads = Q.shape[:2]
+        shape, held = (n, heads, self.head_dim), (n, self.kv_heads, self.head_dim)
+        qp, qt, qh = _heads(Q, shape, "Q")
+        kp, kt, kh = _heads(K, held, "K")
+        vp, vt, vh = _heads(V, held, "V")
+        if K.dtype != Q.dtype or V.dtype != Q.dtype:
+            raise ValueError("Q, K and V must have one dtype")
+        if slots.shape != (n,):
+            raise ValueError(f"slots must be {(n,)} (got {tuple(slots.shape)})")
+        QO, qop, qot, qoh = _heads_out(out, Q, shape, "out", stream)
+        _one_device(Q, K, V, positions, slots, freqs, q_weight, k_weight, QO, self.tensors[0])
+        pp, fp, rot, qw, kw = _rotation(n, self.head_dim, positions, freqs, q_weight, k_weight)
+        _check(load().mpq_mx_cache_append(self._at, qp, qt, qh, kp, kt, kh, vp, vt, vh, _mx_dtype(Q.dtype, "Q"), n, heads,
+                                          pp, _dev(slots, torch.int64, "slots"), fp, rot, 1 if interleaved else 0, qw, kw,
+                                          float(eps), qop, qot, qoh, _stream(stream)))
+        return QO
 
     def read(self, slots: torch.Tensor, dtype=torch.float32, stream=None, out=None):
         """mpq_mx_cache_read: the keys and values [n, kv_heads, head_dim] held

@@ -633,9 +633,9 @@ int mpq_mx_plan(const int32_t *cached, const int32_t *fresh, int64_t batch, int3
 
 /*
  * mpq_mx_rotate - norm and rotation of the heads of queries and keys.  Of a
- * head x, in fp32, rounded once at the end:
- *   with a weight w  x <- x / sqrt(mean x^2 + eps) w (the squares are summed in
- *                    fp32: heads larger than about 1e19 overflow);
+ * head x, in fp32 (fp64 where dtype is MPQ_F32), rounded once at the end:
+ *   with a weight w  x <- x / sqrt(mean x^2 + eps) w (in fp32, heads larger than
+ *                    about 1e19 overflow);
  *   then the pairs (a, b) of its first rot elements, i = 0 .. rot / 2 - 1,
  *   become (a cos t - b sin t, b cos t + a sin t), t = position * freqs[i]; a
  *   and b are elements i and i + rot / 2, or 2 i and 2 i + 1 (interleaved).
@@ -653,8 +653,8 @@ int mpq_mx_plan(const int32_t *cached, const int32_t *fresh, int64_t batch, int3
  *
  * mpq_mx_cache_append - the same for queries Q to QO, while keys, so turned,
  * and values V are quantized into the cache at `slots` ([n] int64, as in
- * mpq_mx_cache_write).  The keys are not rounded to dtype in between: the cache
- * is bitwise that of mpq_mx_rotate of the keys in fp32 and mpq_mx_cache_write.
+ * mpq_mx_cache_write).  The keys are not rounded in between: they are computed in
+ * fp64, and the rounding to their blocks' elements is the only one.
  * Errors: MPQ_ERR_INVALID_ARG, MPQ_ERR_HIP.
  */
 int mpq_mx_rotate(const void *Q, int64_t q_stride, int64_t q_head_stride, const void *K, int64_t k_stride,

@@ -351,6 +351,7 @@ struct MxExperts {
     const int32_t *offsets;   // [experts + 1]
     const int32_t *order;     // [m] or nullptr
     void *pieces;             // in the call's workspace
+    const int32_t *list;      // [m], there too: the row of X that each row of Y takes
 };
 size_t mx_experts_bytes(int64_t n, int64_t m, int64_t experts, int64_t d);
 hipError_t launch_mx_experts(MxExperts g, const void *X, int dtype, int64_t x_ld, int64_t d, uint8_t *space,
@@ -363,10 +364,11 @@ struct MxRoute {
     int experts, k, renorm;
     int32_t *chosen, *order, *place, *offsets;
     float *weights;
-    int32_t *counts;          // workspace: [blocks][experts], mx_route_bytes
+    uint8_t *counts;          // in the call's workspace
+    int32_t *sums;
 };
 size_t mx_route_bytes(int64_t n, int64_t experts);
-hipError_t launch_mx_route(const MxRoute &r, hipStream_t s);
+hipError_t launch_mx_route(MxRoute r, void *space, hipStream_t s);
 
 struct MxCombine {
     const void *Y;            // [m][ldy]

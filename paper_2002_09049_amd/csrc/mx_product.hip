@@ -14,7 +14,7 @@ __global__ void __launch_bounds__(kFewWaves *kWave) mx_few_kernel(MxProduct p)
 {
     const int64_t c0 = block_of(blockIdx.z) * 16, t0 = (int64_t)blockIdx.y * 16 * kNT;
     if (c0 >= p.c) return;
-    few_product<kNT>(p, c0, t0, [](int64_t token) { return token; });
+    few_product<kNT, kFewWaves>(p, c0, t0, [](int64_t token) { return token; });
 }
 
 template <int kN, class T>
@@ -22,7 +22,7 @@ __global__ void __launch_bounds__(kFewWaves *kWave) mx_token_kernel(MxProduct p,
 {
     const int64_t c0 = block_of(blockIdx.z) * 16;
     if (c0 >= p.c) return;
-    token_product<kN, T>(p, c0, 0, (int)p.n, d, [=](int64_t token) { return X + token * x_ld; },
+    token_product<kN, kFewWaves, T>(p, c0, 0, (int)p.n, d, [=](int64_t token) { return X + token * x_ld; },
                          [](int) { return false; });
 }
 

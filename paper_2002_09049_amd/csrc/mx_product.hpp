@@ -94,8 +94,13 @@ __device__ __forceinline__ void store_y(void *Y, int dtype, int64_t at, float v)
 // 16-byte pieces one after another (64, 25088 x 4096: 34 us, 1.6 TB/s of W).
 constexpr int kFewWaves = 8;
 
+// A workgroup may have more than 16 rows of W: kSplit of its wavefronts then take
+// the chunks of the same 16 in turn, and the next kSplit the next 16 rows.
+template <int kSplit>
+constexpr int kFewRows = kFewWaves / kSplit * 16;
+
 // The sums of a workgroup's wavefronts to Y.
-template <int kNT>
+template <int kNT, int kSplit>
 __device__ __forceinline__ void join_waves(const MxProduct &p, float (&part)[kFewWaves][kNT][kWave * 4],
                                            const f32x4 (&acc)[kNT], int64_t c0, int64_t t0)
 {
@@ -103,15 +108,16 @@ __device__ __forceinline__ void join_waves(const MxProduct &p, float (&part)[kFe
 #pragma unroll
     for (int t = 0; t < kNT; ++t) *(f32x4 *)&part[wave][t][lane * 4] = acc[t];
     __syncthreads();
-    // output o of the tile: row o % 16 of W, token o / 16; lane l's register i
-    // holds row 4 (l / 16) + i, token l % 16
-    for (int o = threadIdx.x; o < kNT * 256; o += kFewWaves * kWave) {
-        const int row = o % 16, tok = o / 16;
-        const int at = ((row / 4) * 16 + tok % 16) * 4 + row % 4;
+    // output o of the tile: row o % kRows of W, token o / kRows; lane l's register i
+    // holds row 4 (l / 16) + i of the wavefront's 16, token l % 16
+    constexpr int kRows = kFewRows<kSplit>;
+    for (int o = threadIdx.x; o < kNT * 16 * kRows; o += kFewWaves * kWave) {
+        const int row = o % kRows, tok = o / kRows;
+        const int at = ((row % 16 / 4) * 16 + tok % 16) * 4 + row % 4;
         if (c0 + row >= p.c || t0 + tok >= p.n) continue;
         float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kFewWaves; ++w) v += part[w][tok / 16][at];
+        for (int w = 0; w < kSplit; ++w) v += part[row / 16 * kSplit + w][tok / 16][at];
         if (p.bias) v += p.bias[c0 + row];
         store_y(p.Y, p.dtype, (t0 + tok) * p.ldy + c0 + row, v);
     }
@@ -119,7 +125,7 @@ __device__ __forceinline__ void join_waves(const MxProduct &p, float (&part)[kFe
 
 // The workgroup of rows c0 .. of W and tokens t0 .. (up to p.n); row_of gives a
 // token's row of X.
-template <int kNT, class RowOf>
+template <int kNT, int kSplit, class RowOf>
 __device__ __forceinline__ void few_product(const MxProduct &p, int64_t c0, int64_t t0, RowOf row_of)
 {
     __shared__ __align__(16) float part[kFewWaves][kNT][kWave * 4];
@@ -127,7 +133,7 @@ __device__ __forceinline__ void few_product(const MxProduct &p, int64_t c0, int6
     const int r = lane % 16, g = lane / 16;
     const int nb = p.nb;
     // rows past the end repeat the last one: their sums are not stored
-    const int64_t wrow = min(c0 + r, p.c - 1);
+    const int64_t wrow = min(c0 + wave / kSplit * 16 + r, p.c - 1);
     int64_t xrow[kNT];
     f32x4 acc[kNT];
 #pragma unroll
@@ -147,10 +153,10 @@ __device__ __forceinline__ void few_product(const MxProduct &p, int64_t c0, int6
             acc[t] = multiply_chunk(a, b[t], acc[t]);
         }
     };
-    int k = wave * kChunkBlocks;
-    for (; k + kChunkBlocks <= nb; k += kFewWaves * kChunkBlocks) chunk(std::true_type(), k);
+    int k = wave % kSplit * kChunkBlocks;
+    for (; k + kChunkBlocks <= nb; k += kSplit * kChunkBlocks) chunk(std::true_type(), k);
     if (k < nb) chunk(std::false_type(), k);   // the chunk that the row ends in
-    join_waves<kNT>(p, part, acc, c0, t0);
+    join_waves<kNT, kSplit>(p, part, acc, c0, t0);
 }
 
 // One to kN tokens, quantized on the way: a wavefront quantizes its chunk of
@@ -163,7 +169,7 @@ __device__ __forceinline__ void few_product(const MxProduct &p, int64_t c0, int6
 //
 // The workgroup of rows c0 .. of W and the n tokens t0 ..; at gives the start of
 // a token's row of X, none whether it is zeros instead.
-template <int kN, class T, class At, class None>
+template <int kN, int kSplit, class T, class At, class None>
 __device__ __forceinline__ void token_product(const MxProduct &p, int64_t c0, int64_t t0, int n, int d, At at, None none)
 {
     __shared__ __align__(16) float part[kFewWaves][1][kWave * 4];
@@ -172,7 +178,7 @@ __device__ __forceinline__ void token_product(const MxProduct &p, int64_t c0, in
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = lane % 16, g = lane / 16;
     const int nb = p.nb;
-    const int64_t wrow = min(c0 + r, p.c - 1);
+    const int64_t wrow = min(c0 + wave / kSplit * 16 + r, p.c - 1);
     f32x4 acc[1] = {f32x4{0, 0, 0, 0}};
     struct Chunk {
         Share a;
@@ -213,9 +219,9 @@ __device__ __forceinline__ void token_product(const MxProduct &p, int64_t c0, in
     };
     // this wavefront's chunks inside the rows of X, the next one's loads in
     // flight, then the one that they end in
-    constexpr int kTurn = kFewWaves * kChunkBlocks;
+    constexpr int kTurn = kSplit * kChunkBlocks;
     const int inside = d / kMxBlock;   // whole blocks
-    int k = wave * kChunkBlocks;
+    int k = wave % kSplit * kChunkBlocks;
     const int mine = k + kChunkBlocks <= inside ? (inside - kChunkBlocks - k) / kTurn + 1 : 0;
     Chunk even, odd;
     if (mine > 0) {
@@ -242,7 +248,7 @@ __device__ __forceinline__ void token_product(const MxProduct &p, int64_t c0, in
         fetch(std::false_type(), k, even);
         multiply(even);
     }
-    join_waves<1>(p, part, acc, c0, t0);
+    join_waves<1, kSplit>(p, part, acc, c0, t0);
 }
 
 // Many tokens: a workgroup owns 64 kTM rows of W by 64 kTN tokens, its four
@@ -437,11 +443,10 @@ __device__ __forceinline__ void write_turn(T *to, int64_t step, const float *tur
     }
 }
 
-template <int kTM, int kTN>
+template <int kTM, int kTN, int kJ = kTN < 2 ? 1 : 2>   // kJ: token tiles of a turn
 __device__ __forceinline__ void write_tiles(const MxProduct &p, float *turn, int64_t c0, int64_t t0, int lane,
                                             const f32x16 (&acc)[kTM][kTN])
 {
-    constexpr int kJ = kTN < 2 ? 1 : 2;   // token tiles of a turn
     const int r = lane % 32, h = lane / 32;
 #pragma unroll
     for (int i = 0; i < kTM; i += 2) {
@@ -473,11 +478,122 @@ __device__ __forceinline__ void write_tiles(const MxProduct &p, float *turn, int
     }
 }
 
+// The same for 16-bit values, which are rounded on their way into LDS, so that the
+// whole of a wavefront's rows of W, 32 kTM, is there of 32 tokens at a time: half
+// the bytes through LDS, and a token's 128 or 256 bytes in one store, its reads
+// all ahead of it.  Piece q of a token (eight values) lies in place q ^ (token %
+// 16), of 64 rows q ^ (token / 2 % 8).  bias: of the wavefront's rows, in LDS;
+// between(j) runs while the reads of token tile j are on their way.
+template <class T>
+__device__ __forceinline__ uint32_t packed_pair(float a, float b)
+{
+    typedef T two __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), two));
+}
+
+template <bool kBias, int kTM, int kTN, class T, class Between>
+__device__ __forceinline__ void write_packed(const MxProduct &p, uint8_t *turn, const float *bias, int64_t c0, int64_t t0,
+                                             int lane, const f32x16 (&acc)[kTM][kTN], Between between)
+{
+    constexpr int kPieces = 4 * kTM, kTokens = kWave / kPieces, kTimes = 32 / kTokens;   // of a token; of one load
+    const int r = lane % 32, h = lane / 32;
+    const auto place = [](int token, int piece) {
+        return (token * kPieces + (piece ^ (kTM == 4 ? token % 16 : token / 2 % 8))) * 16;
+    };
+    const int piece = lane % kPieces, token = lane / kPieces;
+    const int64_t row = c0 + 8 * piece;
+    const int live = (int)min((int64_t)8, p.c - row);
+    const bool rows_live = c0 + 32 * kTM <= p.c;
+#pragma unroll
+    for (int j = 0; j < kTN; ++j) {
+#pragma unroll
+        for (int i = 0; i < kTM; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x16 &t = acc[i][j];
+                f32x4 y = f32x4{t[4 * q], t[4 * q + 1], t[4 * q + 2], t[4 * q + 3]};
+                if constexpr (kBias) y += *(const f32x4 *)(bias + 32 * i + 8 * q + 4 * h);
+                *(two_words *)(turn + place(r, 4 * i + q) + 8 * h) =
+                    (uint64_t)packed_pair<T>(y[2], y[3]) << 32 | packed_pair<T>(y[0], y[1]);
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        u32x4 out[kTimes];
+#pragma unroll
+        for (int k = 0; k < kTimes; ++k) out[k] = *(const u32x4 *)(turn + place(token + k * kTokens, piece));
+        between(j);
+        const int64_t first = t0 + 32 * j;
+        const int tokens = (int)min((int64_t)32, p.n - first);
+        T *to = (T *)p.Y + (first + token) * p.ldy + row;
+        if (rows_live && tokens == 32) {
+#pragma unroll
+            for (int k = 0; k < kTimes; ++k) *(loose_vector *)(to + k * kTokens * p.ldy) = out[k];
+        } else {
+#pragma unroll
+            for (int k = 0; k < kTimes; ++k) {
+                T v[8];
+                __builtin_memcpy(v, &out[k], 16);
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    if (token + k * kTokens < tokens && x < live) to[k * kTokens * p.ldy + x] = v[x];
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+// A wavefront's sums to Y: 32 kTM rows of W from c0, 32 kTN tokens from t0.
+// bias: those of the rows lane kTM / 2, + 1 (loaded_bias); bias_at: room for 32 kTM.
+template <int kTM>
+struct Bias {
+    float of[kTM / 2];
+};
+template <int kTM>
+__device__ __forceinline__ Bias<kTM> loaded_bias(const MxProduct &p, int64_t c0, int lane)
+{
+    Bias<kTM> b;
+#pragma unroll
+    for (int i = 0; i < kTM / 2; ++i) {
+        const int64_t row = c0 + lane * (kTM / 2) + i;
+        b.of[i] = p.bias && row < p.c ? p.bias[row] : 0.0f;
+    }
+    return b;
+}
+template <int kTM, int kTN, class Between>
+__device__ __forceinline__ void write_sums(const MxProduct &p, uint8_t *turn, float *bias_at, const Bias<kTM> &bias,
+                                           int64_t c0, int64_t t0, int lane, const f32x16 (&acc)[kTM][kTN], Between between)
+{
+    if (p.dtype == MPQ_F32) {
+#pragma unroll
+        for (int j = 0; j < kTN; ++j) between(j);
+        write_tiles<kTM, kTN, 1>(p, (float *)turn, c0, t0, lane, acc);
+        return;
+    }
+    if (p.bias) {
+#pragma unroll
+        for (int i = 0; i < kTM / 2; ++i) bias_at[lane * (kTM / 2) + i] = bias.of[i];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (p.dtype == MPQ_F16) write_packed<true, kTM, kTN, _Float16>(p, turn, bias_at, c0, t0, lane, acc, between);
+        else write_packed<true, kTM, kTN, __bf16>(p, turn, bias_at, c0, t0, lane, acc, between);
+    } else {
+        if (p.dtype == MPQ_F16) write_packed<false, kTM, kTN, _Float16>(p, turn, bias_at, c0, t0, lane, acc, between);
+        else write_packed<false, kTM, kTN, __bf16>(p, turn, bias_at, c0, t0, lane, acc, between);
+    }
+}
+
 // The tile of this workgroup.  Workgroups are dealt to the eight XCDs in turn,
 // and each XCD has an L2 of its own: an XCD takes a run of consecutive tiles, in
 // an order that goes through four rows of tiles (of W) side by side, so that the
 // 32 workgroups which run there together read 4 + 8 tiles' rows.
 constexpr int kXcds = 8, kSide = 4;
+
+// Tile `at` of that order.
+__device__ __forceinline__ void tile_at(int at, int tiles_m, int tiles_n, int &tm, int &tn)
+{
+    const int group = at / (kSide * tiles_n), in = at - group * (kSide * tiles_n);
+    const int side = min(kSide, tiles_m - group * kSide);
+    tn = __builtin_amdgcn_readfirstlane(in / side);
+    tm = __builtin_amdgcn_readfirstlane(group * kSide + in % side);
+}
 
 __device__ __forceinline__ bool tile_of(int tiles_m, int tiles_n, int &tm, int &tn)
 {
@@ -485,29 +601,16 @@ __device__ __forceinline__ bool tile_of(int tiles_m, int tiles_n, int &tm, int &
     const int xcd = blockIdx.x % kXcds, slot = blockIdx.x / kXcds;
     const int run = tiles / kXcds, more = tiles % kXcds;
     if (slot >= run + (xcd < more ? 1 : 0)) return false;   // the grid is rounded up
-    const int at = xcd * run + min(xcd, more) + slot;
-    const int group = at / (kSide * tiles_n), in = at - group * (kSide * tiles_n);
-    const int side = min(kSide, tiles_m - group * kSide);
-    tn = __builtin_amdgcn_readfirstlane(in / side);
-    tm = __builtin_amdgcn_readfirstlane(group * kSide + in % side);
+    tile_at(xcd * run + min(xcd, more) + slot, tiles_m, tiles_n, tm, tn);
     return true;
 }
 
 // Where the tokens of a tile are: rows t0 .. of X behind each other (kGather
-// false), or those that `order` names: token t0 + i is row order[t0 + i] / choices
-// of the `rows` rows of X, or the row of zeros behind them if it is none of
-// these; without order, row t0 + i itself.  Offsets into all of X's codes stay
-// below kOutside.
+// false), or those that a list names, token t0 + i row `list[t0 + i]`.  Offsets into
+// all of X's codes, `rows` rows of them, stay below kOutside.
 struct MxGather {
-    const int32_t *order;
-    int choices;
+    const int32_t *list;
     int64_t rows;
-    __device__ __forceinline__ int64_t row_of(int64_t at) const
-    {
-        if (!order) return min(at, rows);
-        const int64_t row = (uint32_t)order[at] / (uint32_t)choices;
-        return order[at] < 0 ? rows : min(row, rows);
-    }
 };
 
 // The workgroup of rows c0 .. of W and tokens t0 .. (up to p.n).
@@ -529,7 +632,7 @@ __device__ __forceinline__ void tile_product(const MxProduct &p, int64_t c0, int
     const int row_bytes = p.nb * 16;
     const int64_t wrows = min((int64_t)kBM, p.c - c0), xrows = min((int64_t)kBN, p.n - t0);
     const __amdgpu_buffer_rsrc_t wc = buffer_of(p.wc + c0 * row_bytes, wrows * row_bytes);
-    const __amdgpu_buffer_rsrc_t xc = kGather ? buffer_of(p.xc, (gather.rows + 1) * row_bytes)
+    const __amdgpu_buffer_rsrc_t xc = kGather ? buffer_of(p.xc, gather.rows * row_bytes)
                                               : buffer_of(p.xc + t0 * row_bytes, xrows * row_bytes);
     const int wm = wave % 2 * (kBM / 2), wn = wave / 2 * (kBN / 2);   // the wavefront's quarter
 
@@ -542,7 +645,7 @@ __device__ __forceinline__ void tile_product(const MxProduct &p, int64_t c0, int
 #pragma unroll
         for (int k = 0; k < kTN; ++k) {
             const int at = xrow0 + 16 * k + lane / 4;
-            gathered[k] = tile_gather_offset(at < xrows ? gather.row_of(t0 + at) : -1, lane, row_bytes);
+            gathered[k] = tile_gather_offset(at < xrows ? gather.list[t0 + at] : -1, lane, row_bytes);
         }
     }
     const auto load = [&](int st, int buf, int k) {
@@ -561,7 +664,7 @@ __device__ __forceinline__ void tile_product(const MxProduct &p, int64_t c0, int
         const int row = 256 * i + 64 * wave;
         // (none of them inside the matrix: a buffer of no bytes)
         return row < kBM ? buffer_of(p.ws + (c0 + row) * p.nb, max((int64_t)0, wrows - row) * p.nb)
-               : kGather ? buffer_of(p.xs, (gather.rows + 1) * p.nb)
+               : kGather ? buffer_of(p.xs, gather.rows * p.nb)
                          : buffer_of(p.xs + (t0 + row - kBM) * p.nb, max((int64_t)0, xrows - (row - kBM)) * p.nb);
     };
     uint32_t scale_at[kScaleRows];
@@ -570,7 +673,7 @@ __device__ __forceinline__ void tile_product(const MxProduct &p, int64_t c0, int
         scale_at[i] = (uint32_t)(lane * p.nb);
         const int row = 256 * i + 64 * wave;
         if (kGather && row >= kBM) {
-            const int64_t at = row - kBM + lane, from = at < xrows ? gather.row_of(t0 + at) : -1;
+            const int64_t at = row - kBM + lane, from = at < xrows ? gather.list[t0 + at] : -1;
             scale_at[i] = from < 0 ? kOutside : (uint32_t)(from * p.nb);
         }
     }
@@ -661,7 +764,13 @@ __device__ __forceinline__ void tile_product(const MxProduct &p, int64_t c0, int
     meet<0>();
     static_assert(kTM % 2 == 0 && 32 * (kTN < 2 ? 1 : 2) * kTurnRow * 4 <= kRows * kStageBytes,
                   "a wavefront's part fits its buffer");
-    write_tiles(p, (float *)ring(wave), c0 + wm, t0 + wn, lane, acc);
+    if constexpr (kGather) {
+        static_assert(32 * kTurnRow * 4 + 128 * kTM <= kRows * kStageBytes, "and the bias behind it");
+        write_sums<kTM, kTN>(p, ring(wave), (float *)(ring(wave) + 32 * kTurnRow * 4), loaded_bias<kTM>(p, c0 + wm, lane),
+                             c0 + wm, t0 + wn, lane, acc, [](int) {});
+    } else {
+        write_tiles(p, (float *)ring(wave), c0 + wm, t0 + wn, lane, acc);
+    }
 }
 
 }  // namespace

@@ -14,41 +14,19 @@
 // reaches 5.2 TB/s; these mostly read or mostly write, and the codes, just
 // written when they were timed, may still lie in the last-level cache.
 #include "mpq.h"
-#include "mx.hpp"
+#include "mx_quantize.hpp"
 
 namespace mpq {
 
 namespace {
 
-constexpr int kThreads = 256, kElems = kThreads * 8;
-
-// The row and the place in it of this thread's eight elements.
-__device__ __forceinline__ void place(int w, int64_t &row, int &j)
-{
-    const int64_t first = block_of(blockIdx.y) * kElems;
-    const int64_t row0 = quotient(first, w);
-    const uint32_t off = (uint32_t)(first - row0 * w) + 8 * threadIdx.x;
-    // rows of 2048 or more: the first one or the next
-    const uint32_t more = w >= kElems ? (off >= (uint32_t)w ? 1u : 0u) : small_quotient(off, 1.0f / (float)w);
-    row = row0 + more;
-    j = (int)(off - more * (uint32_t)w);
-}
+constexpr int kThreads = kRowThreads, kElems = kRowElems;
 
 template <class T>
 __global__ void __launch_bounds__(kThreads) mx_quantize_kernel(const T *X, int64_t rows, int d, int64_t ld, int w,
                                                                uint8_t *codes, uint8_t *scales)
 {
-    int64_t row;
-    int j;
-    place(w, row, j);
-    if (row >= rows) return;   // whole quads: w is a multiple of 32
-    float x[8];
-    load8(X + row * ld + j, d - j, x);
-    const uint32_t s = mx_scale_byte<kFp4>(quad_max(largest_bits(x)));
-    uint32_t c[1];
-    mx_codes<kFp4>(x, s, c);
-    *(uint32_t *)(codes + row * (w / 2) + j / 2) = c[0];
-    if (j % kMxBlock == 0) scales[row * (w / kMxBlock) + j / kMxBlock] = (uint8_t)s;
+    quantize_eight(block_of(blockIdx.y), X, rows, d, ld, w, codes, scales);
 }
 
 template <class T>
@@ -57,7 +35,7 @@ __global__ void __launch_bounds__(kThreads) mx_dequantize_kernel(const uint8_t *
 {
     int64_t row;
     int j;
-    place(w, row, j);
+    place_eight(block_of(blockIdx.y), w, row, j);
     if (row >= rows || j >= d) return;
     const uint32_t c[1] = {*(const uint32_t *)(codes + row * (w / 2) + j / 2)};
     float x[8];

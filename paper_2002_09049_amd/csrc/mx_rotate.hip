@@ -4,13 +4,26 @@
 // A head's row: x' = x / sqrt(mean x^2 + eps) w, then each pair (a, b) of its
 // first `rot` elements turns by the angle position * freq: (a cos - b sin, b cos +
 // a sin).  The angle is found in turns, in 64 bits, and its whole turns are
-// dropped before sine and cosine, so a far position costs no accuracy.  They
-// are the same for all heads of a token, so a workgroup takes a few tokens with
-// all their heads, computes one angle a thread into LDS, and goes through the
-// rows: eight elements a thread, 4 ceil(dim / 32) threads a row, rounded up to a
-// power of two for the sum of squares; a quad holds a block of the cache.  The
-// partner of an element half a head away comes through LDS, a wavefront's part
-// each; a row is read whole before it is written, so a call may write in place.
+// dropped before sine and cosine, so a far position costs no accuracy.
+//
+// A wavefront has one token and some of its heads: it computes the token's
+// angles, one a lane, keeps what a lane's eight elements and their partners are
+// multiplied by in registers, and goes through the heads, 64 / kLanes at a time, the
+// loads of the next ones in flight from the start (the weights' and frequencies',
+// waited for first, are issued before them).  A row is kLanes lanes of eight
+// elements (4 ceil(dim / 32) rounded up to a power of two, for the sum of
+// squares); a quad holds a block of the cache.  The partner of an element half a head
+// away comes from the lane half a row away where the whole of a head of 32, 64,
+// 128 or 256 turns, else through the wavefront's part of LDS.  A row is read whole
+// before it is written, so a call may write in place.  Few tokens are cut into more
+// wavefronts, each with its own angles.
+//
+// fp32 outputs, and keys on their way to the cache, are computed in 64 bits up to
+// the one rounding at the end: for a key that is the rounding to its block's
+// elements, whose borders a rounding to fp32 before it would cross.
+#include <algorithm>
+#include <type_traits>
+
 #include "mpq.h"
 #include "mx_cache.hpp"
 
@@ -18,163 +31,310 @@ namespace mpq {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kAngles = kThreads;   // of a workgroup
-
-// Of one launch: tokens and heads of a workgroup.
-struct Share {
-    int tokens, heads, rows;   // rows: heads of all kinds a token has
-};
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kMostHalf = 128;   // pairs of a head
 
 // The sum over the kLanes lanes of a row.
-template <int kLanes>
-__device__ __forceinline__ float row_sum(float v)
+template <int kLanes, class R>
+__device__ __forceinline__ R row_sum(R v)
 {
     v += xstep<0>(v);
     v += xstep<1>(v);
     if constexpr (kLanes >= 8) v += xstep<2>(v);
     if constexpr (kLanes >= 16) v += xstep<3>(v);
     if constexpr (kLanes >= 32) {
-        float a, b;
+        R a, b;
         swap_step<false>(v, a, b);
         v = a + b;
     }
     return v;
 }
 
-// The eight elements at j of a row whose elements lie at `row` in LDS: turned.
-__device__ __forceinline__ void turn_halves(float (&x)[8], const float *row, int j, int half, const float *cos,
-                                            const float *sin)
+// The value of the lane half a row away.
+template <int kLanes>
+__device__ __forceinline__ uint32_t half_away(uint32_t v)
 {
-    if (half % 4 == 0) {   // four neighbours are of one half, their angles aligned
+    if constexpr (kLanes == 4) return dpp<0x4E>(v);              // quad_perm [2,3,0,1]
+    else if constexpr (kLanes == 8) return dpp<0x1B>(dpp<0x141>(v));   // row_half_mirror, quad_perm [3,2,1,0]
+    else if constexpr (kLanes == 16) return dpp<0x128>(v);       // row_ror:8
+    else {
+        uint32_t a, b;
+        swap_step<false>(v, a, b);
+        return threadIdx.x % 32 < 16 ? b : a;
+    }
+}
+
+// Of a lane's eight elements: the place of each one's partner, and whether it is
+// the second of its pair.
+struct Pairs {
+    int half, j;
+    bool interleaved;
+    __device__ __forceinline__ bool turns(int v) const { return j + v < 2 * half; }
+    __device__ __forceinline__ int angle(int v) const
+    {
+        const int at = j + v;
+        return interleaved ? at / 2 : at < half ? at : at - half;
+    }
+    __device__ __forceinline__ bool second(int v) const { return interleaved ? v % 2 : j + v >= half; }
+    __device__ __forceinline__ int partner(int v) const
+    {
+        const int at = j + v;
+        return at < half ? at + half : at < 2 * half ? at - half : at;
+    }
+};
+
+// The partners of a row's elements: kSwap by lanes, else (where a head is odd, or
+// turns in part) through the wavefront's rows in LDS.
+template <int kLanes, bool kSwap, class T>
+__device__ __forceinline__ void exchange(const Eight<T> &e, const float (&x)[8], const Pairs &p, float *row, float (&other)[8])
+{
+    if (p.interleaved) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int at = j + 4 * q;
-            if (at >= 2 * half) continue;
-            const bool upper = at >= half;
-            const int i = upper ? at - half : at;
-            const f32x4 c = *(const f32x4 *)(cos + i), s = *(const f32x4 *)(sin + i);
-            const f32x4 other = *(const f32x4 *)(row + (upper ? i : at + half));
+        for (int v = 0; v < 8; ++v) other[v] = x[v ^ 1];
+        return;
+    }
+    if constexpr (kSwap) {
+        Eight<T> o;
 #pragma unroll
-            for (int v = 0; v < 4; ++v) x[4 * q + v] = x[4 * q + v] * c[v] + (upper ? other[v] : -other[v]) * s[v];
+        for (int i = 0; i < (int)(2 * sizeof(T)); ++i) o.w[i] = half_away<kLanes>(e.w[i]);
+        o.values(other);
+        return;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    *(f32x4 *)(row + p.j) = f32x4{x[0], x[1], x[2], x[3]};
+    *(f32x4 *)(row + p.j + 4) = f32x4{x[4], x[5], x[6], x[7]};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (p.half % 4 == 0) {   // four neighbours' partners are neighbours
+        const f32x4 lo = *(const f32x4 *)(row + p.partner(0)), hi = *(const f32x4 *)(row + p.partner(4));
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            other[v] = lo[v];
+            other[v + 4] = hi[v];
         }
     } else {
 #pragma unroll
-        for (int v = 0; v < 8; ++v) {
-            const int at = j + v;
-            if (at >= 2 * half) continue;
-            const bool upper = at >= half;
-            const int i = upper ? at - half : at;
-            const float other = row[upper ? i : at + half];
-            x[v] = x[v] * cos[i] + (upper ? other : -other) * sin[i];
-        }
+        for (int v = 0; v < 8; ++v) other[v] = row[p.partner(v)];
     }
 }
 
-__device__ __forceinline__ void turn_neighbours(float (&x)[8], int j, int half, const float *cos, const float *sin)
+// y to fp32 so that a later rounding to fewer bits is that of y itself: towards
+// zero, the last bit set if anything was dropped.
+__device__ __forceinline__ float to_odd(double y)
 {
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        const int i = j / 2 + v;
-        if (i >= half) continue;
-        const float a = x[2 * v], b = x[2 * v + 1], c = cos[i], s = sin[i];
-        x[2 * v] = a * c - b * s;
-        x[2 * v + 1] = b * c + a * s;
-    }
+    const float f = (float)y;
+    uint32_t u = __float_as_uint(f);
+    if ((double)f == y || !(fabsf(f) < INFINITY)) return f;
+    if (fabs((double)f) > fabs(y)) --u;
+    return __uint_as_float(u | 1u);
 }
+
+// What a lane's eight elements, and their partners, are multiplied by: weight and
+// cosine, the partner's weight and the sine (the first of a pair minus it).
+template <class R>
+struct Factors {
+    R own[8], other[8];
+
+    // weights: of a head, in LDS
+    __device__ __forceinline__ void set(bool normed, const float *weights, const Pairs &p, int dim, const double *cosines,
+                                        const double *sines)
+    {
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+            const int at = p.j + v;
+            own[v] = normed && at < dim ? (R)weights[at] : (R)1;
+            other[v] = (R)0;
+            if (!p.turns(v)) continue;
+            const R partners = normed ? (R)weights[p.interleaved ? at ^ 1 : p.partner(v)] : (R)1;
+            const R s = partners * (R)sines[p.angle(v)];
+            own[v] *= (R)cosines[p.angle(v)];
+            other[v] = p.second(v) ? s : -s;
+        }
+    }
+
+    // A row's elements x, normed and turned.
+    template <int kLanes, bool kSwap, bool kOdd, class T>
+    __device__ __forceinline__ void apply(const Eight<T> &e, float (&x)[8], bool normed, const Pairs &p, float *row,
+                                          double inverse_dim, float eps) const
+    {
+        R by = (R)1;
+        if (normed) {
+            R sum = (R)0;
+#pragma unroll
+            for (int v = 0; v < 8; ++v) sum = fma((R)x[v], (R)x[v], sum);
+            by = rsqrt(row_sum<kLanes>(sum) * (R)inverse_dim + (R)eps);
+        }
+        float partner[8];
+        if (p.half > 0) exchange<kLanes, kSwap>(e, x, p, row, partner);
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+            R y;
+            if (kSwap || p.turns(v)) y = fma((R)x[v], own[v], (R)partner[v] * other[v]);
+            else y = normed ? (R)x[v] * own[v] : (R)x[v];
+            if (normed) y *= by;
+            if constexpr (kOdd) x[v] = to_odd(y);
+            else x[v] = (float)y;
+        }
+    }
+};
+
+// A wavefront's rows of one kind, from `lo` below `hi`, kHeads at a time; the
+// loads of the next kDepth of a lane are in flight.
+template <int kDepth, int kHeads, class T>
+struct Rows {
+    const T *from;
+    int64_t stride;
+    int lo, hi, live;
+    Eight<T> next[kDepth];
+
+    __device__ __forceinline__ void start(const void *base, int64_t offset, int64_t step, int first, int last, int j, int dim)
+    {
+        from = (const T *)base + offset + j;
+        stride = step;
+        lo = first;
+        hi = last;
+        live = dim - j;
+#pragma unroll
+        for (int i = 0; i < kDepth; ++i)
+            if (lo + i * kHeads < hi) next[i] = load_eight(from + (lo + i * kHeads) * stride, live);
+    }
+    template <class Body>
+    __device__ __forceinline__ void each(Body body)
+    {
+        for (int h = lo; h < hi; h += kDepth * kHeads) {
+#pragma unroll
+            for (int i = 0; i < kDepth; ++i) {
+                const int at = h + i * kHeads, more = at + kDepth * kHeads;
+                if (at >= hi) break;
+                const Eight<T> now = next[i];
+                if (more < hi) next[i] = load_eight(from + more * stride, live);
+                float x[8];
+                now.values(x);
+                body(at, now, x);
+            }
+        }
+    }
+};
 
 // kFmt -1: keys go to KO, values are not looked at.
-template <int kFmt, int kLanes, class T>
-__global__ void __launch_bounds__(kThreads) mx_rotate_kernel(MxRotate r, Share share)
+template <int kFmt, int kLanes, bool kSwap, class T>
+__global__ void __launch_bounds__(kThreads) mx_rotate_kernel(MxRotate r, int slices, int per)
 {
-    __shared__ __align__(16) float cosines[kAngles], sines[kAngles];
-    __shared__ __align__(16) float rows[kThreads * 8];
-    const int half = r.rot / 2, pitch = (half + 3) / 4 * 4;
-    const int64_t token0 = (int64_t)blockIdx.x * share.tokens;
-    const int tokens = (int)min((int64_t)share.tokens, r.n - token0);
-    const int head0 = blockIdx.y * share.heads, heads = min(share.heads, share.rows - head0);
-    for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
-        const int t = i / half, f = i - t * half;
-        const double turns = (double)r.positions[token0 + t] * r.freqs[f] * 0.15915494309189533577;
-        const double half_turns = 2.0 * (turns - rint(turns));
-        // the part that fp32 drops, times the derivative
-        const float x = (float)half_turns, rest = (float)(half_turns - (double)x) * 3.14159265f;
-        float s, c;
-        sincospif(x, &s, &c);
-        sines[t * pitch + f] = s + rest * c;
-        cosines[t * pitch + f] = c - rest * s;
+    constexpr int kHeads = kWave / kLanes, kDepth = sizeof(T) == 4 ? 2 : 4;
+    using Short = std::conditional_t<std::is_same_v<T, float>, double, float>;
+    __shared__ __align__(16) double table[kWaves][2][kMostHalf];
+    __shared__ __align__(16) float weights[kWaves][2][kLanes * 8];
+    __shared__ __align__(16) float rows[kWaves][kSwap ? 4 : kWave * 8];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t item = (int64_t)blockIdx.x * kWaves + wave, token = quotient(item, slices);
+    if (token >= r.n) return;
+    // of the heads of all kinds
+    const int first = (int)(item - token * slices) * per, last = first + per, keys = r.heads, values = keys + r.kv;
+    const int half = r.rot / 2, group = lane / kLanes, j = lane % kLanes * 8, live = r.dim - j;
+    double *cosines = table[wave][0], *sines = table[wave][1];
+    float *row = rows[wave] + (kSwap ? 0 : group * kLanes * 8);
+    const Pairs pairs = {half, j, !kSwap && r.interleaved != 0};
+    const double inverse_dim = 1.0 / (double)r.dim;
+
+    const double position = half > 0 ? (double)r.positions[token] : 0.0;
+    double freqs[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) freqs[i] = lane + i * kWave < half ? r.freqs[lane + i * kWave] : 0.0;
+    float wq[4], wk[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int at = lane + i * kWave;
+        wq[i] = r.qw && at < r.dim ? r.qw[at] : 0.0f;
+        wk[i] = r.kw && at < r.dim ? r.kw[at] : 0.0f;
     }
-    __syncthreads();
-    const int lane = threadIdx.x % kLanes, j = lane * 8;
-    float *row = rows + (threadIdx.x - lane) * 8;
-    for (int i = threadIdx.x / kLanes; i < tokens * heads; i += kThreads / kLanes) {
-        const int t = i / heads, h = head0 + i - t * heads;
-        const int64_t token = token0 + t;
-        const bool query = h < r.heads, value = h >= r.heads + r.kv;
-        const int head = query ? h : value ? h - r.heads - r.kv : h - r.heads;
-        const T *from = query ? (const T *)r.Q + token * r.q_tok + head * r.q_head
-                        : value ? (const T *)r.V + token * r.v_tok + head * r.v_head
-                                : (const T *)r.K + token * r.k_tok + head * r.k_head;
-        const int live = r.dim - j;
-        float x[8];
-        load8(from + j, live, x);
-        if (!value) {
-            const float *w = query ? r.qw : r.kw;
-            if (w) {
-                float sum = 0.0f;
+    int64_t slot = -1;
+    if (kFmt >= 0 && last > keys) slot = r.slots[token];
+    __builtin_amdgcn_sched_barrier(0);
+    Rows<kDepth, kHeads, T> q;
+    q.start(r.Q, token * r.q_tok, r.q_head, first + group, min(last, keys), j, r.dim);
+    Rows<2, kHeads, T> k, v;
+    k.start(r.K, token * r.k_tok, r.k_head, max(first - keys, 0) + group, min(last - keys, r.kv), j, r.dim);
+    if constexpr (kFmt >= 0)
+        v.start(r.V, token * r.v_tok, r.v_head, max(first - values, 0) + group, min(last - values, r.kv), j, r.dim);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int v = 0; v < 8; ++v) sum += x[v] * x[v];
-                const float by = 1.0f / sqrtf(row_sum<kLanes>(sum) / (float)r.dim + r.eps);
-                float weight[8];
-                load8(w + j, live, weight);
+    for (int i = 0; i < 2; ++i) {
+        if (lane + i * kWave >= half) break;
+        const double turns = position * freqs[i] * 0.15915494309189533577;
+        double s, c;
+        sincospi(2.0 * (turns - rint(turns)), &s, &c);
+        cosines[lane + i * kWave] = c;
+        sines[lane + i * kWave] = s;
+    }
 #pragma unroll
-                for (int v = 0; v < 8; ++v) x[v] = x[v] * by * weight[v];
-            }
-            if (half > 0) {
-                if (r.interleaved) {
-                    turn_neighbours(x, j, half, cosines + t * pitch, sines + t * pitch);
-                } else {
-                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                    *(f32x4 *)(row + j) = f32x4{x[0], x[1], x[2], x[3]};
-                    *(f32x4 *)(row + j + 4) = f32x4{x[4], x[5], x[6], x[7]};
-                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                    turn_halves(x, row, j, half, cosines + t * pitch, sines + t * pitch);
-                }
-            }
-        }
-        if (kFmt < 0 || query) {
-            T *to = query ? (T *)r.QO + token * r.qo_tok + head * r.qo_head : (T *)r.KO + token * r.ko_tok + head * r.ko_head;
-            if (live > 0) store8<false>(to + j, live, x);
-        } else {
-            constexpr int kF = kFmt < 0 ? kFp4 : kFmt;
-            const int64_t slot = r.slots[token];
-            if (slot >= 0 && slot < r.c.n_pages * r.c.page && j < r.c.nb * kMxBlock) {
-                int64_t page;
-                int at;
-                find(r.c, slot, page, at);
-                const int64_t ph = page * r.c.heads + head, code = code_at<kF>(r.c, ph, at, j), scale = scale_at(r.c, ph, at, j);
-                write8<kF>(x, (value ? r.c.v : r.c.k) + code, (value ? r.c.vs : r.c.ks) + scale, j % kMxBlock == 0);
-            }
-        }
+    for (int i = 0; i < 4; ++i) {
+        const int at = lane + i * kWave;
+        if (at >= kLanes * 8) break;
+        weights[wave][0][at] = wq[i];
+        weights[wave][1][at] = wk[i];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (first < keys) {
+        const bool normed = r.qw != nullptr;
+        Factors<Short> f;
+        f.set(normed, weights[wave][0], pairs, r.dim, cosines, sines);
+        T *to = (T *)r.QO + token * r.qo_tok + j;
+        q.each([&](int h, const Eight<T> &e, float (&x)[8]) {
+            f.template apply<kLanes, kSwap, false>(e, x, normed, pairs, row, inverse_dim, r.eps);
+            if (live > 0) store8<false>(to + h * r.qo_head, live, x);
+        });
+    }
+    if (last <= keys) return;
+    const bool normed = r.kw != nullptr;
+    if constexpr (kFmt < 0) {
+        Factors<Short> f;
+        f.set(normed, weights[wave][1], pairs, r.dim, cosines, sines);
+        T *to = (T *)r.KO + token * r.ko_tok + j;
+        k.each([&](int h, const Eight<T> &e, float (&x)[8]) {
+            f.template apply<kLanes, kSwap, false>(e, x, normed, pairs, row, inverse_dim, r.eps);
+            if (live > 0) store8<false>(to + h * r.ko_head, live, x);
+        });
+    } else {
+        if (slot < 0 || slot >= r.c.n_pages * r.c.page) return;
+        int64_t page;
+        int at;
+        find(r.c, slot, page, at);
+        const auto keep = [&](int h, const float (&x)[8], uint8_t *codes, uint8_t *scales) {
+            if (j >= r.c.nb * kMxBlock) return;
+            const int64_t ph = page * r.c.heads + h;
+            write8<kFmt>(x, codes + code_at<kFmt>(r.c, ph, at, j), scales + scale_at(r.c, ph, at, j), j % kMxBlock == 0);
+        };
+        v.each([&](int h, const Eight<T> &, const float (&x)[8]) { keep(h, x, r.c.v, r.c.vs); });
+        Factors<double> f;
+        f.set(normed, weights[wave][1], pairs, r.dim, cosines, sines);
+        k.each([&](int h, const Eight<T> &e, float (&x)[8]) {
+            f.template apply<kLanes, kSwap, true>(e, x, normed, pairs, row, inverse_dim, r.eps);
+            keep(h, x, r.c.k, r.c.ks);
+        });
     }
 }
 
-template <int kFmt, class T>
-hipError_t rotate_lanes(const MxRotate &r, const Share &share, dim3 grid, hipStream_t s)
+template <int kFmt, bool kSwap, class T>
+hipError_t rotate_lanes(const MxRotate &r, int lanes, int slices, int per, unsigned blocks, hipStream_t s)
 {
-    const int lanes = (r.dim + kMxBlock - 1) / kMxBlock * 4;
-    auto kern = lanes <= 4 ? mx_rotate_kernel<kFmt, 4, T> : lanes <= 8 ? mx_rotate_kernel<kFmt, 8, T>
-                : lanes <= 16 ? mx_rotate_kernel<kFmt, 16, T> : mx_rotate_kernel<kFmt, 32, T>;
-    hipLaunchKernelGGL(kern, grid, dim3(kThreads), 0, s, r, share);
+    auto kern = lanes == 4 ? mx_rotate_kernel<kFmt, 4, kSwap, T> : lanes == 8 ? mx_rotate_kernel<kFmt, 8, kSwap, T>
+                : lanes == 16 ? mx_rotate_kernel<kFmt, 16, kSwap, T> : mx_rotate_kernel<kFmt, 32, kSwap, T>;
+    hipLaunchKernelGGL(kern, dim3(blocks), dim3(kThreads), 0, s, r, slices, per);
     return hipGetLastError();
 }
 
-template <int kFmt>
-hipError_t rotate_as(const MxRotate &r, const Share &share, dim3 grid, hipStream_t s)
+template <int kFmt, class T>
+hipError_t rotate_swap(const MxRotate &r, int lanes, int slices, int per, unsigned blocks, hipStream_t s)
 {
-    if (r.dtype == MPQ_F32) return rotate_lanes<kFmt, float>(r, share, grid, s);
-    if (r.dtype == MPQ_F16) return rotate_lanes<kFmt, _Float16>(r, share, grid, s);
-    return rotate_lanes<kFmt, __bf16>(r, share, grid, s);
+    if (!r.interleaved && r.rot == r.dim && r.dim == 8 * lanes) return rotate_lanes<kFmt, true, T>(r, lanes, slices, per, blocks, s);
+    return rotate_lanes<kFmt, false, T>(r, lanes, slices, per, blocks, s);
+}
+
+template <int kFmt>
+hipError_t rotate_as(const MxRotate &r, int lanes, int slices, int per, unsigned blocks, hipStream_t s)
+{
+    if (r.dtype == MPQ_F32) return rotate_swap<kFmt, float>(r, lanes, slices, per, blocks, s);
+    if (r.dtype == MPQ_F16) return rotate_swap<kFmt, _Float16>(r, lanes, slices, per, blocks, s);
+    return rotate_swap<kFmt, __bf16>(r, lanes, slices, per, blocks, s);
 }
 
 }  // namespace
@@ -182,19 +342,18 @@ hipError_t rotate_as(const MxRotate &r, const Share &share, dim3 grid, hipStream
 hipError_t launch_mx_rotate(const MxRotate &r, bool append, hipStream_t s)
 {
     if (r.n <= 0) return hipSuccess;
-    Share share;
-    share.rows = r.heads + r.kv + (append ? r.kv : 0);
-    // an angle a thread: as many tokens as that allows
-    const int pitch = (r.rot / 2 + 3) / 4 * 4;
-    share.tokens = pitch == 0 ? 4 : max(1, min(8, kThreads / pitch));
-    share.heads = share.rows;
-    const int64_t blocks = (r.n + share.tokens - 1) / share.tokens;
-    const int splits = (share.rows + share.heads - 1) / share.heads;
-    if (!launchable(blocks, kThreads) || splits > 65535) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks, (unsigned)splits);
+    // lanes of a row, and heads that a wavefront has at a time
+    const int quads = (r.dim + kMxBlock - 1) / kMxBlock, lanes = quads <= 1 ? 4 : quads <= 2 ? 8 : quads <= 4 ? 16 : 32;
+    const int at_once = kWave / lanes, passes = (r.heads + r.kv * (append ? 2 : 1) + at_once - 1) / at_once;
+    // 16 wavefronts a CU
+    const int wanted = (int)std::min((int64_t)passes, std::max((int64_t)1, 4096 / r.n));
+    const int each = (passes + wanted - 1) / wanted, slices = (passes + each - 1) / each;
+    const int64_t blocks = (r.n * slices + kWaves - 1) / kWaves;
+    if (!launchable(blocks, kThreads)) return hipErrorInvalidValue;
     LaunchTimer timer(s, append ? "mx_append_kernel" : "mx_rotate_kernel");
-    if (!append) return rotate_as<-1>(r, share, grid, s);
-    return r.c.fmt == kFp4 ? rotate_as<kFp4>(r, share, grid, s) : rotate_as<kFp8>(r, share, grid, s);
+    if (!append) return rotate_as<-1>(r, lanes, slices, each * at_once, (unsigned)blocks, s);
+    return r.c.fmt == kFp4 ? rotate_as<kFp4>(r, lanes, slices, each * at_once, (unsigned)blocks, s)
+                           : rotate_as<kFp8>(r, lanes, slices, each * at_once, (unsigned)blocks, s);
 }
 
 }  // namespace mpq

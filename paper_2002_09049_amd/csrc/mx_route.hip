@@ -1,19 +1,22 @@
 // Routing of tokens to experts (mpq_mx_route) and the sum of their experts'
 // rows (mpq_mx_combine).
 //
-// Routing: a wavefront has a token, a lane a run of consecutive experts.  A
-// logit is a 32-bit key whose order as an unsigned number is the logits' (NaN
-// and -infinity the smallest, -0 equal to 0), so a round of the choice is one
-// maximum over the lanes and a ballot, whose first lane, and there the first
-// key, is the choice of the lowest index.  The softmax statistics are fp32.
+// Routing: kLanes lanes have a token, a lane kEach consecutive experts, so a
+// wavefront chooses for up to four tokens at a time.  A logit is a key whose order as an
+// unsigned number is the logits' (NaN and -infinity the smallest, -0 equal to 0);
+// a 16-bit logit's key has the expert behind it, so that one maximum over the
+// lanes is a choice, the lowest index first; a 32-bit one takes a minimum over the
+// indexes that hold the maximum as well.  The softmax statistics are fp32.
 //
 // The choices are then sorted by expert, tokens in order: of a workgroup's 64
 // tokens an expert has a mask of 64 bits in LDS (set by "or", whose order does not
 // matter), and a choice's rank among the workgroup's choices of its expert is
 // the number of bits below its token's.  What the workgroups before have chosen
-// is added up by a second kernel (experts in parallel), and a third puts each
-// choice in its place.  Up to 64 tokens one workgroup, and one launch, do it all.
+// is added up from their counts, a byte each, by a second kernel; where that
+// would have every workgroup read too many, a kernel between the two does it
+// once.  Up to 64 tokens one workgroup, and one launch, do it all.
 #include <algorithm>
+#include <type_traits>
 
 #include "mpq.h"
 #include "mx.hpp"
@@ -26,16 +29,119 @@ constexpr int kTokens = 64;       // of a workgroup
 constexpr int kThreads = 1024;
 constexpr int kMostExperts = 1024;
 
-__device__ __forceinline__ uint32_t key_of(float v)
+// Bytes of a workgroup's counts.
+__host__ __device__ __forceinline__ int pitch_of(int experts) { return (experts + 3) / 4 * 4; }
+
+// Maximum, minimum or sum over the kLanes lanes of a token.
+template <int kLanes, class V, class Op>
+__device__ __forceinline__ V lanes_reduce(V v, Op op)
+{
+    v = op(v, xstep<0>(v));
+    v = op(v, xstep<1>(v));
+    v = op(v, xstep<2>(v));
+    v = op(v, xstep<3>(v));
+    if constexpr (kLanes >= 32) {
+        V a, b;
+        swap_step<false>(v, a, b);
+        v = op(a, b);
+    }
+    if constexpr (kLanes >= 64) {
+        V a, b;
+        swap_step<true>(v, a, b);
+        v = op(a, b);
+    }
+    return v;
+}
+
+// The order of a logit's bits; 0 is below all.
+__device__ __forceinline__ uint32_t order_of(float v)
 {
     if (!(v > -INFINITY)) return 0x007fffffu;   // -infinity's
     const uint32_t u = __float_as_uint(v + 0.0f);
     return u >> 31 ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ float value_of(uint32_t key)
+__device__ __forceinline__ float value_of(uint32_t order)
 {
-    return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key);
+    return __uint_as_float(order >> 31 ? order & 0x7fffffffu : ~order);
 }
+// The same of 16 bits.
+template <class T>
+__device__ __forceinline__ uint32_t order16_of(T v)
+{
+    if (!((float)v > -INFINITY)) v = (T)-INFINITY;
+    if ((float)v == 0.0f) v = (T)0.0f;
+    uint16_t u;
+    __builtin_memcpy(&u, &v, 2);
+    return u >> 15 ? (uint16_t)~u : u | 0x8000u;
+}
+template <class T>
+__device__ __forceinline__ float value16_of(uint32_t order)
+{
+    const uint16_t u = (uint16_t)(order >> 15 ? order & 0x7fffu : ~order);
+    T v;
+    __builtin_memcpy(&v, &u, 2);
+    return (float)v;
+}
+
+// A lane's keys of one type of logit.
+template <class T, int kLanes, int kEach>
+struct Keys {
+    static constexpr bool kWhole = std::is_same_v<T, float>;   // the key is the value alone
+    uint32_t key[kEach], most;
+
+    __device__ __forceinline__ void largest()
+    {
+        most = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) most = max(most, key[i]);
+    }
+    __device__ __forceinline__ void load(const T *row, int first, int experts)
+    {
+        T v[kEach];
+        if constexpr (kEach % 8 == 0) {
+#pragma unroll
+            for (int i = 0; i < kEach; i += 8) {
+                const Eight<T> e = load_eight(row + first + i, experts - first - i);
+                __builtin_memcpy(v + i, e.w, sizeof e.w);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) v[i] = first + i < experts ? row[first + i] : (T)0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            if constexpr (kWhole) key[i] = order_of(v[i]);
+            else key[i] = order16_of(v[i]) << 16 | (uint32_t)(0xffff - (first + i));
+            if (first + i >= experts) key[i] = 0;
+        }
+        largest();
+    }
+    __device__ __forceinline__ float value(uint32_t k) const
+    {
+        if constexpr (kWhole) return value_of(k);
+        else return value16_of<T>(k >> 16);
+    }
+    // The largest of all lanes, taken out: its key, and its expert.
+    __device__ __forceinline__ uint32_t take(int first, int &expert)
+    {
+        const uint32_t best = lanes_reduce<kLanes>(most, MaxOp());
+        if constexpr (kWhole) {
+            int at = kMostExperts;
+#pragma unroll
+            for (int i = kEach - 1; i >= 0; --i) at = key[i] == best ? first + i : at;
+            expert = lanes_reduce<kLanes>(at, MinOp());
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) key[i] = first + i == expert ? 0u : key[i];
+        } else {
+            expert = 0xffff - (int)(best & 0xffff);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) key[i] = key[i] == best ? 0u : key[i];
+        }
+        largest();
+        return best;
+    }
+};
+
 // exp(v - top), an infinite top's equals included
 __device__ __forceinline__ float part_of(float v, float top)
 {
@@ -63,55 +169,39 @@ __device__ __forceinline__ void prefix_counts(uint32_t *counts, int experts)
     __syncthreads();
 }
 
-// kEach: experts of a lane.  kAlone: this workgroup has all tokens.
-template <int kEach, bool kAlone, class T>
+// kAlone: this workgroup has all tokens.
+template <int kLanes, int kEach, bool kAlone, class T>
 __global__ void __launch_bounds__(kThreads) mx_choose_kernel(MxRoute r)
 {
     __shared__ unsigned long long masks[kMostExperts];
     __shared__ uint32_t counts[kMostExperts + 1];
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int lane = threadIdx.x % kLanes, first = lane * kEach;
     for (int e = threadIdx.x; e < r.experts; e += kThreads) masks[e] = 0;
     __syncthreads();
     const int64_t token0 = (int64_t)blockIdx.x * kTokens;
     const int tokens = (int)min((int64_t)kTokens, r.n - token0);
-    for (int t = wave; t < tokens; t += kThreads / kWave) {
-        const T *row = (const T *)r.logits + (token0 + t) * r.ld;
-        uint32_t key[kEach], most = 0;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int e = lane * kEach + i;
-            key[i] = e < r.experts ? key_of((float)row[e]) : 0u;
-            most = max(most, key[i]);
-        }
+    for (int t = threadIdx.x / kLanes; t < tokens; t += kThreads / kLanes) {
+        Keys<T, kLanes, kEach> keys;
+        keys.load((const T *)r.logits + (token0 + t) * r.ld, first, r.experts);
         float all = 0.0f, top = 0.0f, mine = 0.0f;
         int chosen = 0;
+        if (!r.renorm) {
+            top = keys.value(lanes_reduce<kLanes>(keys.most, MaxOp()));
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) all += keys.key[i] ? part_of(keys.value(keys.key[i]), top) : 0.0f;
+            all = lanes_reduce<kLanes>(all, SumOp());
+        }
         for (int j = 0; j < r.k; ++j) {
-            const uint32_t best = wave_reduce(most, MaxOp());
-            const int winner = __builtin_ctzll(__ballot(most == best));
-            int e = 0;
-#pragma unroll
-            for (int i = kEach - 1; i >= 0; --i) e = key[i] == best ? i : e;
-            e = readlane(e, winner);
-            if (j == 0) {
-                top = value_of(best);
-                if (!r.renorm) {
-#pragma unroll
-                    for (int i = 0; i < kEach; ++i) all += key[i] ? part_of(value_of(key[i]), top) : 0.0f;
-                    all = wave_reduce(all, SumOp());
-                }
-            }
+            int expert;
+            const float v = keys.value(keys.take(first, expert));
+            if (j == 0) top = v;
             if (lane == j) {
-                chosen = winner * kEach + e;
-                mine = part_of(value_of(best), top);
-            }
-            most = 0;
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                if (lane == winner && i == e) key[i] = 0;
-                most = max(most, key[i]);
+                chosen = expert;
+                mine = v;
             }
         }
-        if (r.renorm) all = wave_reduce(mine, SumOp());
+        mine = lane < r.k ? part_of(mine, top) : 0.0f;
+        if (r.renorm) all = lanes_reduce<kLanes>(mine, SumOp());
         if (lane < r.k) {
             const int64_t at = (token0 + t) * r.k + lane;
             r.chosen[at] = chosen;
@@ -120,14 +210,14 @@ __global__ void __launch_bounds__(kThreads) mx_choose_kernel(MxRoute r)
         }
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < r.experts; e += kThreads) {
-        const uint32_t c = (uint32_t)__popcll(masks[e]);
-        if constexpr (kAlone) counts[e] = c;
-        else r.counts[(int64_t)blockIdx.x * r.experts + e] = (int32_t)c;
-    }
     if constexpr (kAlone) {
+        for (int e = threadIdx.x; e < r.experts; e += kThreads) counts[e] = (uint32_t)__popcll(masks[e]);
         prefix_counts(counts, r.experts);
         for (int e = threadIdx.x; e <= r.experts; e += kThreads) r.offsets[e] = (int32_t)counts[e];
+    } else {
+        const int pitch = pitch_of(r.experts);
+        for (int e = threadIdx.x; e < pitch; e += kThreads)
+            r.counts[(int64_t)blockIdx.x * pitch + e] = e < r.experts ? (uint8_t)__popcll(masks[e]) : 0;
     }
     for (int i = threadIdx.x; i < tokens * r.k; i += kThreads) {
         const int64_t at = token0 * r.k + i;
@@ -142,45 +232,93 @@ __global__ void __launch_bounds__(kThreads) mx_choose_kernel(MxRoute r)
     }
 }
 
-// counts [blocks][experts] to their exclusive sums over the blocks, the sums
-// behind them (row `blocks`).  A workgroup has 16 experts and 64 runs of blocks.
+// Every workgroup's counts to sums [blocks][experts] of the workgroups before it,
+// and the sums of all behind them (row `blocks`).  A workgroup has 16 experts and
+// 64 runs of rows.
 constexpr int kColumns = 16, kRuns = kThreads / kColumns;
-__global__ void __launch_bounds__(kThreads) mx_sum_kernel(int32_t *counts, int blocks, int experts)
+__global__ void __launch_bounds__(kThreads) mx_sum_kernel(const uint8_t *counts, int32_t *to, int blocks, int experts)
 {
     __shared__ int32_t sums[kRuns][kColumns];
     const int column = threadIdx.x % kColumns, run = threadIdx.x / kColumns, e = blockIdx.x * kColumns + column;
-    const int each = (blocks + kRuns - 1) / kRuns, from = min(run * each, blocks), to = min(from + each, blocks);
+    const int each = (blocks + kRuns - 1) / kRuns, from = min(run * each, blocks), end = min(from + each, blocks);
+    const int pitch = pitch_of(experts);
     int32_t sum = 0;
     if (e < experts)
-        for (int b = from; b < to; ++b) sum += counts[(int64_t)b * experts + e];
+        for (int b = from; b < end; ++b) sum += counts[(int64_t)b * pitch + e];
     sums[run][column] = sum;
     __syncthreads();
     if (e >= experts) return;
     int32_t before = 0;
     for (int i = 0; i < run; ++i) before += sums[i][column];
-    for (int b = from; b < to; ++b) {
-        int32_t *c = counts + (int64_t)b * experts + e;
-        const int32_t v = *c;
-        *c = before;
-        before += v;
+    for (int b = from; b < end; ++b) {
+        to[(int64_t)b * experts + e] = before;
+        before += counts[(int64_t)b * pitch + e];
     }
-    if (run == kRuns - 1) counts[(int64_t)blocks * experts + e] = before;
+    if (run == kRuns - 1) to[(int64_t)blocks * experts + e] = before;
 }
 
-__global__ void __launch_bounds__(256) mx_place_kernel(MxRoute r, int blocks)
+// Each choice to its place.  kSummed: by mx_sum_kernel's sums; else this workgroup
+// adds up the counts itself, four experts a word: pairs of 16-bit sums, which
+// hold up to 1023 rows of 64.
+constexpr int kMostAdded = 1023;
+template <bool kSummed>
+__global__ void __launch_bounds__(kThreads) mx_place_kernel(MxRoute r, int blocks)
 {
-    __shared__ uint32_t counts[kMostExperts + 1];
-    for (int e = threadIdx.x; e < r.experts; e += 256) counts[e] = (uint32_t)r.counts[(int64_t)blocks * r.experts + e];
+    __shared__ uint32_t counts[kMostExperts + 1], before[kMostExperts];
+    if constexpr (kSummed) {
+        for (int e = threadIdx.x; e < r.experts; e += kThreads) {
+            counts[e] = (uint32_t)r.sums[(int64_t)blocks * r.experts + e];
+            before[e] = (uint32_t)r.sums[(int64_t)blockIdx.x * r.experts + e];
+        }
+    } else {
+        // two words of pairs for the rows before, two for all
+        __shared__ uint32_t part[4][kThreads];
+        const int words = pitch_of(r.experts) / 4, runs = kThreads / words;
+        const int word = threadIdx.x % words, run = threadIdx.x / words, here = blockIdx.x;
+        uint32_t even = 0, odd = 0, even_before = 0, odd_before = 0;
+        if (run < runs) {
+            const uint32_t *from = (const uint32_t *)r.counts + word;
+            int b = run;
+#pragma unroll 8
+            for (; b < here; b += runs) {
+                const uint32_t v = from[(int64_t)b * words];
+                even += v & 0x00ff00ffu;
+                odd += v >> 8 & 0x00ff00ffu;
+            }
+            even_before = even;
+            odd_before = odd;
+#pragma unroll 8
+            for (; b < blocks; b += runs) {
+                const uint32_t v = from[(int64_t)b * words];
+                even += v & 0x00ff00ffu;
+                odd += v >> 8 & 0x00ff00ffu;
+            }
+        }
+        part[0][threadIdx.x] = even;
+        part[1][threadIdx.x] = odd;
+        part[2][threadIdx.x] = even_before;
+        part[3][threadIdx.x] = odd_before;
+        __syncthreads();
+        for (int e = threadIdx.x; e < r.experts; e += kThreads) {
+            uint32_t all = 0, some = 0;
+            for (int i = 0; i < runs; ++i) {
+                const int at = i * words + e / 4, shift = e % 4 / 2 * 16;
+                all += part[e % 2][at] >> shift & 0xffffu;
+                some += part[2 + e % 2][at] >> shift & 0xffffu;
+            }
+            counts[e] = all;
+            before[e] = some;
+        }
+    }
     prefix_counts(counts, r.experts);
     if (blockIdx.x == 0)
-        for (int e = threadIdx.x; e <= r.experts; e += 256) r.offsets[e] = (int32_t)counts[e];
+        for (int e = threadIdx.x; e <= r.experts; e += kThreads) r.offsets[e] = (int32_t)counts[e];
     const int64_t token0 = (int64_t)blockIdx.x * kTokens;
     const int tokens = (int)min((int64_t)kTokens, r.n - token0);
-    const int32_t *before = r.counts + (int64_t)blockIdx.x * r.experts;
-    for (int i = threadIdx.x; i < tokens * r.k; i += 256) {
+    for (int i = threadIdx.x; i < tokens * r.k; i += kThreads) {
         const int64_t at = token0 * r.k + i;
         const int e = r.chosen[at];
-        const int32_t to = (int32_t)counts[e] + before[e] + r.place[at];
+        const int32_t to = (int32_t)(counts[e] + before[e]) + r.place[at];
         r.place[at] = to;
         r.order[to] = (int32_t)at;
     }
@@ -189,11 +327,14 @@ __global__ void __launch_bounds__(256) mx_place_kernel(MxRoute r, int blocks)
 template <bool kAlone, class T>
 hipError_t choose_as(const MxRoute &r, unsigned blocks, hipStream_t s)
 {
-    auto kern = r.experts <= 64    ? mx_choose_kernel<1, kAlone, T>
-                : r.experts <= 128 ? mx_choose_kernel<2, kAlone, T>
-                : r.experts <= 256 ? mx_choose_kernel<4, kAlone, T>
-                : r.experts <= 512 ? mx_choose_kernel<8, kAlone, T>
-                                   : mx_choose_kernel<16, kAlone, T>;
+    // a choice is kept by the lane of its number
+    auto kern = r.k > 16           ? mx_choose_kernel<64, 16, kAlone, T>
+                : r.experts <= 16  ? mx_choose_kernel<16, 1, kAlone, T>
+                : r.experts <= 64  ? mx_choose_kernel<16, 4, kAlone, T>
+                : r.experts <= 128 ? mx_choose_kernel<16, 8, kAlone, T>
+                : r.experts <= 256 ? mx_choose_kernel<16, 16, kAlone, T>
+                : r.experts <= 512 ? mx_choose_kernel<32, 16, kAlone, T>
+                                   : mx_choose_kernel<64, 16, kAlone, T>;
     hipLaunchKernelGGL(kern, dim3(blocks), dim3(kThreads), 0, s, r);
     return hipGetLastError();
 }
@@ -206,6 +347,15 @@ hipError_t choose(const MxRoute &r, unsigned blocks, hipStream_t s)
     if (r.dtype == MPQ_F16) return choose_as<kAlone, _Float16>(r, blocks, s);
     return choose_as<kAlone, __bf16>(r, blocks, s);
 }
+
+// Whether the workgroups add up the counts themselves: while all of them
+// together read few.
+bool adds_inside(int64_t blocks, int64_t experts)
+{
+    return blocks <= kMostAdded && blocks * blocks * pitch_of((int)experts) <= (int64_t)32 << 20;
+}
+
+size_t count_bytes(int64_t blocks, int64_t experts) { return (size_t)((blocks * pitch_of((int)experts) + 15) / 16 * 16); }
 
 // A thread has eight columns of a token.  Memory bounds it: k rows are read for
 // one that is written.
@@ -247,24 +397,33 @@ hipError_t combine_as(const MxCombine &q, int chunks, dim3 grid, hipStream_t s)
 size_t mx_route_bytes(int64_t n, int64_t experts)
 {
     const int64_t blocks = (n + kTokens - 1) / kTokens;
-    return blocks <= 1 ? 0 : (size_t)((blocks + 1) * experts) * sizeof(int32_t);
+    if (blocks <= 1) return 0;
+    return count_bytes(blocks, experts)
+           + (adds_inside(blocks, experts) ? 0 : (size_t)((blocks + 1) * experts) * sizeof(int32_t));
 }
 
-hipError_t launch_mx_route(const MxRoute &r, hipStream_t s)
+hipError_t launch_mx_route(MxRoute r, void *space, hipStream_t s)
 {
     const unsigned blocks = (unsigned)((r.n + kTokens - 1) / kTokens);
     if (blocks <= 1) return choose<true>(r, 1, s);
+    r.counts = (uint8_t *)space;
+    r.sums = (int32_t *)((uint8_t *)space + count_bytes(blocks, r.experts));
     hipError_t e = choose<false>(r, blocks, s);
     if (e != hipSuccess) return e;
+    if (adds_inside(blocks, r.experts)) {
+        LaunchTimer timer(s, "mx_place_kernel");
+        hipLaunchKernelGGL(mx_place_kernel<false>, dim3(blocks), dim3(kThreads), 0, s, r, (int)blocks);
+        return hipGetLastError();
+    }
     {
         LaunchTimer timer(s, "mx_sum_kernel");
         hipLaunchKernelGGL(mx_sum_kernel, dim3((unsigned)(r.experts + kColumns - 1) / kColumns), dim3(kThreads), 0, s,
-                           r.counts, (int)blocks, r.experts);
+                           r.counts, r.sums, (int)blocks, r.experts);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     LaunchTimer timer(s, "mx_place_kernel");
-    hipLaunchKernelGGL(mx_place_kernel, dim3(blocks), dim3(256), 0, s, r, (int)blocks);
+    hipLaunchKernelGGL(mx_place_kernel<true>, dim3(blocks), dim3(kThreads), 0, s, r, (int)blocks);
     return hipGetLastError();
 }
 

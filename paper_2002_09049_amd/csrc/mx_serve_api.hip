@@ -243,8 +243,7 @@ int mpq_mx_route(const void *logits, int dtype, int64_t n, int64_t experts, int6
     r.place = place;
     r.offsets = offsets;
     r.weights = weights;
-    r.counts = (int32_t *)ws.get();
-    const hipError_t e = mpq::launch_mx_route(r, s);
+    const hipError_t e = mpq::launch_mx_route(r, ws.get(), s);
     const hipError_t freed = ws.close();
     return done(e, freed, "mx route launch");
 }

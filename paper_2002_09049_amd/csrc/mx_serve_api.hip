@@ -251,7 +251,7 @@ int mpq_mx_route(const void *logits, int dtype, int64_t n, int64_t experts, int6
 int64_t mpq_mx_experts_workspace(int64_t n, int64_t m, int64_t experts, int64_t c_out, int64_t d)
 {
     const int rc = check_experts(n, m, experts, c_out, d);
-    return rc != MPQ_OK ? rc : n == 0 || m == 0 || c_out == 0 ? 0 : (int64_t)mpq::mx_experts_bytes(n, m, experts, d);
+    return rc != MPQ_OK ? rc : n == 0 || m == 0 || c_out == 0 ? 0 : (int64_t)mpq::mx_experts_bytes(n, m, experts, c_out, d);
 }
 
 int mpq_mx_experts(const void *X, int x_dtype, int64_t n, int64_t x_ld, const uint8_t *w_codes, const uint8_t *w_scales,
@@ -276,7 +276,7 @@ int mpq_mx_experts(const void *X, int x_dtype, int64_t n, int64_t x_ld, const ui
     if (rc != MPQ_OK || m == 0 || c_out == 0) return rc;
     hipStream_t s = (hipStream_t)stream;
     Workspace ws;
-    rc = ws.open(workspace_opt, workspace_bytes, mpq::mx_experts_bytes(n, m, experts, d), s);
+    rc = ws.open(workspace_opt, workspace_bytes, mpq::mx_experts_bytes(n, m, experts, c_out, d), s);
     if (rc != MPQ_OK) return rc;
     mpq::MxExperts g = {};
     g.p.wc = w_codes;

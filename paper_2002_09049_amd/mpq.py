@@ -555,13 +555,21 @@ def mx_linear(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bias: 
     return Y
 
 
-def _one_device(*tensors):
-    """The tensors of a call (None: an argument that is not given) lie on the
-    current device, where its kernels are launched."""
-    here = torch.cuda.current_device()
+_current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _place(stream, *tensors) -> int:
+    """The stream's handle, and that the tensors of a call (None: an argument that
+    is not given) lie on the current device, where its kernels are launched."""
+    if not tensors[0].is_cuda:
+        raise ValueError(f"every tensor must be a ROCm device tensor (got one on {tensors[0].device})")
+    here = _current()
     for x in tensors:
         if x is not None and x.get_device() != here:
             raise ValueError(f"every tensor must be on the current device, cuda:{here} (got one on {x.device})")
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(here)
+    return _stream(stream)
 
 
 def mx_plan(cached: torch.Tensor, fresh: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor,
@@ -592,7 +600,7 @@ def mx_plan(cached: torch.Tensor, fresh: torch.Tensor, page_table: torch.Tensor,
                            (starts, batch + 1, "starts"), (lengths, batch, "lengths"), (after, 1, "taken")):
             if x.shape != (n,):
                 raise ValueError(f"out's {name} must be {(n,)} (got {tuple(x.shape)})")
-        _one_device(*out)
+        _place(stream, *out)
         _dev(slots, torch.int64, "out's slots")
         for x in (positions, starts, lengths, after):
             _dev(x, i32, "out")
@@ -603,13 +611,12 @@ def mx_plan(cached: torch.Tensor, fresh: torch.Tensor, page_table: torch.Tensor,
         # four in one allocation: 2.3 us less
         positions, starts, lengths, after = _new(cached, (max_tokens + 2 * batch + 2,), i32, stream).split(
             (max_tokens, batch + 1, batch, 1))
-    _one_device(cached, fresh, page_table, free_pages, taken)
+    at = _place(stream, cached, fresh, page_table, free_pages, taken)
     pages = page_table.shape[1]
     _check(load().mpq_mx_plan(_dev(cached, i32, "cached"), _dev(fresh, i32, "fresh"), batch, page_table.data_ptr(),
                               page_table.stride(0) if batch > 1 else pages, pages, _dev(free_pages, i32, "free_pages"),
                               free_pages.shape[0], _dev(taken, i32, "taken"), page_size, max_tokens, slots.data_ptr(),
-                              positions.data_ptr(), starts.data_ptr(), lengths.data_ptr(), after.data_ptr(),
-                              _stream(stream)))
+                              positions.data_ptr(), starts.data_ptr(), lengths.data_ptr(), after.data_ptr(), at))
     return slots, positions, starts, lengths, after
 
 
@@ -627,14 +634,25 @@ def _rotation(n: int, dim: int, positions, freqs, q_weight, k_weight):
             None if k_weight is None else _dev(k_weight, torch.float32, "k_weight"))
 
 
+def _head_rows(x: torch.Tensor, shape, name: str):
+    """(pointer, strides of dimensions 0 and 1) of a 3-D tensor whose last
+    dimension is contiguous."""
+    if x.shape != shape:
+        raise ValueError(f"{name} must be {tuple(shape)} (got {tuple(x.shape)})")
+    token, head, one = x.stride()
+    if one != 1 and shape[2] > 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    return x.data_ptr(), token, head
+
+
 def _heads_out(out, like: torch.Tensor, shape, name: str, stream):
     """(tensor, pointer, strides) of an output of heads like `like`."""
     if out is None:
-        out = _new(like, shape, like.dtype, stream)
+        out = like.new_empty(shape) if stream is None else _new(like, shape, like.dtype, stream)
         return out, out.data_ptr(), shape[1] * shape[2], shape[2]
     if out.dtype != like.dtype:
         raise ValueError(f"{name} must be {like.dtype} (got {out.dtype})")
-    return (out, *_heads(out, shape, name))
+    return (out, *_head_rows(out, shape, name))
 
 
 def mx_rotate(Q: torch.Tensor, K: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor,
@@ -648,19 +666,19 @@ def mx_rotate(Q: torch.Tensor, K: torch.Tensor, positions: torch.Tensor, freqs: 
     which may be Q and K themselves."""
     if Q.dim() != 3 or K.dim() != 3:
         raise ValueError("Q and K must be 3-D [n, heads, head_dim]")
-    n, heads, dim = Q.shape
+    n, heads, dim = shape = Q.shape
     kv = K.shape[1]
-    qp, qt, qh = _heads(Q, (n, heads, dim), "Q")
-    kp, kt, kh = _heads(K, (n, kv, dim), "K")
+    qp, qt, qh = _head_rows(Q, shape, "Q")
+    kp, kt, kh = _head_rows(K, (n, kv, dim), "K")
     if K.dtype != Q.dtype:
         raise ValueError("Q and K must have one dtype")
-    QO, qop, qot, qoh = _heads_out(None if out is None else out[0], Q, (n, heads, dim), "out's Q", stream)
-    KO, kop, kot, koh = _heads_out(None if out is None else out[1], K, (n, kv, dim), "out's K", stream)
-    _one_device(Q, K, positions, freqs, q_weight, k_weight, QO, KO)
+    q_out, k_out = (None, None) if out is None else out
+    at = _place(stream, Q, K, positions, freqs, q_weight, k_weight, q_out, k_out)
+    QO, qop, qot, qoh = _heads_out(q_out, Q, shape, "out's Q", stream)
+    KO, kop, kot, koh = _heads_out(k_out, K, (n, kv, dim), "out's K", stream)
     pp, fp, rot, qw, kw = _rotation(n, dim, positions, freqs, q_weight, k_weight)
     _check(load().mpq_mx_rotate(qp, qt, qh, kp, kt, kh, _mx_dtype(Q.dtype, "Q"), n, heads, kv, dim, pp, fp, rot,
-                                1 if interleaved else 0, qw, kw, float(eps), qop, qot, qoh, kop, kot, koh,
-                                _stream(stream)))
+                                1 if interleaved else 0, qw, kw, eps, qop, qot, qoh, kop, kot, koh, at))
     return QO, KO
 
 
@@ -694,11 +712,11 @@ def mx_route(logits: torch.Tensor, k: int, renorm: bool = True, stream=None, out
             if tuple(x.shape) != shape:
                 raise ValueError(f"out's {name} must be {shape} (got {tuple(x.shape)})")
             _dev(x, torch.float32 if x is weights else i32, f"out's {name}")
-        _one_device(*out)
-    _one_device(logits, workspace)
+        _place(stream, *out)
+    at = _place(stream, logits, workspace)
     wp, wn, _own = _space(workspace, lambda: mx_route_workspace(n, experts, k), stream, logits)
     _check(load().mpq_mx_route(lp, dt, n, experts, ld, k, 1 if renorm else 0, chosen.data_ptr(), weights.data_ptr(),
-                               order.data_ptr(), place.data_ptr(), offsets.data_ptr(), wp, wn, _stream(stream)))
+                               order.data_ptr(), place.data_ptr(), offsets.data_ptr(), wp, wn, at))
     return chosen, weights, order, place, offsets
 
 
@@ -726,9 +744,11 @@ def mx_experts(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, offse
     xp, xt, x_ld = _rows(X, "X")
     n, d = X.shape
     wide = -(-d // MX_ROW) * MX_ROW
-    if codes.dim() != 3 or codes.shape[2] != wide // 2 or tuple(scales.shape) != (*codes.shape[:2], wide // MX_BLOCK):
-        raise ValueError(f"weights: codes and scales do not hold rows of {d} of every expert")
-    experts, c = codes.shape[:2]
+    if codes.dim() != 3 or codes.shape[2] != wide // 2:
+        raise ValueError(f"weights: codes do not hold rows of {d} of every expert")
+    experts, c, _ = codes.shape
+    if scales.shape != (experts, c, wide // MX_BLOCK):
+        raise ValueError(f"weights: scales must be {(experts, c, wide // MX_BLOCK)} (got {tuple(scales.shape)})")
     if offsets.shape != (experts + 1,):
         raise ValueError(f"offsets must be {(experts + 1,)}")
     if order is not None and order.dim() != 1:
@@ -737,13 +757,12 @@ def mx_experts(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, offse
     if bias is not None and bias.shape != (experts, c):
         raise ValueError(f"bias must be {(experts, c)}")
     Y, yp, dt, ld = _rows_out(out, m, c, X.dtype if dtype is None else dtype, X, stream)
-    _one_device(X, codes, scales, offsets, order, bias, Y, workspace)
+    at = _place(stream, X, codes, scales, offsets, order, bias, Y, workspace)
     wp, wn, _own = _space(workspace, lambda: mx_experts_workspace(n, m, experts, c, d), stream, X)
     _check(load().mpq_mx_experts(xp, xt, n, x_ld, _dev(codes, torch.uint8, "codes"), _dev(scales, torch.uint8, "scales"),
                                  experts, c, d, _dev(offsets, torch.int32, "offsets"),
                                  None if order is None else _dev(order, torch.int32, "order") or _NO_BYTES, m, k,
-                                 None if bias is None else _dev(bias, torch.float32, "bias"), yp, dt, ld, wp, wn,
-                                 _stream(stream)))
+                                 None if bias is None else _dev(bias, torch.float32, "bias"), yp, dt, ld, wp, wn, at))
     return Y
 
 
@@ -765,9 +784,9 @@ def mx_combine(Y: torch.Tensor, place: torch.Tensor, weights: torch.Tensor, resi
         rp, _, r_ld = _rows(residual, "residual")
         rp = rp or None
     Z, zp, dt, ld = _rows_out(out, n, c, Y.dtype if dtype is None else dtype, Y, stream)
-    _one_device(Y, place, weights, residual, Z)
+    at = _place(stream, Y, place, weights, residual, Z)
     _check(load().mpq_mx_combine(yp, yt, m, c, y_ld, _dev(place, torch.int32, "place"),
-                                 _dev(weights, torch.float32, "weights"), n, k, rp, r_ld, zp, dt, ld, _stream(stream)))
+                                 _dev(weights, torch.float32, "weights"), n, k, rp, r_ld, zp, dt, ld, at))
     return Z
 
 
@@ -829,21 +848,21 @@ class MXCache:
         and V are quantized into the slots [n] (int64, as in write)."""
         if Q.dim() != 3:
             raise ValueError("Q must be 3-D [n, q_heads, head_dim]")
-        n, heads = Q.shape[:2]
+        n, heads, _ = Q.shape
         shape, held = (n, heads, self.head_dim), (n, self.kv_heads, self.head_dim)
-        qp, qt, qh = _heads(Q, shape, "Q")
-        kp, kt, kh = _heads(K, held, "K")
-        vp, vt, vh = _heads(V, held, "V")
+        qp, qt, qh = _head_rows(Q, shape, "Q")
+        kp, kt, kh = _head_rows(K, held, "K")
+        vp, vt, vh = _head_rows(V, held, "V")
         if K.dtype != Q.dtype or V.dtype != Q.dtype:
             raise ValueError("Q, K and V must have one dtype")
         if slots.shape != (n,):
             raise ValueError(f"slots must be {(n,)} (got {tuple(slots.shape)})")
+        at = _place(stream, Q, K, V, positions, slots, freqs, q_weight, k_weight, out, self.tensors[0])
         QO, qop, qot, qoh = _heads_out(out, Q, shape, "out", stream)
-        _one_device(Q, K, V, positions, slots, freqs, q_weight, k_weight, QO, self.tensors[0])
         pp, fp, rot, qw, kw = _rotation(n, self.head_dim, positions, freqs, q_weight, k_weight)
         _check(load().mpq_mx_cache_append(self._at, qp, qt, qh, kp, kt, kh, vp, vt, vh, _mx_dtype(Q.dtype, "Q"), n, heads,
                                           pp, _dev(slots, torch.int64, "slots"), fp, rot, 1 if interleaved else 0, qw, kw,
-                                          float(eps), qop, qot, qoh, _stream(stream)))
+                                          eps, qop, qot, qoh, at))
         return QO
 
     def read(self, slots: torch.Tensor, dtype=torch.float32, stream=None, out=None):

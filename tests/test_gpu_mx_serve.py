@@ -1,7 +1,7 @@
 """A serving step's operators (mpq_mx_plan, _rotate, _cache_append, _route,
 _experts, _combine) through the binding against the plain 64-bit implementation
-of mx_serve_ref: whole numbers equal, the cache's bytes those of the calls that
-append joins, other values within bounds that follow from fp32 sums.
+of mx_serve_ref: whole numbers equal, the cache's bytes those of heads turned and
+quantized in 64 bits, other values within bounds that follow from fp32 sums.
 
 Bounds, with u = 2^-24 and h half a step of the output's type (relative):
   turned heads  mx_serve_ref.turned's units, and h |y|.
@@ -15,6 +15,7 @@ there."""
 import numpy as np
 import pytest
 
+import mx_ref
 import mx_serve_ref as ref
 from gpu_util import say
 
@@ -217,36 +218,72 @@ def test_rotate_leaves_the_rest():
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("fmt", ["fp4", "fp8"])
 @pytest.mark.parametrize("n,heads,kv,dim,rot,page", [(1, 8, 2, 128, 128, 16), (5, 7, 1, 80, 40, 48), (37, 2, 2, 33, 10, 16),
-                                                     (130, 6, 3, 64, 64, 64), (20, 4, 4, 256, 128, 32), (3, 2, 1, 192, 0, 16)])
-def test_append_is_the_calls_that_it_joins(n, heads, kv, dim, rot, page, fmt, dtype):
+                                                     (130, 6, 3, 64, 64, 64), (20, 4, 4, 256, 128, 32), (3, 2, 1, 192, 0, 16),
+                                                     (9, 5, 5, 32, 32, 16), (12, 2, 1, 256, 256, 16)])
+def test_append(n, heads, kv, dim, rot, page, fmt, dtype):
     import torch
     from paper_2002_09049_amd import mpq
     rng = np.random.default_rng(n + dim)
     for interleaved, normed, layout in ((False, True, 0), (True, True, 1), (False, False, 2)):
         Q, K, V = (_heads(rng, n, h, dim, dtype, layout) for h in (heads, kv, kv))
-        K = K.clone() if layout != 1 else K
         K[n // 2, 0, dim // 2] = float("inf")
-        positions, freqs = _dev((np.arange(n) * 7919).astype(np.int32)), _dev(_freqs(rot))
-        w = [_dev(rng.uniform(0.5, 1.5, dim).astype(np.float32)) if normed else None for _ in "qk"]
+        V[0, kv - 1, 0] = float("nan")
+        positions, freqs = (np.arange(n) * 7919).astype(np.int32), _freqs(rot)
+        w = [rng.uniform(0.5, 1.5, dim).astype(np.float32) if normed else None for _ in "qk"]
+        on = [None if x is None else _dev(x) for x in w]
         pages = -(-n // page) + 2
         slots = rng.permutation(pages * page)[:n]
-        slots[n // 3] = -1
+        if n > 1:
+            slots[n // 3] = -1
         if n > 4:
             slots[4] = pages * page
-        slots = _dev(slots.astype(np.int64))
-        caches = [mpq.MXCache.empty(pages, page, kv, dim, fmt) for _ in range(2)]
-        for c in caches:
-            for t in c.tensors:
-                t.fill_(77)
-        q = caches[0].append(Q, K, V, positions, slots, freqs, *w, eps=1e-5, interleaved=interleaved)
-        want = mpq.mx_rotate(Q, K, positions, freqs, *w, eps=1e-5, interleaved=interleaved)[0]
-        k32 = mpq.mx_rotate(Q.float(), K.float(), positions, freqs, *w, eps=1e-5, interleaved=interleaved)[1]
-        caches[1].write(k32, V.float(), slots)
-        assert torch.equal(q, want)
-        for a, b in zip(*(c.tensors for c in caches)):
-            assert torch.equal(a, b)
-        again = caches[0].append(Q, K, V, positions, slots, freqs, *w, eps=1e-5, interleaved=interleaved, out=Q)
-        assert again is Q and torch.equal(Q, want)
+        cache = mpq.MXCache.empty(pages, page, kv, dim, fmt)
+        for t in cache.tensors:
+            t.fill_(77)
+        q = cache.append(Q, K, V, _dev(positions), _dev(slots.astype(np.int64)), _dev(freqs), *on, eps=1e-5,
+                         interleaved=interleaved)
+        assert torch.equal(q, mpq.mx_rotate(Q, K, _dev(positions), _dev(freqs), *on, eps=1e-5, interleaved=interleaved)[0])
+        live = (slots >= 0) & (slots < pages * page)
+        where, at = slots[live] // page, slots[live] % page
+        with np.errstate(invalid="ignore"):
+            turned, _ = ref.turned(_f64(K), positions, freqs, w[1], float(np.float32(1e-5)), interleaved)
+        for x, codes, scales in ((turned, cache.tensors[0], cache.tensors[2]), (_f64(V), cache.tensors[1], cache.tensors[3])):
+            c, sc = mx_ref.quantize(mx_ref.padded(x[live], 32), fmt)
+            codes, scales = codes.cpu().numpy(), scales.cpu().numpy()
+            got = codes[where, :, at]
+            # the elements' values, so a zero may have either sign: of a head that holds an
+            # infinity the others are products with 0, whose sign goes by their order
+            assert np.array_equal(mx_ref.values(mx_ref.unpack(got) if fmt == "fp4" else got, sc, fmt), mx_ref.values(c, sc, fmt),
+                                  equal_nan=True)
+            assert np.array_equal(scales[where, :, :, at], sc)
+            # the other places are as they were
+            codes[where, :, at], scales[where, :, :, at] = 77, 77
+            assert (codes == 77).all() and (scales == 77).all()
+        before = Q.clone()
+        again = cache.append(Q, K, V, _dev(positions), _dev(slots.astype(np.int64)), _dev(freqs), *on, eps=1e-5,
+                             interleaved=interleaved, out=Q)
+        assert again is Q and torch.equal(Q, q) and (n == 1 or (rot == 0 and not normed) or not torch.equal(Q, before))
+
+
+def test_append_rounds_once():
+    """A key just beside the border of two elements goes to its own side: in fp32
+    it would lie on the border, and fall to the even element."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    cache = mpq.MXCache.empty(1, 16, 1, 32, "fp8")
+    # 1.0625 lies half way from 1 to 1.125; 1.1875 from 1.125 to 1.25.  Weights in
+    # fp32 times keys in fp32: 1.0625 + 2^-26, and 1.1875 - 2^-26 or so, in fp64.
+    x = np.zeros((1, 1, 32), np.float32)
+    x[0, 0, :3] = 448.0, 1 + 2.0 ** -13, 1 - 2.0 ** -13
+    w = np.ones(32, np.float32)
+    w[1] = np.float32(1.0625) * np.float32(1 - 2.0 ** -13 + 2.0 ** -23)
+    w[2] = np.float32(1.1875) * np.float32(1 + 2.0 ** -13)
+    exact = x[0, 0].astype(np.float64) * w / np.sqrt((x[0, 0].astype(np.float64) ** 2).mean() + 1e-6)
+    t = [_dev(x) for _ in "qkv"]
+    cache.append(*t, _dev(np.zeros(1, np.int32)), _dev(np.zeros(1, np.int64)), _dev(np.zeros(0)), _dev(w), _dev(w))
+    c, s = mx_ref.quantize(exact[None, None], "fp8")
+    assert np.array_equal(cache.tensors[0][0, :, 0].cpu().numpy(), c[0]) and cache.tensors[2][0, 0, 0, 0].item() == s[0, 0, 0]
+    torch.cuda.synchronize()
 
 
 def test_rotate_past_32_bit_offsets():
@@ -368,11 +405,17 @@ def test_route_many_tokens():
 # ---------------------------------------------------------------- experts
 
 
-def _weights(rng, experts, c, d):
+def _drawn(rng, shape):
+    """As _activations, drawn on the device."""
     import torch
+    g = torch.Generator(device="cuda").manual_seed(int(rng.integers(2 ** 31)))
+    x = torch.randn(shape, generator=g, device="cuda") * torch.exp(torch.randn(shape[-1:], generator=g, device="cuda"))
+    return torch.where(torch.rand(shape, generator=g, device="cuda") < 0.02, torch.zeros_like(x), x)
+
+
+def _weights(rng, experts, c, d):
     from paper_2002_09049_amd import mpq
-    W = _dev(_activations(rng, (experts * c, d)) / np.sqrt(d), torch.float32)
-    codes, scales = mpq.mx_quantize(W)
+    codes, scales = mpq.mx_quantize(_drawn(rng, (experts * c, d)) / d ** 0.5)
     return codes.reshape(experts, c, -1), scales.reshape(experts, c, -1)
 
 
@@ -409,8 +452,8 @@ def _check_experts(rng, n, k, experts, c, d, dtype, out_dtype, counts=None, bias
     first = rng.integers(0, tail + 1)
     offsets = _dev(np.concatenate([[first], first + np.cumsum(counts)]).astype(np.int32))
     order = _dev(rng.permutation(m).astype(np.int32)) if gather else None
-    X = _activations(rng, (n, d))
-    X = _dev(np.concatenate([np.full((n, 1 * layout), 9.0), X, np.full((n, 2 * layout), 9.0)], 1), _dt(dtype))[:, layout:layout + d]
+    X = torch.full((n, d + 3 * layout), 9.0, dtype=_dt(dtype), device="cuda")[:, layout:layout + d]
+    X.copy_(_drawn(rng, (n, d)))
     b = _dev(rng.standard_normal((experts, c)).astype(np.float32)) if bias else None
     wide = torch.full((m + 2, c + 3 * layout), 3.5, dtype=_dt(out_dtype), device="cuda")
     Y = wide[1:1 + m, layout:layout + c]
@@ -439,6 +482,35 @@ def test_experts(n, k, experts, c, d, dtype):
     _check_experts(rng, n, k, experts, c, d, dtype, dtype)
     _check_experts(rng, n, k, experts, c, d, dtype, out, bias=True, layout=1, tail=min(3, n * k - 1))
     _check_experts(rng, n, 1, experts, c, d, dtype, dtype, bias=True, gather=False)
+
+
+WAYS = [
+    ("mx_experts_token_kernel", 1, 8, 16, 2500, 300), ("mx_experts_token_kernel", 4, 16, 40, 1100, 600),
+    ("mx_experts_few_kernel", 60, 1, 50, 300, 700), ("mx_experts_few_kernel", 60, 1, 50, 1030, 3000),
+    ("mx_experts_few_kernel", 100, 1, 9, 200, 8200), ("mx_experts_few_kernel", 4, 16, 64, 5001, 1000),
+    ("mx_experts_tile_kernel<2,1>", 600, 1, 21, 2050, 260), ("mx_experts_tile_kernel<2,1>", 700, 4, 70, 130, 2100),
+    ("mx_experts_tile_kernel<2,2>", 4000, 2, 40, 400, 1000), ("mx_experts_tile_kernel<2,2>", 3000, 1, 4, 700, 900),
+    ("mx_experts_stay_kernel", 4100, 2, 2, 2050, 200), ("mx_experts_stay_kernel", 8000, 3, 7, 1100, 1290),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kernel,n,k,experts,c,d", WAYS)
+def test_experts_by_every_kernel(kernel, n, k, experts, c, d, dtype):
+    """Sizes at which the rule takes each kernel, several tiles a workgroup where
+    those stay; all types of outputs, strided, with and without bias and order."""
+    from paper_2002_09049_amd import mpq
+    rng = np.random.default_rng(n + c + d)
+    for out, bias, gather, layout, tail in ((dtype, False, True, 0, 0), ("f32", True, True, 1, 2), ("bf16", True, n > 4, 0, 0),
+                                            ("f16", False, True, 1, 0)):
+        mpq.timing_enable(True)
+        try:
+            _check_experts(rng, n, k, experts, c, d, dtype, out, bias=bias, gather=gather, layout=layout, tail=tail)
+            names = {name for name, _ in mpq.timing_read()}
+        finally:
+            mpq.timing_enable(False)
+        if gather:
+            assert kernel in names, names
 
 
 @pytest.mark.parametrize("counts", [[0, 0, 0, 0], [0, 64, 0, 0], [16, 17, 15, 16], [1, 0, 62, 1], [0, 0, 0, 64], [3, 0, 0, 2]])

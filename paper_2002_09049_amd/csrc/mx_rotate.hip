@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kThreads) mx_rotate_kernel(MxRotate r, int sli
     __shared__ __align__(16) float weights[kWaves][2][kLanes * 8];
     __shared__ __align__(16) float rows[kWaves][kSwap ? 4 : kWave * 8];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int64_t item = (int64_t)blockIdx.x * kWaves + wave, token = quotient(item, slices);
+    const int64_t item = block_of(blockIdx.y) * kWaves + wave, token = quotient(item, slices);
     if (token >= r.n) return;
     // of the heads of all kinds
     const int first = (int)(item - token * slices) * per, last = first + per, keys = r.heads, values = keys + r.kv;
@@ -314,27 +314,27 @@ __global__ void __launch_bounds__(kThreads) mx_rotate_kernel(MxRotate r, int sli
 }
 
 template <int kFmt, bool kSwap, class T>
-hipError_t rotate_lanes(const MxRotate &r, int lanes, int slices, int per, unsigned blocks, hipStream_t s)
+hipError_t rotate_lanes(const MxRotate &r, int lanes, int slices, int per, dim3 grid, hipStream_t s)
 {
     auto kern = lanes == 4 ? mx_rotate_kernel<kFmt, 4, kSwap, T> : lanes == 8 ? mx_rotate_kernel<kFmt, 8, kSwap, T>
                 : lanes == 16 ? mx_rotate_kernel<kFmt, 16, kSwap, T> : mx_rotate_kernel<kFmt, 32, kSwap, T>;
-    hipLaunchKernelGGL(kern, dim3(blocks), dim3(kThreads), 0, s, r, slices, per);
+    hipLaunchKernelGGL(kern, grid, dim3(kThreads), 0, s, r, slices, per);
     return hipGetLastError();
 }
 
 template <int kFmt, class T>
-hipError_t rotate_swap(const MxRotate &r, int lanes, int slices, int per, unsigned blocks, hipStream_t s)
+hipError_t rotate_swap(const MxRotate &r, int lanes, int slices, int per, dim3 grid, hipStream_t s)
 {
-    if (!r.interleaved && r.rot == r.dim && r.dim == 8 * lanes) return rotate_lanes<kFmt, true, T>(r, lanes, slices, per, blocks, s);
-    return rotate_lanes<kFmt, false, T>(r, lanes, slices, per, blocks, s);
+    if (!r.interleaved && r.rot == r.dim && r.dim == 8 * lanes) return rotate_lanes<kFmt, true, T>(r, lanes, slices, per, grid, s);
+    return rotate_lanes<kFmt, false, T>(r, lanes, slices, per, grid, s);
 }
 
 template <int kFmt>
-hipError_t rotate_as(const MxRotate &r, int lanes, int slices, int per, unsigned blocks, hipStream_t s)
+hipError_t rotate_as(const MxRotate &r, int lanes, int slices, int per, dim3 grid, hipStream_t s)
 {
-    if (r.dtype == MPQ_F32) return rotate_swap<kFmt, float>(r, lanes, slices, per, blocks, s);
-    if (r.dtype == MPQ_F16) return rotate_swap<kFmt, _Float16>(r, lanes, slices, per, blocks, s);
-    return rotate_swap<kFmt, __bf16>(r, lanes, slices, per, blocks, s);
+    if (r.dtype == MPQ_F32) return rotate_swap<kFmt, float>(r, lanes, slices, per, grid, s);
+    if (r.dtype == MPQ_F16) return rotate_swap<kFmt, _Float16>(r, lanes, slices, per, grid, s);
+    return rotate_swap<kFmt, __bf16>(r, lanes, slices, per, grid, s);
 }
 
 }  // namespace
@@ -349,11 +349,11 @@ hipError_t launch_mx_rotate(const MxRotate &r, bool append, hipStream_t s)
     const int wanted = (int)std::min((int64_t)passes, std::max((int64_t)1, 4096 / r.n));
     const int each = (passes + wanted - 1) / wanted, slices = (passes + each - 1) / each;
     const int64_t blocks = (r.n * slices + kWaves - 1) / kWaves;
-    if (!launchable(blocks, kThreads)) return hipErrorInvalidValue;
+    const dim3 grid(grid_x(blocks), (unsigned)grid_rows(blocks));
     LaunchTimer timer(s, append ? "mx_append_kernel" : "mx_rotate_kernel");
-    if (!append) return rotate_as<-1>(r, lanes, slices, each * at_once, (unsigned)blocks, s);
-    return r.c.fmt == kFp4 ? rotate_as<kFp4>(r, lanes, slices, each * at_once, (unsigned)blocks, s)
-                           : rotate_as<kFp8>(r, lanes, slices, each * at_once, (unsigned)blocks, s);
+    if (!append) return rotate_as<-1>(r, lanes, slices, each * at_once, grid, s);
+    return r.c.fmt == kFp4 ? rotate_as<kFp4>(r, lanes, slices, each * at_once, grid, s)
+                           : rotate_as<kFp8>(r, lanes, slices, each * at_once, grid, s);
 }
 
 }  // namespace mpq

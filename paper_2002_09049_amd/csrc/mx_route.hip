@@ -1,12 +1,16 @@
 // Routing of tokens to experts (mpq_mx_route) and the sum of their experts'
 // rows (mpq_mx_combine).
 //
-// Routing: kLanes lanes have a token, a lane kEach consecutive experts, so a
-// wavefront chooses for up to four tokens at a time.  A logit is a key whose order as an
-// unsigned number is the logits' (NaN and -infinity the smallest, -0 equal to 0);
-// a 16-bit logit's key has the expert behind it, so that one maximum over the
-// lanes is a choice, the lowest index first; a 32-bit one takes a minimum over the
-// indexes that hold the maximum as well.  The softmax statistics are fp32.
+// Routing: kLanes lanes have a token, a lane kEach consecutive experts: a whole
+// wavefront for one while tokens are few (its steps are what takes time then), up
+// to four tokens a wavefront where they fill the GPU (instructions are).  A logit
+// is a key whose order as an unsigned number is the logits' (NaN and -infinity the
+// smallest, -0 equal to 0); a 16-bit logit's key has the expert behind it.  A round
+// of the choice is a maximum over the lanes; of 16-bit logits that is a choice, the
+// lowest index first, of 32-bit ones the first lane that holds it, and there the first
+// key, is.  The softmax statistics are fp32.  16384 tokens, 256 experts, 8 choices:
+// 9.0 us (bf16) and 12.2 us (fp32), by a wavefront a token 19.6 us; 200 tokens, 300
+// experts, 10 choices, fp32: 7.7 us by a wavefront a token, by half a one 18.5.
 //
 // The choices are then sorted by expert, tokens in order: of a workgroup's 64
 // tokens an expert has a mask of 64 bits in LDS (set by "or", whose order does not
@@ -25,9 +29,11 @@ namespace mpq {
 
 namespace {
 
-constexpr int kTokens = 64;       // of a workgroup
 constexpr int kThreads = 1024;
 constexpr int kMostExperts = 1024;
+
+// Tokens of a workgroup: a wavefront's each, or as many as a mask has bits.
+__host__ __device__ __forceinline__ int tokens_of(int64_t n) { return n > 64 && n <= 4096 ? 16 : 64; }
 
 // Bytes of a workgroup's counts.
 __host__ __device__ __forceinline__ int pitch_of(int experts) { return (experts + 3) / 4 * 4; }
@@ -53,7 +59,7 @@ __device__ __forceinline__ V lanes_reduce(V v, Op op)
     return v;
 }
 
-// The order of a logit's bits; 0 is below all.
+// The order of a logit; 0 is below all.
 __device__ __forceinline__ uint32_t order_of(float v)
 {
     if (!(v > -INFINITY)) return 0x007fffffu;   // -infinity's
@@ -83,10 +89,10 @@ __device__ __forceinline__ float value16_of(uint32_t order)
     return (float)v;
 }
 
-// A lane's keys of one type of logit.
+// A lane's keys.
 template <class T, int kLanes, int kEach>
 struct Keys {
-    static constexpr bool kWhole = std::is_same_v<T, float>;   // the key is the value alone
+    static constexpr bool kAlone = std::is_same_v<T, float>;   // a key is the order alone
     uint32_t key[kEach], most;
 
     __device__ __forceinline__ void largest()
@@ -110,7 +116,7 @@ struct Keys {
         }
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            if constexpr (kWhole) key[i] = order_of(v[i]);
+            if constexpr (kAlone) key[i] = order_of(v[i]);
             else key[i] = order16_of(v[i]) << 16 | (uint32_t)(0xffff - (first + i));
             if (first + i >= experts) key[i] = 0;
         }
@@ -118,22 +124,31 @@ struct Keys {
     }
     __device__ __forceinline__ float value(uint32_t k) const
     {
-        if constexpr (kWhole) return value_of(k);
+        if constexpr (kAlone) return value_of(k);
         else return value16_of<T>(k >> 16);
     }
-    // The largest of all lanes, taken out: its key, and its expert.
-    __device__ __forceinline__ uint32_t take(int first, int &expert)
+    // The largest of all lanes, taken out; its expert to *expert.
+    __device__ __forceinline__ uint32_t take(int first, uint16_t *expert)
     {
         const uint32_t best = lanes_reduce<kLanes>(most, MaxOp());
-        if constexpr (kWhole) {
-            int at = kMostExperts;
+        if constexpr (kAlone) {
+            const unsigned long long have = __ballot(most == best);
+            unsigned first_lane;
+            if constexpr (kLanes == 64) first_lane = (unsigned)__builtin_ctzll(have);
+            else first_lane = (unsigned)__builtin_ctz((uint32_t)(have >> (threadIdx.x % kWave / kLanes * kLanes)));
+            const bool winner = threadIdx.x % kLanes == first_lane;
+            bool open = winner;
+            int at = 0;
 #pragma unroll
-            for (int i = kEach - 1; i >= 0; --i) at = key[i] == best ? first + i : at;
-            expert = lanes_reduce<kLanes>(at, MinOp());
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) key[i] = first + i == expert ? 0u : key[i];
+            for (int i = 0; i < kEach; ++i) {
+                const bool taken = open && key[i] == best;
+                at = taken ? i : at;
+                key[i] = taken ? 0u : key[i];
+                open = open && !taken;
+            }
+            if (winner) *expert = (uint16_t)(first + at);
         } else {
-            expert = 0xffff - (int)(best & 0xffff);
+            if (first == 0) *expert = (uint16_t)(0xffff - (best & 0xffff));
 #pragma unroll
             for (int i = 0; i < kEach; ++i) key[i] = key[i] == best ? 0u : key[i];
         }
@@ -171,20 +186,21 @@ __device__ __forceinline__ void prefix_counts(uint32_t *counts, int experts)
 
 // kAlone: this workgroup has all tokens.
 template <int kLanes, int kEach, bool kAlone, class T>
-__global__ void __launch_bounds__(kThreads) mx_choose_kernel(MxRoute r)
+__global__ void __launch_bounds__(kThreads) mx_choose_kernel(MxRoute r, int of_block)
 {
     __shared__ unsigned long long masks[kMostExperts];
     __shared__ uint32_t counts[kMostExperts + 1];
+    __shared__ uint16_t taken[kThreads];   // a lane each: its token's choice of that number
     const int lane = threadIdx.x % kLanes, first = lane * kEach;
+    uint16_t *choices = taken + (threadIdx.x - lane);
     for (int e = threadIdx.x; e < r.experts; e += kThreads) masks[e] = 0;
     __syncthreads();
-    const int64_t token0 = (int64_t)blockIdx.x * kTokens;
-    const int tokens = (int)min((int64_t)kTokens, r.n - token0);
+    const int64_t token0 = (int64_t)blockIdx.x * of_block;
+    const int tokens = (int)min((int64_t)of_block, r.n - token0);
     for (int t = threadIdx.x / kLanes; t < tokens; t += kThreads / kLanes) {
         Keys<T, kLanes, kEach> keys;
         keys.load((const T *)r.logits + (token0 + t) * r.ld, first, r.experts);
         float all = 0.0f, top = 0.0f, mine = 0.0f;
-        int chosen = 0;
         if (!r.renorm) {
             top = keys.value(lanes_reduce<kLanes>(keys.most, MaxOp()));
 #pragma unroll
@@ -192,22 +208,21 @@ __global__ void __launch_bounds__(kThreads) mx_choose_kernel(MxRoute r)
             all = lanes_reduce<kLanes>(all, SumOp());
         }
         for (int j = 0; j < r.k; ++j) {
-            int expert;
-            const float v = keys.value(keys.take(first, expert));
+            const float v = keys.value(keys.take(first, choices + j));
             if (j == 0) top = v;
-            if (lane == j) {
-                chosen = expert;
-                mine = v;
-            }
+            if (lane == j) mine = v;
         }
         mine = lane < r.k ? part_of(mine, top) : 0.0f;
         if (r.renorm) all = lanes_reduce<kLanes>(mine, SumOp());
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (lane < r.k) {
+            const int chosen = choices[lane];
             const int64_t at = (token0 + t) * r.k + lane;
             r.chosen[at] = chosen;
             r.weights[at] = all > 0.0f ? mine / all : 0.0f;
             atomicOr(&masks[chosen], 1ull << t);
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
     __syncthreads();
     if constexpr (kAlone) {
@@ -244,12 +259,14 @@ __global__ void __launch_bounds__(kThreads) mx_sum_kernel(const uint8_t *counts,
     const int pitch = pitch_of(experts);
     int32_t sum = 0;
     if (e < experts)
+#pragma unroll 8
         for (int b = from; b < end; ++b) sum += counts[(int64_t)b * pitch + e];
     sums[run][column] = sum;
     __syncthreads();
     if (e >= experts) return;
     int32_t before = 0;
     for (int i = 0; i < run; ++i) before += sums[i][column];
+#pragma unroll 8
     for (int b = from; b < end; ++b) {
         to[(int64_t)b * experts + e] = before;
         before += counts[(int64_t)b * pitch + e];
@@ -262,7 +279,7 @@ __global__ void __launch_bounds__(kThreads) mx_sum_kernel(const uint8_t *counts,
 // hold up to 1023 rows of 64.
 constexpr int kMostAdded = 1023;
 template <bool kSummed>
-__global__ void __launch_bounds__(kThreads) mx_place_kernel(MxRoute r, int blocks)
+__global__ void __launch_bounds__(kThreads) mx_place_kernel(MxRoute r, int blocks, int of_block)
 {
     __shared__ uint32_t counts[kMostExperts + 1], before[kMostExperts];
     if constexpr (kSummed) {
@@ -313,8 +330,8 @@ __global__ void __launch_bounds__(kThreads) mx_place_kernel(MxRoute r, int block
     prefix_counts(counts, r.experts);
     if (blockIdx.x == 0)
         for (int e = threadIdx.x; e <= r.experts; e += kThreads) r.offsets[e] = (int32_t)counts[e];
-    const int64_t token0 = (int64_t)blockIdx.x * kTokens;
-    const int tokens = (int)min((int64_t)kTokens, r.n - token0);
+    const int64_t token0 = (int64_t)blockIdx.x * of_block;
+    const int tokens = (int)min((int64_t)of_block, r.n - token0);
     for (int i = threadIdx.x; i < tokens * r.k; i += kThreads) {
         const int64_t at = token0 * r.k + i;
         const int e = r.chosen[at];
@@ -324,32 +341,46 @@ __global__ void __launch_bounds__(kThreads) mx_place_kernel(MxRoute r, int block
     }
 }
 
+// A wavefront a token.
 template <bool kAlone, class T>
-hipError_t choose_as(const MxRoute &r, unsigned blocks, hipStream_t s)
+auto choose_wide(int experts)
 {
-    // a choice is kept by the lane of its number
-    auto kern = r.k > 16           ? mx_choose_kernel<64, 16, kAlone, T>
-                : r.experts <= 16  ? mx_choose_kernel<16, 1, kAlone, T>
-                : r.experts <= 64  ? mx_choose_kernel<16, 4, kAlone, T>
-                : r.experts <= 128 ? mx_choose_kernel<16, 8, kAlone, T>
-                : r.experts <= 256 ? mx_choose_kernel<16, 16, kAlone, T>
-                : r.experts <= 512 ? mx_choose_kernel<32, 16, kAlone, T>
-                                   : mx_choose_kernel<64, 16, kAlone, T>;
-    hipLaunchKernelGGL(kern, dim3(blocks), dim3(kThreads), 0, s, r);
+    return experts <= 64    ? mx_choose_kernel<64, 1, kAlone, T>
+           : experts <= 128 ? mx_choose_kernel<64, 2, kAlone, T>
+           : experts <= 256 ? mx_choose_kernel<64, 4, kAlone, T>
+           : experts <= 512 ? mx_choose_kernel<64, 8, kAlone, T>
+                            : mx_choose_kernel<64, 16, kAlone, T>;
+}
+
+template <class T>
+hipError_t choose_as(const MxRoute &r, int64_t blocks, hipStream_t s)
+{
+    const int of_block = tokens_of(r.n);
+    auto kern = blocks <= 1 ? choose_wide<true, T>(r.experts) : choose_wide<false, T>(r.experts);
+    if (of_block == 64 && blocks > 1 && r.k <= 16) {   // a choice is kept by the lane of its number
+        if (r.experts <= 16) kern = mx_choose_kernel<16, 1, false, T>;
+        else if (r.experts <= 64) kern = mx_choose_kernel<16, 4, false, T>;
+        else if (r.experts <= 128) kern = mx_choose_kernel<16, 8, false, T>;
+        else if (r.experts <= 256) kern = mx_choose_kernel<16, 16, false, T>;
+        else if (r.experts <= 512) kern = mx_choose_kernel<32, 16, false, T>;
+    }
+    hipLaunchKernelGGL(kern, dim3((unsigned)std::max((int64_t)1, blocks)), dim3(kThreads), 0, s, r, of_block);
     return hipGetLastError();
 }
 
-template <bool kAlone>
-hipError_t choose(const MxRoute &r, unsigned blocks, hipStream_t s)
+hipError_t choose(const MxRoute &r, int64_t blocks, hipStream_t s)
 {
     LaunchTimer timer(s, "mx_choose_kernel");
-    if (r.dtype == MPQ_F32) return choose_as<kAlone, float>(r, blocks, s);
-    if (r.dtype == MPQ_F16) return choose_as<kAlone, _Float16>(r, blocks, s);
-    return choose_as<kAlone, __bf16>(r, blocks, s);
+    if (r.dtype == MPQ_F32) return choose_as<float>(r, blocks, s);
+    if (r.dtype == MPQ_F16) return choose_as<_Float16>(r, blocks, s);
+    return choose_as<__bf16>(r, blocks, s);
 }
 
-// Whether the workgroups add up the counts themselves: while all of them
-// together read few.
+int64_t blocks_of(int64_t n) { return (n + tokens_of(n) - 1) / tokens_of(n); }
+
+// Whether the workgroups add up the counts themselves: while all of them together
+// read few (16384 tokens, 256 experts: 6.4 us; with mx_sum_kernel before, which has
+// to be waited for, 4.4 + 4.2; 65536 tokens, 128 experts by that 6.3 + 7.0).
 bool adds_inside(int64_t blocks, int64_t experts)
 {
     return blocks <= kMostAdded && blocks * blocks * pitch_of((int)experts) <= (int64_t)32 << 20;
@@ -396,7 +427,7 @@ hipError_t combine_as(const MxCombine &q, int chunks, dim3 grid, hipStream_t s)
 
 size_t mx_route_bytes(int64_t n, int64_t experts)
 {
-    const int64_t blocks = (n + kTokens - 1) / kTokens;
+    const int64_t blocks = blocks_of(n);
     if (blocks <= 1) return 0;
     return count_bytes(blocks, experts)
            + (adds_inside(blocks, experts) ? 0 : (size_t)((blocks + 1) * experts) * sizeof(int32_t));
@@ -404,15 +435,16 @@ size_t mx_route_bytes(int64_t n, int64_t experts)
 
 hipError_t launch_mx_route(MxRoute r, void *space, hipStream_t s)
 {
-    const unsigned blocks = (unsigned)((r.n + kTokens - 1) / kTokens);
-    if (blocks <= 1) return choose<true>(r, 1, s);
+    const int64_t blocks = blocks_of(r.n);
+    const int of_block = tokens_of(r.n);
+    if (blocks <= 1) return choose(r, blocks, s);
     r.counts = (uint8_t *)space;
     r.sums = (int32_t *)((uint8_t *)space + count_bytes(blocks, r.experts));
-    hipError_t e = choose<false>(r, blocks, s);
+    hipError_t e = choose(r, blocks, s);
     if (e != hipSuccess) return e;
     if (adds_inside(blocks, r.experts)) {
         LaunchTimer timer(s, "mx_place_kernel");
-        hipLaunchKernelGGL(mx_place_kernel<false>, dim3(blocks), dim3(kThreads), 0, s, r, (int)blocks);
+        hipLaunchKernelGGL(mx_place_kernel<false>, dim3((unsigned)blocks), dim3(kThreads), 0, s, r, (int)blocks, of_block);
         return hipGetLastError();
     }
     {
@@ -423,7 +455,7 @@ hipError_t launch_mx_route(MxRoute r, void *space, hipStream_t s)
         if (e != hipSuccess) return e;
     }
     LaunchTimer timer(s, "mx_place_kernel");
-    hipLaunchKernelGGL(mx_place_kernel<true>, dim3(blocks), dim3(kThreads), 0, s, r, (int)blocks);
+    hipLaunchKernelGGL(mx_place_kernel<true>, dim3((unsigned)blocks), dim3(kThreads), 0, s, r, (int)blocks, of_block);
     return hipGetLastError();
 }
 

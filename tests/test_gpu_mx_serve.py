@@ -307,6 +307,21 @@ def test_rotate_past_32_bit_offsets():
     torch.cuda.empty_cache()
 
 
+def test_rotate_past_one_launch_dimension():
+    """More workgroups than go in one row of a grid: 2^22 tokens and some."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    torch.manual_seed(0)
+    n = 2 ** 22 + 9
+    x = torch.randn((n, 2, 8), device="cuda").bfloat16()
+    p = torch.arange(n, device="cuda", dtype=torch.int32)
+    f = _dev(_freqs(8))
+    q, k = mpq.mx_rotate(x[:, :1], x[:, 1:], p, f)
+    for part in (slice(0, 100), slice(2 ** 22 - 50, n)):
+        want = mpq.mx_rotate(x[part, :1], x[part, 1:], p[part].contiguous(), f)
+        assert torch.equal(q[part], want[0]) and torch.equal(k[part], want[1])
+
+
 def test_rotate_and_append_many_tokens():
     """More tokens and heads than one row of anything; against torch in 64 bits."""
     import torch

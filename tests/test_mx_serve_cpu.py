@@ -96,12 +96,12 @@ def test_route_refusals(mpq):
            dict(experts=1025, ld=1025), dict(ld=7), dict(k=0), dict(k=9), dict(experts=100, ld=100, k=65), dict(renorm=2),
            dict(chosen=None), dict(chosen=66), dict(weights=None), dict(weights=66), dict(order=None), dict(order=66),
            dict(place=None), dict(place=66), dict(offsets=None), dict(offsets=66), dict(space=68, nbytes=1 << 20),
-           dict(n=65, space=64, nbytes=15)]
+           dict(n=65, space=64, nbytes=47)]
     _refused(mpq, lib.mpq_mx_route, ok, bad)
     for args in ((-1, 8, 2), (3, 0, 1), (3, 1025, 1), (3, 8, 9), (3, 8, 0)):
         assert lib.mpq_mx_route_workspace(*args) == mpq.MPQ_ERR_INVALID_ARG
-    # a byte for every expert and 64 tokens, and for many tokens their sums; one group of 64 needs none
-    assert mpq.mx_route_workspace(64, 8, 2) == 0 and mpq.mx_route_workspace(65, 8, 2) == 2 * 8
+    # a byte for every expert and 16 or 64 tokens, and for many tokens their sums; 64 tokens need none
+    assert mpq.mx_route_workspace(64, 8, 2) == 0 and mpq.mx_route_workspace(65, 8, 2) == 48
     assert mpq.mx_route_workspace(1 << 20, 8, 2) == 16384 * 8 + 16385 * 8 * 4
 
 

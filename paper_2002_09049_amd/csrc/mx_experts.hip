@@ -338,14 +338,16 @@ __global__ void __launch_bounds__(256) mx_experts_stay_kernel(MxExperts g)
                 else meet<kLoads>();
                 then.read(lds_scales[q == 3 ? (four + 1) % 2 : four % 2][(q + 1) % 4], wm, wn, r, h);
                 __builtin_amdgcn_sched_barrier(0);
-                multiply_operands<0>(first, now, acc, [&](int i) {
-                    second.read(i, ring(q), 1, wm, wn, r, h);
-                    load(st + 3, (q + 3) % 4, i);
-                    if (q == 2) place_scales(four + 1, i);
+                multiply_spread<0>(first, now, acc, [&](int i, int j) {
+                    if (j == 0) second.read_one<false>(i, ring(q), 1, wm, wn, r, h);
+                    if (j == 1) second.read_one<true>(i, ring(q), 1, wm, wn, r, h);
+                    if (j == 2) load(st + 3, (q + 3) % 4, i);
+                    if (j == 3 && q == 2) place_scales(four + 1, i);
                 });
-                multiply_operands<1>(second, now, acc, [&](int i) {
-                    first.read(i, ring((q + 1) % 4), 0, wm, wn, r, h);
-                    load(st + 3, (q + 3) % 4, kTM + i);
+                multiply_spread<1>(second, now, acc, [&](int i, int j) {
+                    if (j == 0) first.read_one<false>(i, ring((q + 1) % 4), 0, wm, wn, r, h);
+                    if (j == 1) first.read_one<true>(i, ring((q + 1) % 4), 0, wm, wn, r, h);
+                    if (j == 2) load(st + 3, (q + 3) % 4, kTM + i);
                 });
                 if (q == 2) {
                     pin();

@@ -345,6 +345,14 @@ struct Operands {
         a[i] = *(const u32x4 *)(stage + (wm + 32 * i + r) * kStageBytes + at);
         if (i < kTN) b[i] = *(const u32x4 *)(stage + (64 * kTM + wn + 32 * i + r) * kStageBytes + at);
     }
+    // one of the two: W's, the tokens'
+    template <bool kTokens>
+    __device__ __forceinline__ void read_one(int i, const uint8_t *stage, int step, int wm, int wn, int r, int h)
+    {
+        const int at = ((2 * h + step) ^ (r / 4 % 4)) * 16;
+        if constexpr (kTokens) b[i] = *(const u32x4 *)(stage + (64 * kTM + wn + 32 * i + r) * kStageBytes + at);
+        else a[i] = *(const u32x4 *)(stage + (wm + 32 * i + r) * kStageBytes + at);
+    }
 };
 
 // The scales of the lane's rows for one stage, two bytes (a step each) a row
@@ -376,6 +384,17 @@ struct Scales {
     }
 };
 
+// Product of row tiles i and j of a step kS.
+template <int kS, int kTM, int kTN>
+__device__ __forceinline__ f32x16 multiply_pair(const Operands<kTM, kTN> &o, const Scales<kTM, kTN> &sc, int i, int j, f32x16 acc)
+{
+    // byte of the word: the odd tile's pair is its upper half
+    if (i % 2 == 0 && j % 2 == 0) return multiply_tile<kS, kS>(o.a[i], sc.a[i / 2], o.b[j], sc.b[j / 2], acc);
+    if (i % 2 == 0) return multiply_tile<kS, kS + 2>(o.a[i], sc.a[i / 2], o.b[j], sc.b[j / 2], acc);
+    if (j % 2 == 0) return multiply_tile<kS + 2, kS>(o.a[i], sc.a[i / 2], o.b[j], sc.b[j / 2], acc);
+    return multiply_tile<kS + 2, kS + 2>(o.a[i], sc.a[i / 2], o.b[j], sc.b[j / 2], acc);
+}
+
 // The products of one step; after(i) runs behind those of row tile i.
 template <int kS, int kTM, int kTN, class After>
 __device__ __forceinline__ void multiply_operands(const Operands<kTM, kTN> &o, const Scales<kTM, kTN> &sc,
@@ -384,21 +403,29 @@ __device__ __forceinline__ void multiply_operands(const Operands<kTM, kTN> &o, c
 #pragma unroll
     for (int i = 0; i < kTM; ++i) {
 #pragma unroll
-        for (int j = 0; j < kTN; ++j) {
-            // byte of the word: the odd tile's pair is its upper half
-            if (i % 2 == 0 && j % 2 == 0)
-                acc[i][j] = multiply_tile<kS, kS>(o.a[i], sc.a[i / 2], o.b[j], sc.b[j / 2], acc[i][j]);
-            else if (i % 2 == 0)
-                acc[i][j] = multiply_tile<kS, kS + 2>(o.a[i], sc.a[i / 2], o.b[j], sc.b[j / 2], acc[i][j]);
-            else if (j % 2 == 0)
-                acc[i][j] = multiply_tile<kS + 2, kS>(o.a[i], sc.a[i / 2], o.b[j], sc.b[j / 2], acc[i][j]);
-            else
-                acc[i][j] = multiply_tile<kS + 2, kS + 2>(o.a[i], sc.a[i / 2], o.b[j], sc.b[j / 2], acc[i][j]);
-        }
+        for (int j = 0; j < kTN; ++j) acc[i][j] = multiply_pair<kS>(o, sc, i, j, acc[i][j]);
         __builtin_amdgcn_sched_barrier(0);
         after(i);
         __builtin_amdgcn_sched_barrier(0);
     }
+}
+
+// The same with after(i, j) behind each product: what it issues has the time of one
+// product, so that little work behind every one hides where much behind every
+// fourth does not (a stage of 256 by 256 tiles 1540 cycles, so XX).
+template <int kS, int kTM, int kTN, class After>
+__device__ __forceinline__ void multiply_spread(const Operands<kTM, kTN> &o, const Scales<kTM, kTN> &sc,
+                                                f32x16 (&acc)[kTM][kTN], After after)
+{
+#pragma unroll
+    for (int i = 0; i < kTM; ++i)
+#pragma unroll
+        for (int j = 0; j < kTN; ++j) {
+            acc[i][j] = multiply_pair<kS>(o, sc, i, j, acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+            after(i, j);
+            __builtin_amdgcn_sched_barrier(0);
+        }
 }
 
 // The sums to Y.  Register v of a tile is row 8 (v / 4) + 4 h + v % 4 of W, token

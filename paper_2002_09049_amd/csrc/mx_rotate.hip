@@ -32,7 +32,6 @@ namespace mpq {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
-constexpr int kMostHalf = 128;   // pairs of a head
 
 // The sum over the kLanes lanes of a row.
 template <int kLanes, class R>
@@ -177,9 +176,9 @@ struct Factors {
     }
 };
 
-// A wavefront's rows of one kind, from `lo` below `hi`, kHeads at a time; the
-// loads of the next kDepth of a lane are in flight.
-template <int kDepth, int kHeads, class T>
+// A lane's rows of one kind, every kStep-th from `lo` below `hi`; the loads of the
+// next kDepth are in flight.
+template <int kDepth, int kStep, class T>
 struct Rows {
     const T *from;
     int64_t stride;
@@ -195,15 +194,15 @@ struct Rows {
         live = dim - j;
 #pragma unroll
         for (int i = 0; i < kDepth; ++i)
-            if (lo + i * kHeads < hi) next[i] = load_eight(from + (lo + i * kHeads) * stride, live);
+            if (lo + i * kStep < hi) next[i] = load_eight(from + (lo + i * kStep) * stride, live);
     }
     template <class Body>
     __device__ __forceinline__ void each(Body body)
     {
-        for (int h = lo; h < hi; h += kDepth * kHeads) {
+        for (int h = lo; h < hi; h += kDepth * kStep) {
 #pragma unroll
             for (int i = 0; i < kDepth; ++i) {
-                const int at = h + i * kHeads, more = at + kDepth * kHeads;
+                const int at = h + i * kStep, more = at + kDepth * kStep;
                 if (at >= hi) break;
                 const Eight<T> now = next[i];
                 if (more < hi) next[i] = load_eight(from + more * stride, live);
@@ -215,30 +214,44 @@ struct Rows {
     }
 };
 
-// kFmt -1: keys go to KO, values are not looked at.
-template <int kFmt, int kLanes, bool kSwap, class T>
+// kFmt -1: keys go to KO, values are not looked at.  kMany: the rows of a wavefront
+// at a time are of as many tokens, each with all its heads; else of one.
+template <int kFmt, int kLanes, bool kSwap, bool kMany, class T>
 __global__ void __launch_bounds__(kThreads) mx_rotate_kernel(MxRotate r, int slices, int per)
 {
-    constexpr int kHeads = kWave / kLanes, kDepth = sizeof(T) == 4 ? 2 : 4;
+    constexpr int kRows = kWave / kLanes, kDepth = sizeof(T) == 4 ? 2 : 4;
+    constexpr int kTokens = kMany ? kRows : 1, kStep = kMany ? 1 : kRows;
+    constexpr int kPairs = kTokens * kLanes * 4;   // angles of the wavefront
+    constexpr int kTimes = (kPairs + kWave - 1) / kWave;
     using Short = std::conditional_t<std::is_same_v<T, float>, double, float>;
-    __shared__ __align__(16) double table[kWaves][2][kMostHalf];
+    __shared__ __align__(16) double table[kWaves][2][kPairs];
     __shared__ __align__(16) float weights[kWaves][2][kLanes * 8];
     __shared__ __align__(16) float rows[kWaves][kSwap ? 4 : kWave * 8];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int64_t item = block_of(blockIdx.y) * kWaves + wave, token = quotient(item, slices);
-    if (token >= r.n) return;
-    // of the heads of all kinds
-    const int first = (int)(item - token * slices) * per, last = first + per, keys = r.heads, values = keys + r.kv;
-    const int half = r.rot / 2, group = lane / kLanes, j = lane % kLanes * 8, live = r.dim - j;
-    double *cosines = table[wave][0], *sines = table[wave][1];
+    const int group = lane / kLanes, j = lane % kLanes * 8, live = r.dim - j;
+    const int64_t item = block_of(blockIdx.y) * kWaves + wave, share = quotient(item, slices), token0 = share * kTokens;
+    if (token0 >= r.n) return;
+    const int64_t token = kMany ? min(token0 + group, r.n - 1) : token0;
+    // of the heads of all kinds; none behind the last token
+    const int own = kMany ? 0 : group, slice = (int)(item - share * slices) * per, keys = r.heads, values = keys + r.kv;
+    const int last = !kMany || token0 + group < r.n ? slice + per : 0;
+    const int half = r.rot / 2;
+    double *const angles_c = table[wave][0], *const angles_s = table[wave][1];
+    const double *cosines = angles_c + (kMany ? group * half : 0), *sines = angles_s + (kMany ? group * half : 0);
     float *row = rows[wave] + (kSwap ? 0 : group * kLanes * 8);
     const Pairs pairs = {half, j, !kSwap && r.interleaved != 0};
     const double inverse_dim = 1.0 / (double)r.dim;
 
-    const double position = half > 0 ? (double)r.positions[token] : 0.0;
-    double freqs[2];
+    // angle `lane` and every 64th: of token token0 + angle / half
+    double turns[kTimes];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) freqs[i] = lane + i * kWave < half ? r.freqs[lane + i * kWave] : 0.0;
+    for (int i = 0; i < kTimes; ++i) {
+        const int angle = lane + i * kWave;
+        turns[i] = 0.0;
+        if (angle >= kTokens * half) continue;
+        const int t = kMany ? (int)small_quotient((uint32_t)angle, 1.0f / (float)half) : 0;
+        turns[i] = (double)r.positions[min(token0 + t, r.n - 1)] * r.freqs[angle - t * half];
+    }
     float wq[4], wk[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -247,23 +260,24 @@ __global__ void __launch_bounds__(kThreads) mx_rotate_kernel(MxRotate r, int sli
         wk[i] = r.kw && at < r.dim ? r.kw[at] : 0.0f;
     }
     int64_t slot = -1;
-    if (kFmt >= 0 && last > keys) slot = r.slots[token];
+    if (kFmt >= 0 && slice + per > keys) slot = r.slots[token];
     __builtin_amdgcn_sched_barrier(0);
-    Rows<kDepth, kHeads, T> q;
-    q.start(r.Q, token * r.q_tok, r.q_head, first + group, min(last, keys), j, r.dim);
-    Rows<2, kHeads, T> k, v;
-    k.start(r.K, token * r.k_tok, r.k_head, max(first - keys, 0) + group, min(last - keys, r.kv), j, r.dim);
+    Rows<kDepth, kStep, T> q;
+    q.start(r.Q, token * r.q_tok, r.q_head, slice + own, min(last, keys), j, r.dim);
+    Rows<2, kStep, T> k, v;
+    k.start(r.K, token * r.k_tok, r.k_head, max(slice - keys, 0) + own, min(last - keys, r.kv), j, r.dim);
     if constexpr (kFmt >= 0)
-        v.start(r.V, token * r.v_tok, r.v_head, max(first - values, 0) + group, min(last - values, r.kv), j, r.dim);
+        v.start(r.V, token * r.v_tok, r.v_head, max(slice - values, 0) + own, min(last - values, r.kv), j, r.dim);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if (lane + i * kWave >= half) break;
-        const double turns = position * freqs[i] * 0.15915494309189533577;
+    for (int i = 0; i < kTimes; ++i) {
+        const int angle = lane + i * kWave;
+        if (angle >= kTokens * half) break;
+        const double t = turns[i] * 0.15915494309189533577;
         double s, c;
-        sincospi(2.0 * (turns - rint(turns)), &s, &c);
-        cosines[lane + i * kWave] = c;
-        sines[lane + i * kWave] = s;
+        sincospi(2.0 * (t - rint(t)), &s, &c);
+        angles_c[angle] = c;
+        angles_s[angle] = s;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -273,7 +287,7 @@ __global__ void __launch_bounds__(kThreads) mx_rotate_kernel(MxRotate r, int sli
         weights[wave][1][at] = wk[i];
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (first < keys) {
+    if (slice < keys) {
         const bool normed = r.qw != nullptr;
         Factors<Short> f;
         f.set(normed, weights[wave][0], pairs, r.dim, cosines, sines);
@@ -283,7 +297,7 @@ __global__ void __launch_bounds__(kThreads) mx_rotate_kernel(MxRotate r, int sli
             if (live > 0) store8<false>(to + h * r.qo_head, live, x);
         });
     }
-    if (last <= keys) return;
+    if (slice + per <= keys) return;
     const bool normed = r.kw != nullptr;
     if constexpr (kFmt < 0) {
         Factors<Short> f;
@@ -294,12 +308,14 @@ __global__ void __launch_bounds__(kThreads) mx_rotate_kernel(MxRotate r, int sli
             if (live > 0) store8<false>(to + h * r.ko_head, live, x);
         });
     } else {
-        if (slot < 0 || slot >= r.c.n_pages * r.c.page) return;
-        int64_t page;
-        int at;
-        find(r.c, slot, page, at);
+        // (the same in all lanes, and in scalar registers, but with many tokens)
+        const bool held = slot >= 0 && slot < r.c.n_pages * r.c.page;
+        if (!kMany && !held) return;
+        int64_t page = 0;
+        int at = 0;
+        if (!kMany || held) find(r.c, slot, page, at);
         const auto keep = [&](int h, const float (&x)[8], uint8_t *codes, uint8_t *scales) {
-            if (j >= r.c.nb * kMxBlock) return;
+            if ((kMany && !held) || j >= r.c.nb * kMxBlock) return;
             const int64_t ph = page * r.c.heads + h;
             write8<kFmt>(x, codes + code_at<kFmt>(r.c, ph, at, j), scales + scale_at(r.c, ph, at, j), j % kMxBlock == 0);
         };
@@ -313,28 +329,31 @@ __global__ void __launch_bounds__(kThreads) mx_rotate_kernel(MxRotate r, int sli
     }
 }
 
-template <int kFmt, bool kSwap, class T>
+template <int kFmt, bool kSwap, bool kMany, class T>
 hipError_t rotate_lanes(const MxRotate &r, int lanes, int slices, int per, dim3 grid, hipStream_t s)
 {
-    auto kern = lanes == 4 ? mx_rotate_kernel<kFmt, 4, kSwap, T> : lanes == 8 ? mx_rotate_kernel<kFmt, 8, kSwap, T>
-                : lanes == 16 ? mx_rotate_kernel<kFmt, 16, kSwap, T> : mx_rotate_kernel<kFmt, 32, kSwap, T>;
+    auto kern = lanes == 4 ? mx_rotate_kernel<kFmt, 4, kSwap, kMany, T> : lanes == 8 ? mx_rotate_kernel<kFmt, 8, kSwap, kMany, T>
+                : lanes == 16 ? mx_rotate_kernel<kFmt, 16, kSwap, kMany, T> : mx_rotate_kernel<kFmt, 32, kSwap, kMany, T>;
     hipLaunchKernelGGL(kern, grid, dim3(kThreads), 0, s, r, slices, per);
     return hipGetLastError();
 }
 
 template <int kFmt, class T>
-hipError_t rotate_swap(const MxRotate &r, int lanes, int slices, int per, dim3 grid, hipStream_t s)
+hipError_t rotate_swap(const MxRotate &r, int lanes, bool many, int slices, int per, dim3 grid, hipStream_t s)
 {
-    if (!r.interleaved && r.rot == r.dim && r.dim == 8 * lanes) return rotate_lanes<kFmt, true, T>(r, lanes, slices, per, grid, s);
-    return rotate_lanes<kFmt, false, T>(r, lanes, slices, per, grid, s);
+    const bool swap = !r.interleaved && r.rot == r.dim && r.dim == 8 * lanes;
+    if (swap && many) return rotate_lanes<kFmt, true, true, T>(r, lanes, slices, per, grid, s);
+    if (swap) return rotate_lanes<kFmt, true, false, T>(r, lanes, slices, per, grid, s);
+    if (many) return rotate_lanes<kFmt, false, true, T>(r, lanes, slices, per, grid, s);
+    return rotate_lanes<kFmt, false, false, T>(r, lanes, slices, per, grid, s);
 }
 
 template <int kFmt>
-hipError_t rotate_as(const MxRotate &r, int lanes, int slices, int per, dim3 grid, hipStream_t s)
+hipError_t rotate_as(const MxRotate &r, int lanes, bool many, int slices, int per, dim3 grid, hipStream_t s)
 {
-    if (r.dtype == MPQ_F32) return rotate_swap<kFmt, float>(r, lanes, slices, per, grid, s);
-    if (r.dtype == MPQ_F16) return rotate_swap<kFmt, _Float16>(r, lanes, slices, per, grid, s);
-    return rotate_swap<kFmt, __bf16>(r, lanes, slices, per, grid, s);
+    if (r.dtype == MPQ_F32) return rotate_swap<kFmt, float>(r, lanes, many, slices, per, grid, s);
+    if (r.dtype == MPQ_F16) return rotate_swap<kFmt, _Float16>(r, lanes, many, slices, per, grid, s);
+    return rotate_swap<kFmt, __bf16>(r, lanes, many, slices, per, grid, s);
 }
 
 }  // namespace
@@ -342,18 +361,24 @@ hipError_t rotate_as(const MxRotate &r, int lanes, int slices, int per, dim3 gri
 hipError_t launch_mx_rotate(const MxRotate &r, bool append, hipStream_t s)
 {
     if (r.n <= 0) return hipSuccess;
-    // lanes of a row, and heads that a wavefront has at a time
+    // lanes of a row, and rows that a wavefront has at a time
     const int quads = (r.dim + kMxBlock - 1) / kMxBlock, lanes = quads <= 1 ? 4 : quads <= 2 ? 8 : quads <= 4 ? 16 : 32;
-    const int at_once = kWave / lanes, passes = (r.heads + r.kv * (append ? 2 : 1) + at_once - 1) / at_once;
+    const int at_once = kWave / lanes, rows = r.heads + r.kv * (append ? 2 : 1);
+    // many: where tokens fill the GPU and one has few rows (append, 9 rows of 128 dims,
+    // 24480 tokens: 37 us, by a wavefront a token 68; 48 of 32, 5110: 19.5 and 23.7; but
+    // 48 of 128, 16384: 89 and 82)
+    const bool many = r.n >= 4096 && (rows + at_once - 1) / at_once <= 4;
+    const int step = many ? 1 : at_once, passes = (rows + step - 1) / step;
+    const int64_t shares = many ? (r.n + at_once - 1) / at_once : r.n;
     // 16 wavefronts a CU
-    const int wanted = (int)std::min((int64_t)passes, std::max((int64_t)1, 4096 / r.n));
+    const int wanted = (int)std::min((int64_t)passes, std::max((int64_t)1, 4096 / shares));
     const int each = (passes + wanted - 1) / wanted, slices = (passes + each - 1) / each;
-    const int64_t blocks = (r.n * slices + kWaves - 1) / kWaves;
+    const int64_t blocks = (shares * slices + kWaves - 1) / kWaves;
     const dim3 grid(grid_x(blocks), (unsigned)grid_rows(blocks));
     LaunchTimer timer(s, append ? "mx_append_kernel" : "mx_rotate_kernel");
-    if (!append) return rotate_as<-1>(r, lanes, slices, each * at_once, grid, s);
-    return r.c.fmt == kFp4 ? rotate_as<kFp4>(r, lanes, slices, each * at_once, grid, s)
-                           : rotate_as<kFp8>(r, lanes, slices, each * at_once, grid, s);
+    if (!append) return rotate_as<-1>(r, lanes, many, slices, each * step, grid, s);
+    return r.c.fmt == kFp4 ? rotate_as<kFp4>(r, lanes, many, slices, each * step, grid, s)
+                           : rotate_as<kFp8>(r, lanes, many, slices, each * step, grid, s);
 }
 
 }  // namespace mpq

@@ -164,7 +164,9 @@ def _freqs(rot, theta=10000.0):
 
 
 SHAPES = [(1, 1, 1, 1, 0), (1, 32, 8, 128, 128), (3, 2, 1, 2, 2), (5, 7, 1, 80, 40), (4, 3, 3, 33, 10), (9, 4, 2, 64, 64),
-          (17, 5, 5, 40, 20), (2, 6, 3, 256, 256), (33, 2, 2, 192, 96), (130, 8, 2, 96, 96), (7, 3, 1, 255, 254), (4, 2, 2, 8, 6)]
+          (17, 5, 5, 40, 20), (2, 6, 3, 256, 256), (33, 2, 2, 192, 96), (130, 8, 2, 96, 96), (7, 3, 1, 255, 254), (4, 2, 2, 8, 6),
+          # several tokens a wavefront
+          (4099, 2, 1, 128, 128), (4097, 3, 1, 80, 40), (4110, 1, 1, 256, 256), (4101, 5, 2, 30, 16), (4098, 2, 1, 64, 64)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -219,7 +221,8 @@ def test_rotate_leaves_the_rest():
 @pytest.mark.parametrize("fmt", ["fp4", "fp8"])
 @pytest.mark.parametrize("n,heads,kv,dim,rot,page", [(1, 8, 2, 128, 128, 16), (5, 7, 1, 80, 40, 48), (37, 2, 2, 33, 10, 16),
                                                      (130, 6, 3, 64, 64, 64), (20, 4, 4, 256, 128, 32), (3, 2, 1, 192, 0, 16),
-                                                     (9, 5, 5, 32, 32, 16), (12, 2, 1, 256, 256, 16)])
+                                                     (9, 5, 5, 32, 32, 16), (12, 2, 1, 256, 256, 16),
+                                                     (4099, 2, 1, 128, 128, 16), (4097, 1, 2, 80, 40, 48), (4101, 3, 2, 32, 32, 16)])
 def test_append(n, heads, kv, dim, rot, page, fmt, dtype):
     import torch
     from paper_2002_09049_amd import mpq

@@ -412,7 +412,8 @@ __device__ __forceinline__ void multiply_operands(const Operands<kTM, kTN> &o, c
 
 // The same with after(i, j) behind each product: what it issues has the time of one
 // product, so that little work behind every one hides where much behind every
-// fourth does not (a stage of 256 by 256 tiles 1540 cycles, so XX).
+// fourth does not (a stage of 256 by 256 tiles 1530 cycles, so 1440; its 32 products
+// take 1024).
 template <int kS, int kTM, int kTN, class After>
 __device__ __forceinline__ void multiply_spread(const Operands<kTM, kTN> &o, const Scales<kTM, kTN> &sc,
                                                 f32x16 (&acc)[kTM][kTN], After after)

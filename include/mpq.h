@@ -23,7 +23,8 @@
  *  - A layer with so many channels or weights that its launch would have 2^32
  *    threads is refused with MPQ_ERR_HIP (fits: 64 threads or more a channel;
  *    reconstruction: 2^36 weights; integer scales: 2^32 of them; of the
- *    microscaled calls only a product of 2^37 outputs and more).
+ *    microscaled calls only a product, of one matrix or by experts, of 2^37
+ *    outputs and more).
  *
  * Codes and scales (readings of the paper, shared with the test oracle)
  *  - bits b in [2, 8]; codes are the integers [-M, M] with M = 2^(b-1) - 1,

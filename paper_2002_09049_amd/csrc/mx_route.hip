@@ -35,7 +35,8 @@ constexpr int kThreads = 1024;
 constexpr int kMostExperts = 1024;
 
 // Tokens of a workgroup: a wavefront's each, or as many as a mask has bits.
-__host__ __device__ __forceinline__ int tokens_of(int64_t n) { return n > 64 && n <= 4096 ? 16 : 64; }
+constexpr int64_t kFew = 4096;
+__host__ __device__ __forceinline__ int tokens_of(int64_t n) { return n > 64 && n <= kFew ? 16 : 64; }
 
 // Bytes of a workgroup's counts.
 __host__ __device__ __forceinline__ int pitch_of(int experts) { return (experts + 3) / 4 * 4; }
@@ -431,8 +432,10 @@ size_t mx_route_bytes(int64_t n, int64_t experts)
 {
     const int64_t blocks = blocks_of(n);
     if (blocks <= 1) return 0;
-    return count_bytes(blocks, experts)
-           + (adds_inside(blocks, experts) ? 0 : (size_t)((blocks + 1) * experts) * sizeof(int32_t));
+    const size_t bytes = count_bytes(blocks, experts)
+                         + (adds_inside(blocks, experts) ? 0 : (size_t)((blocks + 1) * experts) * sizeof(int32_t));
+    // (a little past kFew workgroups are fewer: not below what fewer tokens take)
+    return n > kFew ? std::max(bytes, mx_route_bytes(kFew, experts)) : bytes;
 }
 
 hipError_t launch_mx_route(MxRoute r, void *space, hipStream_t s)

@@ -683,7 +683,8 @@ def mx_rotate(Q: torch.Tensor, K: torch.Tensor, positions: torch.Tensor, freqs: 
 
 
 def mx_route_workspace(n: int, experts: int, k: int) -> int:
-    """mpq_mx_route_workspace: the bytes of a workspace of mx_route."""
+    """mpq_mx_route_workspace: the bytes of a workspace of mx_route (enough for
+    fewer tokens too)."""
     v = load().mpq_mx_route_workspace(n, experts, k)
     if v < 0:
         _check(int(v))

@@ -129,6 +129,22 @@ def test_experts_refusals(mpq):
     assert mpq.mx_experts_workspace(30, 60, 3, 5, 40) >= 31 * (64 + 4)
 
 
+# about every number of tokens at which the work is cut in another way
+STEPS = sorted({0, 1 << 20} | {v for t in (1, 2, 4, 5, 16, 64, 256, 1023, 1024, 4096, 8192, 16384, 65472, 65536)
+                               for v in (t - 1, t, t + 1)})
+
+
+EXPERTS_OF_STEPS = [1, 2, 3, 8, 50, 64, 257, 600, 1000, 1024]
+
+
+@pytest.mark.parametrize("experts", EXPERTS_OF_STEPS)
+def test_a_routing_workspace_for_more_tokens_does_for_fewer(mpq, experts):
+    """What a server allocates for its longest step holds for every shorter one."""
+    for k in sorted({1, min(experts, 8)}):
+        sizes = [mpq.mx_route_workspace(n, experts, k) for n in STEPS]
+        assert sizes == sorted(sizes), (k, [n for n, a, b in zip(STEPS[1:], sizes, sizes[1:]) if b < a])
+
+
 def test_combine_refusals(mpq):
     lib = mpq.load()
     ok = dict(Y=64, yt=1, m=6, c=5, y_ld=5, place=64, weights=64, n=3, k=2, R=64, r_ld=5, Z=64, dtype=1, ld=5, stream=None)

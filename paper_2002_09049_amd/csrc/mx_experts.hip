@@ -514,14 +514,16 @@ hipError_t launch_few_rows(const MxExperts &g, int64_t pieces, hipStream_t s)
 
 }  // namespace
 
-// The quantized rows of X and one of zeros, the pieces, and the list of rows.
+// The quantized rows of X and one of zeros, the pieces, and the list of rows.  The
+// pieces are counted as the smallest ones, of 16 rows, whatever the way: so what a
+// call takes does not fall as n, m, experts, c or d grow.
 size_t mx_experts_bytes(int64_t n, int64_t m, int64_t experts, int64_t c, int64_t d)
 {
     const Way way = way_of(n, m, experts, c, d);
     if (way.rows == 0) return 0;
     const int64_t w = mx_row(d);
     return (size_t)((n + 1) * (w / 2) + ((n + 1) * (w / 32) + 15) / 16 * 16)
-           + sizeof(Piece) * (size_t)(1 + most_pieces(m, experts, way.rows)) + (size_t)m * sizeof(int32_t);
+           + sizeof(Piece) * (size_t)(1 + most_pieces(m, experts, 16)) + (size_t)m * sizeof(int32_t);
 }
 
 hipError_t launch_mx_experts(MxExperts g, const void *X, int dtype, int64_t x_ld, int64_t d, uint8_t *space, hipStream_t s)

@@ -723,7 +723,7 @@ def mx_route(logits: torch.Tensor, k: int, renorm: bool = True, stream=None, out
 
 def mx_experts_workspace(n: int, m: int, experts: int, c: int, d: int) -> int:
     """mpq_mx_experts_workspace: the bytes of a workspace of mx_experts with n
-    rows of X and m of Y."""
+    rows of X and m of Y (enough for fewer of both too)."""
     v = load().mpq_mx_experts_workspace(n, m, experts, c, d)
     if v < 0:
         _check(int(v))

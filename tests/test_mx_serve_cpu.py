@@ -145,6 +145,22 @@ def test_a_routing_workspace_for_more_tokens_does_for_fewer(mpq, experts):
         assert sizes == sorted(sizes), (k, [n for n, a, b in zip(STEPS[1:], sizes, sizes[1:]) if b < a])
 
 
+@pytest.mark.parametrize("experts", EXPERTS_OF_STEPS)
+def test_an_experts_workspace_for_more_rows_does_for_fewer(mpq, experts):
+    k = min(experts, 8)
+    for c, d in ((256, 256), (1000, 40), (95, 6623), (5632, 512), (2048, 4000)):
+        wide = -(-d // 128) * 128
+        fits = [n for n in STEPS if n * k <= 1 << 26 and (n + 1) * wide < 1 << 32]
+        sizes = [mpq.mx_experts_workspace(n, n * k, experts, c, d) for n in fits]
+        assert sizes == sorted(sizes), (c, d, [n for n, a, b in zip(fits[1:], sizes, sizes[1:]) if b < a])
+        for n in (1, 3, 4, 5, 300):   # more rows of the same tokens
+            sizes = [mpq.mx_experts_workspace(n, m, experts, c, d) for m in STEPS]
+            assert sizes == sorted(sizes), (n, c, d, [m for m, a, b in zip(STEPS[1:], sizes, sizes[1:]) if b < a])
+        for m in (8, 64, 65, 1000):   # more tokens of as many rows
+            sizes = [mpq.mx_experts_workspace(n, m, experts, c, d) for n in fits if n > 0]
+            assert sizes == sorted(sizes), (m, c, d)
+
+
 def test_combine_refusals(mpq):
     lib = mpq.load()
     ok = dict(Y=64, yt=1, m=6, c=5, y_ld=5, place=64, weights=64, n=3, k=2, R=64, r_ld=5, Z=64, dtype=1, ld=5, stream=None)

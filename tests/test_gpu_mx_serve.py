@@ -904,6 +904,58 @@ def test_calls_on_another_stream():
         assert torch.equal(a, b)
 
 
+def test_every_call_on_another_stream():
+    """With stream=, work and memory are the stream's: the same bits as on the
+    current one, which is busy.  All inputs are there before either pass, and each
+    pass has a page table, a cache and outputs of its own."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    rng = np.random.default_rng(9)
+    n, k, experts, c, d = 150, 2, 8, 96, 256
+    codes, scales = _weights(rng, experts, c, d)
+    X = _dev(_activations(rng, (n, d)), torch.bfloat16)
+    logits = _dev(rng.standard_normal((n, experts)), torch.float32)
+    Q, K, V = (_heads(rng, n, h, 64, "bf16", 0) for h in (4, 2, 2))
+    f = _dev(_freqs(64))
+    cached, fresh = _dev(np.array([5, 40, 0], np.int32)), _dev(np.array([50, 1, 99], np.int32))
+    held = np.full((3, 8), -1, np.int32)
+    held[0, 0], held[1, :3] = 60, (61, 62, 63)
+    free, taken = _dev(rng.permutation(60).astype(np.int32)), _dev(np.zeros(1, np.int32))
+    tables = [_dev(held) for _ in range(2)]
+    caches = [mpq.MXCache.empty(64, 16, 2, 64) for _ in range(2)]
+    for cache in caches:
+        for t in cache.tensors:
+            t.fill_(77)
+    stream = torch.cuda.Stream()
+    busy = torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+
+    def calls(table, cache, stream):
+        plan = mpq.mx_plan(cached, fresh, table, free, taken, 16, n, stream=stream)
+        slots, positions = plan[:2]
+        q = cache.append(Q, K, V, positions, slots, f, stream=stream)
+        turned = mpq.mx_rotate(Q, K, positions, f, stream=stream)
+        route = mpq.mx_route(logits, k, stream=stream)
+        y = mpq.mx_experts(X, codes, scales, route[4], route[2], k, stream=stream)
+        z = mpq.mx_combine(y, route[3], route[1], stream=stream)
+        return [*plan, table, q, *turned, *route, y, z, *cache.tensors]
+
+    for _ in range(10):
+        busy = busy @ busy * 1e-3
+    got = calls(tables[0], caches[0], stream)
+    with torch.cuda.stream(stream):   # (waits for this stream alone: the other is still busy)
+        there = [t.cpu() for t in got]
+    torch.cuda.synchronize()
+    want = calls(tables[1], caches[1], None)
+    torch.cuda.synchronize()
+    assert len(got) == len(want)
+    for i, (a, b, early) in enumerate(zip(want, got, there)):
+        assert torch.equal(a, b) and torch.equal(a.cpu(), early), i
+    slots, positions, starts, lengths, after, table = ref.plan(cached.tolist(), fresh.tolist(), held, free.tolist(), 0, 16, n)
+    for a, b in zip(got, (slots, positions, starts, lengths, [after], table)):
+        assert np.array_equal(a.cpu().numpy(), b)
+
+
 def test_refusals_of_the_binding():
     """Shapes, types and devices, before the library is called."""
     import torch

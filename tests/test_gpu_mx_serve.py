@@ -956,6 +956,29 @@ def test_every_call_on_another_stream():
         assert np.array_equal(a.cpu().numpy(), b)
 
 
+def test_one_workspace_for_steps_of_every_size():
+    """Allocated once, for the longest step: the shorter ones give what they give
+    with new memory."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    rng = np.random.default_rng(10)
+    experts, k, c, d = 1000, 3, 24, 130
+    codes, scales = _weights(rng, experts, c, d)
+    most = 4200
+    X = _dev(_activations(rng, (most, d)), torch.bfloat16)
+    logits = _dev(rng.standard_normal((most, experts)), torch.float32)
+    routing = torch.empty((mpq.mx_route_workspace(most, experts, k),), dtype=torch.uint8, device="cuda")
+    products = torch.empty((mpq.mx_experts_workspace(most, most * k, experts, c, d),), dtype=torch.uint8, device="cuda")
+    for n in (most, 4097, 4096, 4095, 700, 341, 65, 64, 5, 4, 1):
+        routing.fill_(n % 251)
+        products.fill_(n % 251)
+        got, want = mpq.mx_route(logits[:n], k, workspace=routing), mpq.mx_route(logits[:n], k)
+        for a, b in zip(got, want):
+            assert torch.equal(a, b), n
+        y = mpq.mx_experts(X[:n], codes, scales, got[4], got[2], k, workspace=products)
+        assert torch.equal(y, mpq.mx_experts(X[:n], codes, scales, got[4], got[2], k)), n
+
+
 def test_refusals_of_the_binding():
     """Shapes, types and devices, before the library is called."""
     import torch

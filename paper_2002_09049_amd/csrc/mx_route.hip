@@ -279,8 +279,12 @@ __global__ void __launch_bounds__(kThreads) mx_sum_kernel(const uint8_t *counts,
 
 // Each choice to its place.  kSummed: by mx_sum_kernel's sums; else this workgroup
 // adds up the counts itself, four experts a word: pairs of 16-bit sums, which
-// hold up to 1023 rows of 64.
-constexpr int kMostAdded = 1023;
+// hold up to 1023 rows of 64.  A word's rows are shared by up to kMostParts threads,
+// whose sums a thread an expert then adds one by one: as many as the workgroup
+// has threads for, and sums of no rows among them, took 21.6 us for 2 or 4 experts and 12.5
+// for 8, at 100 tokens or 16384, where 32 take 3.5 to 5.0 (16: as long, but 60000 tokens
+// of 8 experts 10.3 and 9.0; 64: 0.2 to 0.6 more).
+constexpr int kMostAdded = 1023, kMostParts = 32;
 template <bool kSummed>
 __global__ void __launch_bounds__(kThreads) mx_place_kernel(MxRoute r, int blocks, int of_block)
 {
@@ -293,7 +297,7 @@ __global__ void __launch_bounds__(kThreads) mx_place_kernel(MxRoute r, int block
     } else {
         // two words of pairs for the rows before, two for all
         __shared__ uint32_t part[4][kThreads];
-        const int words = pitch_of(r.experts) / 4, runs = kThreads / words;
+        const int words = pitch_of(r.experts) / 4, runs = min(min(kThreads / words, kMostParts), blocks);
         const int word = threadIdx.x % words, run = threadIdx.x / words, here = blockIdx.x;
         uint32_t even = 0, odd = 0, even_before = 0, odd_before = 0;
         if (run < runs) {

@@ -529,6 +529,26 @@ def test_route_long(n, experts, k, dtype):
         _check_long_route(x, k, renorm, mpq.mx_route(logits, k, renorm))
 
 
+@pytest.mark.parametrize("experts", [1, 2, 4, 5, 8, 33, 128])
+@pytest.mark.parametrize("n", [65, 100, 496, 513, 4096, 4097, 8200, 65472])
+def test_route_counts_of_few_and_many_workgroups(n, experts):
+    """Fewer workgroups' counts than threads to add them, as many, and more, of few
+    experts and many; and all tokens to one expert, whose sum takes 16 bits whole."""
+    import torch
+    from paper_2002_09049_amd import mpq
+    x = torch.randn((n, experts), generator=torch.Generator("cuda").manual_seed(n + experts), device="cuda")
+    crowd = torch.zeros_like(x)
+    crowd[:, experts // 2] = 1.0
+    for logits in (x, crowd):
+        k = min(2, experts)
+        chosen, _, order, place, offsets = mpq.mx_route(logits, k)
+        want = torch.sort(logits, dim=-1, descending=True, stable=True)[1][:, :k]
+        flat = want.reshape(-1)
+        assert torch.equal(chosen.long(), want) and torch.equal(order.long(), torch.argsort(flat, stable=True))
+        assert torch.equal(order.long()[place.reshape(-1).long()], torch.arange(n * k, device="cuda"))
+        assert offsets.tolist() == [0] + torch.cumsum(torch.bincount(flat, minlength=experts), 0).tolist()
+
+
 @pytest.mark.parametrize("n,experts,k,dtype", [(4096, 1000, 9, "f32"), (4095, 1024, 64, "bf16"), (70000, 50, 6, "f16"),
                                                (65473, 3, 2, "bf16"), (40000, 257, 8, "bf16"), (37777, 511, 10, "f32")])
 def test_route_counts_summed_apart(n, experts, k, dtype):

@@ -716,7 +716,7 @@ int mpq_mx_route(const void *logits, int dtype, int64_t n, int64_t experts, int6
  *   workspace_opt, workspace_bytes  as for mpq_mx_linear, of at least
  *               mpq_mx_experts_workspace(n, m, experts, c_out, d) bytes, which do
  *               for smaller n and m too.
- * How the work is cut follows from n, m, experts and c_out, and so do the last
+ * How the work is cut follows from n, m, experts, c_out and d, and so do the last
  * bits of a row; they do not depend on the other rows or on the groups' sizes.
  * Errors: MPQ_ERR_INVALID_ARG, MPQ_ERR_NOMEM, MPQ_ERR_HIP.
  */

@@ -206,7 +206,8 @@ __global__ void __launch_bounds__(256) mx_experts_tile_kernel(MxExperts g)
 // through LDS takes the ring's fourth buffer, and the rows of the one after while
 // this one is multiplied.  65536 rows for 64 experts, timed in turn with tiles of
 // 256 x 256 that do not stay: 5632 x 2048 551 us and 591, 2048 x 2816 285 and 305.
-// At 2.6 to 3.0 PFLOP/s the clock is 1.8 GHz, and 43% of the CUs' cycles are products.
+// 43% of the CUs' cycles are products, and the others are what bounds it: at the clock
+// that it runs at, 1.8 GHz, products alone would be 7.5 PFLOP/s, and it reaches 2.6 to 3.0.
 __global__ void __launch_bounds__(256) mx_experts_stay_kernel(MxExperts g)
 {
     constexpr int kTM = 4, kTN = 4, kBM = 64 * kTM, kBN = 64 * kTN, kRows = kBM + kBN;
@@ -422,6 +423,8 @@ hipError_t launch_token_split(const MxExperts &g, const T *X, int64_t x_ld, int 
 //   c 5632, d 2048  15.7 14.6 16.7 26.4      c 5632, d 8192   44.5 35.0 36.1 47.8
 // Four tokens (whose rows are quantized by every wavefront): c 256, d 2048 11.5 8.5
 // 7.4 9.3; c 1024, d 2048 12.5 14.0 18.0 23.2; c 2048, d 512 10.8 15.9 24.2 34.7.
+// (Three of 256 rows of W, 384 workgroups by eight: 8.8, and by four 7.3: there the
+// bound that one token's times give is too high.)
 template <class T>
 hipError_t launch_token(const MxExperts &g, const T *X, int64_t x_ld, int d, hipStream_t s)
 {
@@ -464,8 +467,10 @@ struct Way {
 
 // By a model of the times, us, as launch_mx_product's: a round of 256 tiles takes
 // its ends and its stages of K; of m rows of E experts about E (mean / rows + 1 / 2)
-// pieces come, at least E, and half a round is lost at the end.  Measured, us,
-// bf16, with the launch before (4 us and more), 64 experts of 2048 x 2048:
+// pieces come, at least E, and half a round is lost at the end.  The launch before
+// is not in it, as it is the same for all of them; the times measured have it (4 us
+// for few rows, 13 for 8192 of 2048, 17 for 4096 of 8192: of the 61.0 us below, where
+// the model gives the tiles 32, they take 48).  us, bf16, 64 experts of 2048 x 2048:
 //    mean rows    8    16    32    48    64    100   128   200   256   400   700  1024
 //    wavefronts  41.9  55.6  89.4   124   158   236   294   447   566   871  1505  2193
 //    128 x 64    33.4  33.0  36.9  39.0  40.6  51.0  56.2  76.9  94.9   137   235   324
@@ -476,9 +481,24 @@ struct Way {
 // themselves win while few rows have most experts to themselves (mean 1.2, 64 of
 // 2048 x 2816: 30.7, tiles 33.3; of 2048 x 8192: 71, 93; mean 4.8: 41.1 and 37.3)
 // or tiles are too few to fill the CUs (8 experts, mean 4, of 256 x 8192: 11.6,
-// 21.3; of 2048 x 2816: 12.0, 13.4).  Up to four tokens go in one launch, unless
-// several read much (four, 32 choices: 36 MB of W 12.8, in two launches 12.5; 196
-// MB 46.5, 36.4; 18 MB 10.5, 10.6; 9 MB 7.2, 9.5).
+// 21.3; of 2048 x 2816: 12.0, 13.4).
+//
+// Up to four tokens go in one launch, unless several read much of W.  64 experts, 8
+// choices, us in one launch and in two (each side forced, on the same kernels):
+//    c x d         one token    two           three         four
+//    1024 x 512    5.6   8.4    6.6   8.9     9.5   9.4     7.0   9.4
+//    1024 x 2048   6.3   9.2    8.4  10.9    12.9  13.6    12.2  14.4
+//    1024 x 8192  10.5  14.1   19.1  20.6    31.9  24.0    30.5  29.0
+//    2048 x 512    5.8   8.6    7.1   9.4    10.3  10.0    10.4  10.5
+//    2048 x 2048   7.4  10.6   12.2  14.0    20.0  17.2    20.6  17.3
+//    2048 x 8192  17.3  21.0   30.8  29.5    54.2  39.1    56.3  48.7
+//    5632 x 512    7.7   9.8   13.5  12.4    17.9  14.3    22.1  16.8
+//    5632 x 2048  14.3  17.0   29.2  25.4    37.6  30.8    45.9  36.0
+//    5632 x 8192  34.9  40.6   90.4  68.0     130   101     182   131
+// (256 rows of W: one launch is the faster throughout.)  40 MB of W leaves three on the
+// slower side: 5632 x 512 with two and three tokens (25 and 37 MB: 1.10 and 1.24 of
+// the faster one) and 1024 x 8192 with two (71 MB: 1.07).  What the bytes do not
+// count is that each of c / 64 times m workgroups quantizes its rows itself.
 Way way_of(int64_t n, int64_t m, int64_t experts, int64_t c, int64_t d)
 {
     const double weights = (double)m * (double)c * (double)mx_row(d) * 17.0 / 32.0;

@@ -1,15 +1,18 @@
-// Where the product's kernels load a stage's codes from: byte offsets into a
-// buffer that begins at the workgroup's first row and ends behind the last row
-// that it has (mx_product.hip).  A lane of a row past that end, and every lane
-// of a stage past the rows' end, gets an offset outside the buffer, whose loads
-// give zeros.  tests/host/mx_stage_host.cpp goes through them on the CPU.
+// Where the products' kernels (mx_product.hpp, mx_experts.hip) load a stage's codes
+// from: byte offsets into a buffer that begins at the workgroup's first row and ends
+// behind the last row that it has, or, where rows are gathered, holds all rows of X.
+// A lane of a row past the end, and every lane of a stage past the rows' end, gets
+// an offset outside the buffer, whose loads give zeros.  tests/host/mx_stage_host.cpp
+// and mx_gather_host.cpp go through them on the CPU.
 #pragma once
 
 #include <stdint.h>
 
 namespace mpq {
 
-constexpr uint32_t kOutside = 0x80000000u;   // past every buffer (256 rows of at most 2^21 bytes)
+// Past every buffer: 256 rows of at most 2^21 bytes, and of gathered rows 2^31 - 1
+// bytes, above which mpq_mx_experts refuses X.
+constexpr uint32_t kOutside = 0x80000000u;
 
 // Tiles: stages of 128 elements.  Load k of a wavefront whose rows begin at
 // row0 covers 16 rows, lane l row row0 + 16 k + l / 4; its offset is the sum of

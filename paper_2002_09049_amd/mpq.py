@@ -582,7 +582,8 @@ def mx_plan(cached: torch.Tensor, fresh: torch.Tensor, page_table: torch.Tensor,
     given away.  Returns (slots [max_tokens] int64, positions [max_tokens] int32,
     starts [batch + 1] int32, lengths [batch] int32, taken [1] int32 for the next
     step; more than there are free pages if some are missing), or writes them to
-    the five tensors of out."""
+    the five tensors of out.  New positions, starts, lengths and taken are parts of
+    one allocation: whoever keeps one of them keeps 4 * max_tokens bytes and more."""
     if cached.dim() != 1 or fresh.shape != cached.shape:
         raise ValueError("cached and fresh must be [batch]")
     batch = cached.shape[0]
